@@ -68,7 +68,8 @@ typedef enum {
     ZNNI_ERR_WORKSPACE = -4,        /* workspace smaller than znni_conv3d_fft_workspace reports            */
     ZNNI_ERR_FLAGS = -5,            /* unknown flag bit, or more than one of the ZNNI_MAC_* bits           */
     ZNNI_ERR_HIP = -6,              /* a HIP call or kernel launch failed                                  */
-    ZNNI_ERR_ALIGN = -7             /* a device pointer is not 16-byte aligned (workspace: 256-byte)       */
+    ZNNI_ERR_ALIGN = -7,            /* a device pointer is not 16-byte aligned (workspace: 256-byte)       */
+    ZNNI_ERR_TYPE = -8              /* not one of znni_type                                                */
 } znni_status;
 
 /* flags */
@@ -326,6 +327,103 @@ znni_status znni_mpf(int S, int f, const int n[3], const int p[3], const float* 
  * Needs no workspace; asynchronous on `stream`.
  */
 znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const float* in, float* out, void* stream);
+
+/*
+ * Attention over the voxels of a volume as tokens: what follows a convolutional stem.  A map [f][nx][ny][nz] read voxel by
+ * voxel, x slowest, is a sequence whose near past is the last slabs (a sliding window) and in which every token has three
+ * coordinates (rotary positions with several axes); keys and values of slabs that went before are kept in 8 bits.
+ *
+ * Conventions, besides those at the top of this file:
+ *   - `type` is a znni_type, the type of all tensors of heads of a call; scores, softmax statistics and sums are fp32.
+ *   - A tensor of heads is a znni_heads: element (token t, head h, d) lies at data[t * token + h * head + d], strides in
+ *     elements.  Data 16-byte aligned, strides multiples of 16 bytes (zero and negative ones included for what is read),
+ *     D a multiple of 8.  ZNNI_ERR_ALIGN, ZNNI_ERR_UNSUPPORTED_SIZE.
+ *   - Query head h reads key and value head h / (Hq / Hk); Hk divides Hq.  ZNNI_ERR_SHAPE.
+ *   - A row at position p sees key j if j <= p + right and (j >= p - left or j < sinks): the window, and the first tokens,
+ *     which stay visible to all rows that come after them.  ZNNI_ALL for left or right: no end.  What lies in keys and
+ *     values that a row does not see, infinities and NaN included, has no influence on it.  A row that sees nothing, or whose weights
+ *     are all zero, is zero.
+ *   - Lengths of zero are fine; a call without tokens launches nothing.
+ *   - Results are deterministic; a row's depends on how many keys its call says there may be at most (max_k, max_len), by
+ *     rounding only.
+ */
+typedef enum { ZNNI_F32 = 0, ZNNI_BF16 = 1, ZNNI_F16 = 2 } znni_type;
+
+typedef struct {
+    void* data;
+    long long token, head;
+} znni_heads;
+
+#define ZNNI_ALL 2147483647
+
+/*
+ * Rotary positions with several axes (x, y, z of a volume; time).  The first R = sum of sections[] pairs of every head are
+ * turned, pair j by the angle pos[t][a] * freq[j], where a is the axis whose section holds j (sections in order, each >= 0):
+ *     (u, v) -> (u cos - v sin, u sin + v cos)
+ * pair j = elements (j, R + j), or (2j, 2j + 1) with ZNNI_ROPE_NEIGHBOURS; the elements from 2R on are copied.
+ *   pos [T][axes] signed (the negative turns back, which is the gradient too), freq [R]: device, 4-byte aligned
+ *   q [T][Hq][D] -> q_out, k [T][Hk][D] -> k_out (Hk = 0: no k, pointers may be NULL); an output may be its input
+ *   D <= 512, 1 <= axes <= ZNNI_ROPE_MAX_AXES, 2R <= D
+ * Angles are reduced in 64 bits, so that long positions lose nothing.  No workspace; asynchronous on `stream`.
+ */
+#define ZNNI_ROPE_MAX_AXES 4
+enum { ZNNI_ROPE_NEIGHBOURS = 1u };
+
+znni_status znni_rope_axes(int type, int T, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const int* pos,
+                           const float* freq, int axes, const int* sections, const znni_heads* q_out, const znni_heads* k_out,
+                           unsigned flags, void* stream);
+
+/*
+ * Attention with a sliding window and first tokens that stay visible, over B sequences of any lengths, one behind the other:
+ *   q [cu_q[B]][Hq][D], k and v [cu_k[B]][Hk][D] -> out as q; cu_q, cu_k [B+1] device: where each sequence starts
+ *   max_q, max_k: no sequence is longer (host; what the launch is made for.  Rows past max_q are not written.)
+ * Query i of a sequence of nq queries and nk keys stands at position p = nk - nq + i (the last query at the last key);
+ * with fewer keys than queries the first rows may see none.  out = sum of v over the keys that the row sees, weighted by
+ * softmax(scale q.k).  D <= 128.  left, right, sinks >= 0.  out must not overlap the inputs.
+ * The workspace (znni_attn_window_workspace bytes, may be zero: then NULL will do; 256-byte aligned) holds the parts of rows
+ * whose keys are split over workgroups.
+ */
+znni_status znni_attn_window_workspace(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks,
+                                       size_t* bytes);
+
+znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                             const int* cu_q, const int* cu_k, int max_q, int max_k, int left, int right, int sinks, float scale,
+                             const znni_heads* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The 8-bit cache of keys and values.  Tokens of a sequence lie in pages of ZNNI_KV8_PAGE; table [B][width] (device) names
+ * the pages of each sequence in order.  A page holds e4m3 codes (4 exponent, 3 mantissa bits, largest 448), a value is
+ * code * scale, one power of two as scale for the keys and one for the values of a page and head:
+ *   kcodes [pages][Hk][ZNNI_KV8_PAGE][D]      vcodes [pages][Hk][D][ZNNI_KV8_PAGE]      scales [pages][Hk][2] fp32 (k, v)
+ * (values with the tokens innermost: a token's product with them then reads 16 tokens at once.)  Codes 16-byte aligned,
+ * D a multiple of 8 up to 128.  Slots behind a sequence's last token may hold anything; pages that no row sees are not read
+ * and their table entries may be anything; an entry outside [0, pages) that is reached counts as a page that no row sees.
+ *
+ * znni_kv8_append puts k, v [cu[B]][Hk][D] behind the start[b] tokens that sequence b holds already (cu [B+1], start [B],
+ * device; max_new: no sequence gets more).  scale = 2^E with the least E for which the largest finite magnitude among the page's
+ * tokens is at most 448 * 2^E, E >= -126, by the tokens that are there: a page that is filled further keeps its scale if the new
+ * tokens fit and else gets the larger one, its older codes rounded once more (exact above the type's subnormals).  Rounding
+ * to nearest, ties to even; infinities become the largest code, NaN stay.  No page may be named twice by what a call writes.
+ * Tokens past the table's width or in pages outside [0, pages) are dropped.
+ */
+#define ZNNI_KV8_PAGE 64
+
+znni_status znni_kv8_append(int type, int B, int Hk, int D, const znni_heads* k, const znni_heads* v, const int* cu, const int* start,
+                            int max_new, unsigned char* kcodes, unsigned char* vcodes, float* scales, int pages, const int* table,
+                            int width, void* stream);
+
+/*
+ * Attention of the last Lq tokens of each of B sequences over the cache: q [B*Lq][Hq][D] -> out, token i of sequence b at
+ * position p = lens[b] - Lq + i (rows before the first token are zero), visibility with right = 0.  lens [B] device, counted
+ * as at most width * ZNNI_KV8_PAGE; max_len: no sequence is longer (host; the launch is made for it).  Keys and values are taken as they stand in the cache.
+ * Other arguments as for znni_attn_window and znni_kv8_append.
+ */
+znni_status znni_kv8_attn_workspace(int type, int B, int Lq, int Hq, int Hk, int D, int max_len, int left, int sinks, size_t* bytes);
+
+znni_status znni_kv8_attn(int type, int B, int Lq, int Hq, int Hk, int D, const znni_heads* q, const unsigned char* kcodes,
+                          const unsigned char* vcodes, const float* scales, int pages, const int* table, int width,
+                          const int* lens, int max_len, int left, int sinks, float scale, const znni_heads* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid: a plain device-to-device copy of `bytes` bytes (a multiple of 16; both pointers 16-byte

@@ -688,19 +688,20 @@ using namespace znni;
 
 extern "C" {
 
-int znni_version(void) { return 200; }
+int znni_version(void) { return 300; }
 
 const char* znni_status_string(int st)
 {
     switch (st) {
         case ZNNI_OK: return "ok";
         case ZNNI_ERR_NULL: return "a required pointer is NULL";
-        case ZNNI_ERR_SHAPE: return "bad layer shape (need S,f,f' >= 1 and 1 <= k <= n on every axis, counts within launch limits)";
-        case ZNNI_ERR_UNSUPPORTED_SIZE: return "no supported transform size for this image edge";
+        case ZNNI_ERR_SHAPE: return "bad shape (layers: need S,f,f' >= 1 and 1 <= k <= n on every axis, counts within launch limits; attention: see the call's limits)";
+        case ZNNI_ERR_UNSUPPORTED_SIZE: return "no supported transform size for this image edge, or head size that the operator does not take";
         case ZNNI_ERR_WORKSPACE: return "workspace too small";
         case ZNNI_ERR_FLAGS: return "unknown flag bit, or more than one multiply-accumulate form requested";
         case ZNNI_ERR_HIP: return "HIP call or kernel launch failed";
         case ZNNI_ERR_ALIGN: return "device pointer not sufficiently aligned";
+        case ZNNI_ERR_TYPE: return "unknown element type";
     }
     return "unknown status";
 }

@@ -1,0 +1,86 @@
+"""Rotary positions with several axes against the formula in 64 bits: one rounding to the type, sines and cosines in fp32."""
+import pytest
+import torch
+
+import attention_ref as R
+from paper_1606_05688_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _case(seed, T, Hq, Hk, D, sections, dtype, far=300):
+    g = torch.Generator().manual_seed(seed)
+    q, k = (torch.randn(T, h, D, generator=g).to(dtype) for h in (Hq, Hk))
+    pos = torch.randint(-far, far, (T, len(sections)), generator=g, dtype=torch.int32)
+    freq = torch.cat([10000.0 ** (-torch.arange(n) / n) for n in sections] + [torch.zeros(0)]).float()
+    return q, k, pos, freq
+
+
+def _tol(x, exp, dtype):
+    # products and their sum in fp32 from factors good to 2^-22 (sine, cosine and the reduced angle, at most pi, in fp32), one rounding
+    big = x.double().abs().amax(-1, keepdim=True)
+    return R.UNIT[dtype] * exp.abs() + 2.0 ** -20 * big + 1e-12
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("pairing", ["halves", "neighbours"])
+@pytest.mark.parametrize("T,Hq,Hk,D,sections", [
+    (1, 1, 1, 8, (4,)), (3, 2, 1, 16, (2, 3, 3)), (100, 16, 4, 128, (16, 24, 24)), (77, 5, 5, 40, (5, 6, 6)), (1025, 3, 1, 64, (7, 0, 9)),
+    (9, 2, 2, 512, (64, 64, 64, 64)), (5, 33, 3, 24, (0,)), (2, 1, 1, 136, (40,)), (4000, 2, 1, 32, (8,)),
+])
+def test_against_the_formula(dtype, pairing, T, Hq, Hk, D, sections):
+    print(f"[rope] {dtype} {pairing} {(T, Hq, Hk, D, sections)}", flush=True)
+    q, k, pos, freq = _case(T + D, T, Hq, Hk, D, sections, dtype)
+    got = B.znni_rope_axes(q.to(DEV), k.to(DEV), pos.to(DEV), freq.to(DEV), sections, pairing=pairing)
+    for x, y in zip((q, k), got):
+        exp = R.rope(x.double(), pos, freq, sections, pairing)
+        R.check(y, exp, _tol(x, exp, dtype))
+        assert torch.equal(y.cpu()[..., 2 * sum(sections):], x[..., 2 * sum(sections):])
+
+
+def test_long_positions_keep_their_angle():
+    """Positions of 2^30: the angle is reduced in 64 bits, where a product in fp32 would be off by tens of turns."""
+    q, k, pos, freq = _case(1, 64, 2, 1, 64, (16, 16), torch.float32, far=1 << 30)
+    got, _ = B.znni_rope_axes(q.to(DEV), k.to(DEV), pos.to(DEV), freq.to(DEV), (16, 16))
+    exp = R.rope(q.double(), pos, freq, (16, 16), "halves")
+    # 2^30 radians are 1.7e8 turns, whose product in 64 bits is off by 2^-53 of that: under 2^-20 of a radian
+    R.check(got, exp, _tol(q, exp, torch.float32))
+
+
+@pytest.mark.parametrize("pairing,sections", [("halves", (4, 4, 8)), ("halves", (5, 4, 4)), ("neighbours", (5, 4, 4))])
+def test_strides_in_place_and_queries_alone(pairing, sections):
+    g = torch.Generator().manual_seed(5)
+    T, H, D = 37, 6, 40
+    packed = torch.randn(T, H + 2, D, generator=g).bfloat16()
+    pos = torch.randint(0, 50, (T, 3), generator=g, dtype=torch.int32)
+    freq = torch.rand(sum(sections), generator=g)
+    exp = R.rope(packed.double(), pos, freq, sections, pairing)
+    dev, p, f = packed.to(DEV), pos.to(DEV), freq.to(DEV)
+    q, k = dev[:, :H - 2], dev[:, H - 2:H]
+    heads_first = torch.empty(H - 2, T, D, dtype=torch.bfloat16, device=DEV)
+    B.znni_rope_axes(q, None, p, f, sections, pairing=pairing, out_q=heads_first.transpose(0, 1))
+    tol = _tol(packed, exp, torch.bfloat16)
+    R.check(heads_first.transpose(0, 1), exp[:, :H - 2], tol[:, :H - 2])
+    B.znni_rope_axes(q, k, p, f, sections, pairing=pairing, out_q=q, out_k=k)                 # in place
+    R.check(dev[:, :H], exp[:, :H], tol[:, :H])
+    assert torch.equal(dev[:, H:].cpu(), packed[:, H:])                                       # what lies beside it stays
+    zeros = B.znni_rope_axes(dev[:0], dev[:0], p[:0], f, sections)
+    assert zeros[0].shape == (0, H + 2, D)
+
+
+def test_negative_positions_turn_back_and_are_the_gradient():
+    """<R(p) x, y> = <x, R(-p) y>, and differences of <R(p) x, y> along x are R(-p) y."""
+    q, k, pos, freq = _case(8, 20, 4, 4, 64, (10, 10, 12), torch.float32)
+    x, y, p, f = q.to(DEV), k.to(DEV), pos.to(DEV), freq.to(DEV)
+    there, _ = B.znni_rope_axes(x, None, p, f, (10, 10, 12))
+    back, _ = B.znni_rope_axes(there, None, -p, f, (10, 10, 12))
+    assert (back - x).abs().max() <= 2.0 ** -19 * x.abs().max()
+    grad, _ = B.znni_rope_axes(y, None, -p, f, (10, 10, 12))
+    g = torch.Generator().manual_seed(2)
+    for _ in range(5):
+        d = torch.randn(q.shape, generator=g).to(DEV)
+        up, _ = B.znni_rope_axes(x + 0.5 * d, None, p, f, (10, 10, 12))
+        down, _ = B.znni_rope_axes(x - 0.5 * d, None, p, f, (10, 10, 12))
+        slope = ((up.double() - down.double()) * y.double()).sum()
+        assert abs(slope - (grad.double() * d.double()).sum()) <= 2.0 ** -18 * (y.abs().double() * 2 * (x.abs() + d.abs()).amax(-1, keepdim=True)).sum()
