@@ -1,7 +1,7 @@
 // kv8_attn.hip -- attention of the last tokens of sequences over the 8-bit cache.
 //
 // Bound by memory: every code of a visible page is read once.  A wave has sixteen rows (a token's heads that share a key
-// and value head, and the tokens after it) and walks pages of its own; four waves of a workgroup take turns in a part of
+// and value head, and the tokens after it) and walks pages of its own; eight waves of a workgroup take turns in a part of
 // the pages, several workgroups share a sequence, a second kernel joins their parts.  Per page, on 16x16x32 products:
 //   scores^T [64 keys][16 rows] = K Q^T, keys ordered so that a lane's 16 scores of its row are 16 keys that follow each
 //   other: then the weights are the right operand of  out^T [D][16 rows] = V^T W^T  as they stand, and V^T's operand is
@@ -29,7 +29,7 @@ struct Kv8Args {
     float* parts;        // [B][Hk][row tile][splits][16 rows][D], then as many [16 rows][2]: maximum (in powers of two) and sum
 };
 
-constexpr int KV8_WAVES = 4, KV8_ROWS = 16;
+constexpr int KV8_WAVES = 8, KV8_ROWS = 16;
 
 // bf16 terms that hold a query (exactly) and a weight (to the type's last bit and more)
 template <typename T> struct Terms;
@@ -123,7 +123,7 @@ __device__ inline unsigned nan_codes(unsigned x)       // bit 7 of every byte th
 }
 
 template <typename T, int NC, bool FULL>
-__global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8(Kv8Args a, Heads<const T> q, Heads<T> out)
+__global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8(Kv8Args a, Heads<const T> q, Heads<T> out)
 {
     constexpr int NX = 2 * NC, NQ = Terms<T>::q, NW = Terms<T>::w, DP = 32 * NC, LD = DP + 4;
     __shared__ __align__(16) float acc_s[KV8_WAVES][KV8_ROWS][LD];
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * KV8_WAVES, 2) void k_kv8(Kv8Args a, Heads<cons
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
 
-    // the four waves' parts of a row
+    // the waves' parts of a row
     if (u == 0) { top_s[wave][r] = top; sum_s[wave][r] = sum; }
 #pragma unroll
     for (int x = 0; x < NX; ++x) *(f32x4*)&acc_s[wave][r][16 * x + 4 * u] = acc[x];
@@ -362,16 +362,20 @@ __global__ __launch_bounds__(256) void k_kv8_join(Kv8Args a, int B, Heads<T> out
     if (l + 64 < a.D) y[l + 64] = (T)(n == 0.f ? 0.f : o1 / n);
 }
 
-// How many workgroups share a sequence's pages: about three workgroups a compute unit in all, no wave with less than a page.
+// How many workgroups share a sequence's pages.  A call whose waves have two pages at most is not split, which saves the
+// launch that joins (13 pages of 4 heads: 8.7 against 10.1 us).  Else a workgroup for every compute unit, none with less than a page a wave
+// (16 heads of 47 pages: 24.6 us unsplit, 15.0 split), and more of them where sequences are long, since lengths may differ (64
+// sequences of up to 16384 tokens: 128 us unsplit, 116 in four; 64 of 8192 each 100 and 106).
 static int kv8_splits(int B, int Lq, int Hq, int Hk, int max_len, int left, int sinks)
 {
     const long long tiles = ((long long)Lq * (Hq / Hk) + KV8_ROWS - 1) / KV8_ROWS, groups = tiles * Hk * B;
     const long long seen = (long long)left + Lq < max_len ? (long long)left + Lq + (sinks < max_len ? sinks : max_len) : max_len;
-    const long long pages = ((seen < max_len ? seen : max_len) + PAGE - 1) / PAGE + 1;
-    long long n = (768 + groups - 1) / groups;
-    const long long most = (pages + KV8_WAVES - 1) / KV8_WAVES;
-    if (n > most) n = most;
-    return n < 1 ? 1 : (int)n;
+    const long long pages = ((seen < max_len ? seen : max_len) + PAGE - 1) / PAGE;
+    if (pages <= 2 * KV8_WAVES) return 1;
+    const long long fill = (256 + groups - 1) / groups, most = (pages + KV8_WAVES - 1) / KV8_WAVES;
+    const long long even = pages / 64 < 1024 / groups ? pages / 64 : 1024 / groups;
+    const long long n = fill > even ? fill : even;
+    return (int)(n < most ? n : most);
 }
 
 static size_t kv8_parts(int B, int Lq, int Hq, int Hk, int D, int splits)
