@@ -1,7 +1,19 @@
 // attn_window.hip -- attention with a sliding window and first tokens that stay visible, over sequences of any lengths.
+//
+// A workgroup has 128 rows of one key and value head: tokens times the query heads that share it, so that keys and values
+// are read once for all of them; a wave has 32 rows.  It walks the key tiles that any row sees (sinks, then the window),
+// double-buffered in LDS, loads going from memory to LDS without registers in between.  Per tile, on 32x32 products:
+//   scores^T [keys][32 rows] = K Q^T: a lane has one row, half of its scores; maximum and weights are lane-local but for one
+//   exchange; the weights as they stand are the right operand of  out^T [D][32 rows] += V^T W^T.
+// V^T's operand: 16-bit types by transposing LDS reads, fp32 (products of fp32) by plain ones, keys permuted to match.
+// Rows in LDS are permuted by 16-byte chunks so that neither kind of read meets a bank twice.
 #include "attn_common.h"
+#include "attn_join.h"
 
 namespace znni {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct AttnArgs {
     int Hq, Hk, D;
@@ -9,77 +21,388 @@ struct AttnArgs {
     const int* cu_k;
     Window w;
     float scale;
+    int B, max_q, tiles, splits, tile_rows;     // row tiles of a sequence, workgroups that share a tile's keys, rows of a tile in `parts`
+    float* parts;
+    float2* stats;
 };
 
-constexpr int AROW_THREADS = 256;
+constexpr int BM = 128, ATTN_THREADS = 256;
 
-// One workgroup a row and head, as the formula has it: scores of 256 keys, running maximum and sum, weighted values.
-template <typename T>
-__global__ __launch_bounds__(AROW_THREADS) void k_attn_rows(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
+template <typename T, int NC>
+struct AttnTile {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int BN = F32 ? 32 : 64;                       // keys
+    static constexpr int EC = 16 / sizeof(T);                      // elements of a 16-byte chunk
+    static constexpr int RS = NC == 3 ? 128 : 32 * NC;             // elements of a row in LDS
+    static constexpr int CR = RS / EC;                             // its chunks
+    static constexpr int PER = BN * CR / ATTN_THREADS;             // chunks a thread brings
+    // Chunk c of key j lies at c ^ swizzle(j).  Scores read one chunk of 32 keys, 16 bytes a lane: 256 bytes of
+    // consecutive keys get different places; values read, 16-bit: four keys, 64 bytes each, fp32: two keys four apart, 128 bytes each.
+    __device__ static int swizzle_k(int j) { return CR >= 16 ? j & 15 : CR == 8 ? j >> 1 & 7 : j >> 2 & 3; }
+    __device__ static int swizzle_v(int j)
+    {
+        if (F32) return CR >= 16 ? (j >> 2 & 1) << 3 : 0;
+        return CR == 16 ? (j & 3) << 2 : CR == 8 ? (j >> 1 & 1) << 2 : 0;
+    }
+};
+
+__device__ inline void to_lds(const void* src, void* dst)
 {
-    __shared__ float qs[ATTN_DMAX], p[AROW_THREADS], red[AROW_THREADS / 64], sum2[ATTN_DMAX];
-    const int b = blockIdx.z, h = blockIdx.y, i = blockIdx.x, t = threadIdx.x;
-    const int nq = a.cu_q[b + 1] - a.cu_q[b], nk = a.cu_k[b + 1] - a.cu_k[b];
-    if (i >= nq) return;
-    const int hk = h / (a.Hq / a.Hk);
-    const long long pos = (long long)nk - nq + i, k0 = a.cu_k[b];
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+__device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename T>
+struct Mfma;
+template <>
+struct Mfma<bf16> {
+    typedef bf16 V __attribute__((ext_vector_type(8)));
+    typedef bf16 V4 __attribute__((ext_vector_type(4)));
+    __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    __device__ static bool odd(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u); }
+};
+template <>
+struct Mfma<f16> {
+    typedef f16 V __attribute__((ext_vector_type(8)));
+    typedef f16 V4 __attribute__((ext_vector_type(4)));
+    __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    __device__ static bool odd(unsigned x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
+    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7c00u) == 0x7c00u ? 0u : x & 0xffffu) | ((x & 0x7c000000u) == 0x7c000000u ? 0u : x & 0xffff0000u); }
+};
+template <>
+struct Mfma<float> {
+    typedef float V __attribute__((ext_vector_type(4)));
+    __device__ static f32x16 mul(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+    __device__ static bool odd(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u; }
+    __device__ static unsigned cleared(unsigned x) { return odd(x) ? 0u : x; }
+};
+
+// Key tiles that rows at positions p0 .. p1 see: those of sinks alone, then those of the window.
+template <int BN>
+struct KeyTiles {
+    int sink_tiles, first, n;
+    __device__ KeyTiles(long long p0, long long p1, int nk, const Window& w)
+    {
+        int lo, hi, x, y;
+        window_of(p0, nk, w, &lo, &x);
+        window_of(p1, nk, w, &y, &hi);
+        first = lo / BN;
+        sink_tiles = min((min(w.sinks, hi + 1) + BN - 1) / BN, first);
+        n = hi < lo ? sink_tiles : sink_tiles + hi / BN - first + 1;
+    }
+    __device__ int base(int i) const { return (i < sink_tiles ? i : first + i - sink_tiles) * BN; }
+};
+
+// Whether rows at p0 .. p1 all see keys j0 .. j0 + n - 1, and whether any sees any of them.
+__device__ inline bool all_see(long long p0, long long p1, int j0, int n, const Window& w)
+{
+    return j0 + n - 1 <= p0 + w.right && (j0 >= p1 - w.left || j0 + n <= w.sinks);
+}
+__device__ inline bool any_sees(long long p0, long long p1, int j0, int n, const Window& w)
+{
+    return p1 >= p0 && j0 <= p1 + w.right && (j0 + n - 1 >= p0 - w.left || j0 < w.sinks);
+}
+
+template <typename T, int NC>
+__global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
+{
+    using G = AttnTile<T, NC>;
+    using M = Mfma<T>;
+    constexpr bool F32 = G::F32;
+    constexpr int BN = G::BN, KT = BN / 32, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
+    __shared__ __align__(1024) T ks[2][BN * RS];
+    __shared__ __align__(1024) T vs[2][BN * RS];
+
+    int id = blockIdx.x;
+    const int split = id % a.splits; id /= a.splits;
+    const int tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
+    const int hk = id % a.Hk, b = id / a.Hk;
+    const int q0 = a.cu_q[b], nq = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
+    const int group = a.Hq / a.Hk;
+    const long long rows = (long long)min(nq, a.max_q) * group, row0 = (long long)tile * BM;
+    if (row0 >= rows) return;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
+    const long long base = (long long)nk - nq, last = min(row0 + BM, rows) - 1;
+    const long long pb0 = base + row0 / group, pb1 = base + last / group;              // positions of the workgroup
+    const long long wrow0 = row0 + wave * 32, wlast = min(wrow0 + 31, rows - 1);
+    const bool has = wrow0 < rows;
+    const long long p0 = has ? base + wrow0 / group : 0, p1 = has ? base + wlast / group : -1;       // of the wave
+    const long long row = min(wrow0 + c32, rows - 1);
+    const long long pos = base + row / group;                                          // of the lane
     int lo, hi;
     window_of(pos, nk, a.w, &lo, &hi);
-    const int first = min(min(a.w.sinks, lo), hi + 1), n = first + max(0, hi - lo + 1);
-    const T* qr = q.row(a.cu_q[b] + (long long)i, h);
-    for (int d = t; d < a.D; d += AROW_THREADS) qs[d] = (float)qr[d];
-    float m = -INFINITY, l = 0.f, acc = 0.f;
-    const int d = t & (ATTN_DMAX - 1), half = t / ATTN_DMAX;
-    for (int j0 = 0; j0 < n; j0 += AROW_THREADS) {
-        const int j = j0 + t, key = j < first ? j : lo + j - first;
-        float s = -INFINITY;
-        __syncthreads();
-        if (j < n) {
-            const T* kr = k.row(k0 + key, hk);
-            s = 0.f;
-            for (int e = 0; e < a.D; ++e) s += qs[e] * (float)kr[e];
-            s *= a.scale;
+    const int qh = hk * group + (int)(row % group);
+
+    const KeyTiles<BN> tiles(pb0, pb1, nk, a.w);
+    const int per = (tiles.n + a.splits - 1) / a.splits, begin = split * per, end = min(tiles.n, begin + per);
+
+    // what this thread brings of a tile: PER chunks of keys and of values, 64 consecutive ones a wave
+    const T* kp = k.row(k0, hk);
+    const T* vp = v.row(k0, hk);
+    const bool near = k.token >= 0 && v.token >= 0 && k.token < (1 << 22) && v.token < (1 << 22);
+    unsigned ko[PER], vo[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int slot = (i * 4 + wave) * 64 + l, j = slot / CR, c = slot % CR;
+        ko[i] = ((unsigned)j * (unsigned)k.token + (c ^ G::swizzle_k(j)) * EC) * (unsigned)sizeof(T);
+        vo[i] = ((unsigned)j * (unsigned)v.token + (c ^ G::swizzle_v(j)) * EC) * (unsigned)sizeof(T);
+    }
+    auto bring = [&](int buf, int j0) {
+        const bool fast = near && j0 + BN <= nk;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = (i * 4 + wave) * 64, slot = at + l, j = slot / CR, ck = slot % CR ^ G::swizzle_k(j), cv = slot % CR ^ G::swizzle_v(j);
+            const long long jj = min(j0 + j, nk - 1);
+            const T* ks_src = fast ? (const T*)((const char*)(kp + j0 * k.token) + ko[i]) : kp + jj * k.token + ck * EC;
+            const T* vs_src = fast ? (const T*)((const char*)(vp + j0 * v.token) + vo[i]) : vp + jj * v.token + cv * EC;
+            if (ck * EC < a.D) to_lds(ks_src, &ks[buf][at * EC]);
+            if (cv * EC < a.D) to_lds(vs_src, &vs[buf][at * EC]);
         }
-        float top = s;
-        for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        if ((t & 63) == 0) red[t >> 6] = top;
-        __syncthreads();
-        float mn = m;
-        for (int x = 0; x < AROW_THREADS / 64; ++x) mn = fmaxf(mn, red[x]);
-        const float base = mn == -INFINITY ? 0.f : mn, old = expf(m - base);
-        p[t] = j < n ? expf(s - base) : 0.f;
-        m = mn;
-        __syncthreads();
-        l *= old;
-        acc *= old;
-        const int c = min(AROW_THREADS, n - j0);
-        for (int x = 0; x < c; ++x) l += p[x];
-        if (d < a.D)
-            for (int x = half; x < c; x += AROW_THREADS / ATTN_DMAX) {
-                const int y = j0 + x;
-                acc += p[x] * (float)v.row(k0 + (y < first ? y : lo + y - first), hk)[d];
+    };
+    // chunks past a head's end are never brought: zero
+    if (a.D < RS)
+        for (int i = t; i < 2 * BN * CR; i += ATTN_THREADS) {
+            const int slot = i % (BN * CR), j = slot / CR;
+            if ((slot % CR ^ G::swizzle_k(j)) * EC >= a.D) *(uint4*)&ks[i / (BN * CR)][slot * EC] = make_uint4(0, 0, 0, 0);
+            if ((slot % CR ^ G::swizzle_v(j)) * EC >= a.D) *(uint4*)&vs[i / (BN * CR)][slot * EC] = make_uint4(0, 0, 0, 0);
+        }
+    if (begin < end) bring(0, tiles.base(begin));
+
+    // queries: the right operand of the scores
+    constexpr int QS = F32 ? 4 * NC : 2 * NC;          // steps of 8 (4 a lane, in fp32) or 16 elements (8 a lane)
+    typename M::V qf[QS];
+    {
+        const T* p = q.row(q0 + row / group, qh);
+#pragma unroll
+        for (int c = 0; c < QS; ++c) {
+            const int d = (2 * c + h) * EC;
+            if (d < a.D) qf[c] = *(const typename M::V*)(p + d);
+            else
+#pragma unroll
+                for (int e = 0; e < EC; ++e) qf[c][e] = (T)0.f;
+        }
+    }
+
+    f32x16 acc[NC];
+#pragma unroll
+    for (int x = 0; x < NC; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+    const float by = a.scale * 1.44269504088896340736f;
+
+    for (int it = begin; it < end; ++it) {
+        const int buf = (it - begin) & 1, j0 = tiles.base(it);
+        wait_and_meet();
+        if (it + 1 < end) bring(buf ^ 1, tiles.base(it + 1));
+        // values that are not finite, where some rows do not see them: out of the product, into the rows that do
+        bool odd = false;
+        if (!all_see(pb0, pb1, j0, BN, a.w) || j0 + BN > nk) {
+            bool x = false;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
+                x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
+            }
+            odd = __syncthreads_or(x);
+            if (odd) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    uint4* y = (uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
+                    *y = make_uint4(M::cleared(y->x), M::cleared(y->y), M::cleared(y->z), M::cleared(y->w));
+                }
+                __syncthreads();
+            }
+        }
+        if (!any_sees(p0, p1, j0, BN, a.w)) continue;
+
+        f32x16 s[KT];
+#pragma unroll
+        for (int n = 0; n < KT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+            const int j = n * 32 + c32;
+            const T* kr = &ks[buf][j * RS];
+            const int z = G::swizzle_k(j);
+#pragma unroll
+            for (int c = 0; c < QS; ++c) {
+                const typename M::V x = *(const typename M::V*)(kr + ((2 * c + h) ^ z) * EC);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n] = M::mul(x[e], qf[c][e], s[n]);
+                } else {
+                    s[n] = M::mul(x, qf[c], s[n]);
+                }
+            }
+        }
+        float mx = -INFINITY;
+        const bool whole = all_see(p0, p1, j0, BN, a.w) && j0 + BN <= nk;
+#pragma unroll
+        for (int n = 0; n < KT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[n][i] *= by;
+                if (!whole) {
+                    const int j = j0 + n * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                    if (!(j <= hi && (j >= lo || j < a.w.sinks))) s[n][i] = -INFINITY;
+                }
+                mx = fmaxf(mx, s[n][i]);
+            }
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__any(mx > top)) {
+            const float now = fmaxf(top, mx), old = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
+            sum *= old;
+#pragma unroll
+            for (int x = 0; x < NC; ++x) acc[x] *= old;
+            top = now;
+        }
+        const float zero = top == -INFINITY ? 0.f : top;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < KT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - zero);
+                part[i & 3] += s[n][i];
+            }
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
+
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int j = 8 * (i / 4) + 4 * h + i % 4;
+                const T* vr = &vs[buf][j * RS];
+                const int z = G::swizzle_v(j) * EC;
+#pragma unroll
+                for (int x = 0; x < NC; ++x) acc[x] = M::mul(vr[(32 * x + c32) ^ z], s[0][i], acc[x]);
+            }
+        } else {
+            const int r = l >> 2 & 3, cc = l & 3, g = l >> 4 & 1;
+#pragma unroll
+            for (int n = 0; n < 2 * KT; ++n) {
+                typename M::V w;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = (T)s[n / 2][8 * (n & 1) + e];
+#pragma unroll
+                for (int x = 0; x < NC; ++x) {
+                    typename M::V y;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int j = 16 * n + 8 * e + 4 * h + r, c = 4 * x + 2 * g + (cc >> 1);
+                        const s16x4 p = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (__attribute__((address_space(3))) s16x4*)&vs[buf][j * RS + (c ^ G::swizzle_v(j)) * EC + (cc & 1) * 4]);
+                        const typename M::V4 f = __builtin_bit_cast(typename M::V4, p);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[4 * e + i] = f[i];
+                    }
+                    acc[x] = M::mul(y, w, acc[x]);
+                }
+            }
+        }
+        if (odd)
+            for (int j = j0; j < min(j0 + BN, nk); ++j) {
+                const bool see = j <= hi && (j >= lo || j < a.w.sinks);
+                const T* vr = vp + (long long)j * v.token;
+#pragma unroll
+                for (int x = 0; x < NC; ++x)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = 32 * x + 8 * (i / 4) + 4 * h + i % 4;
+                        const float y = d < a.D ? (float)vr[d] : 0.f;
+                        if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
+                    }
             }
     }
-    __syncthreads();
-    if (half) sum2[d] = acc;
-    __syncthreads();
-    if (!half && d < a.D) out.row(a.cu_q[b] + (long long)i, h)[d] = (T)(l == 0.f ? 0.f : (acc + sum2[d]) / l);
+    sum += __shfl_xor(sum, 32);
+    if (wrow0 + c32 >= rows) return;
+    if (a.splits == 1) {
+        T* y = out.row(q0 + row / group, qh);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * x + 2 * i + 4 * h;
+                if (d < a.D) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    T4 o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = (T)(sum == 0.f ? 0.f : acc[x][i + e] * inv);
+                    *(T4*)(y + d) = o;
+                }
+            }
+    } else {
+        const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wave * 32 + c32;
+        if (h == 0) a.stats[at] = make_float2(top, sum);
+        float* y = a.parts + at * a.D;
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * x + 2 * i + 4 * h;
+                if (d < a.D) *(float4*)(y + d) = make_float4(acc[x][i], acc[x][i + 1], acc[x][i + 2], acc[x][i + 3]);
+            }
+    }
+}
+
+struct AttnPlan {
+    int tiles, splits, tile_rows;
+    long long groups;                  // workgroups without splitting
+    size_t rows;                       // rows of parts
+};
+
+// Few row tiles over many keys: workgroups share the keys of a tile until the chip has two for every compute unit, each with four
+// tiles at least.
+static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
+{
+    AttnPlan p;
+    const long long rows = (long long)max_q * (Hq / Hk);
+    const long long tiles = (rows + BM - 1) / BM;
+    p.tiles = (int)(tiles < INT_MAX ? tiles : INT_MAX);
+    p.groups = tiles * Hk * B;
+    p.tile_rows = (int)(rows < BM ? rows : BM);
+    const int bn = type == ZNNI_F32 ? 32 : 64;
+    const long long tokens = (rows < BM ? max_q : BM / (Hq / Hk) + 2);
+    long long seen = (long long)left + right + tokens + (sinks < max_k ? sinks : max_k);
+    if (seen > max_k) seen = max_k;
+    const long long most = (seen + bn - 1) / bn / 4;
+    long long n = p.groups > 0 && p.groups < 512 ? 512 / p.groups : 1;
+    if (n > most) n = most;
+    p.splits = n < 1 ? 1 : (int)n;
+    p.rows = p.splits == 1 ? 0 : (size_t)p.groups * p.splits * p.tile_rows;
+    return p;
 }
 
 template <typename T>
-static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+static znni_status launch_attn(const AttnArgs& a, int max_q, const AttnPlan& p, const znni_heads* q, const znni_heads* k, const znni_heads* v,
                                const znni_heads* out, hipStream_t st)
 {
-    k_attn_rows<T><<<dim3((unsigned)max_q, (unsigned)a.Hq, (unsigned)B), dim3(AROW_THREADS), 0, st>>>(
-        a, heads_of<const T>(q), heads_of<const T>(k), heads_of<const T>(v), heads_of<T>(out));
-    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+    const dim3 grid((unsigned)(p.groups * p.splits)), block(ATTN_THREADS);
+    const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v);
+    const Heads<T> o = heads_of<T>(out);
+    switch ((a.D + 31) / 32) {
+        case 1: k_attn<T, 1><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+        case 2: k_attn<T, 2><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+        case 3: k_attn<T, 3><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+        default: k_attn<T, 4><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+    }
+    if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    if (p.splits == 1) return ZNNI_OK;
+    const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, a.parts, a.stats};
+    return launch_join<T>(j, a.B, o, st);
 }
 
 static znni_status attn_shape(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
 {
     if (!type_ok(type)) return ZNNI_ERR_TYPE;
     if (B < 0 || B > 65535 || max_q < 0 || max_k < 0 || left < 0 || right < 0 || sinks < 0) return ZNNI_ERR_SHAPE;
-    return heads_shape(Hq, Hk, D);
+    const znni_status rc = heads_shape(Hq, Hk, D);
+    if (rc) return rc;
+    // a workgroup for every row tile and key head
+    const long long rows = (long long)max_q * (Hq / Hk), tiles = (rows + BM - 1) / BM;
+    return rows > INT_MAX || tiles * Hk > INT_MAX / (B ? B : 1) ? ZNNI_ERR_SHAPE : ZNNI_OK;
 }
 
 }  // namespace znni
@@ -94,7 +417,8 @@ znni_status znni_attn_window_workspace(int type, int B, int Hq, int Hk, int D, i
     if (!bytes) return ZNNI_ERR_NULL;
     const znni_status rc = attn_shape(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks);
     if (rc) return rc;
-    *bytes = 0;
+    const AttnPlan p = attn_plan(type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    *bytes = p.rows * (D + 2) * sizeof(float);
     return ZNNI_OK;
 }
 
@@ -112,12 +436,15 @@ znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_
     if (((uintptr_t)cu_q | (uintptr_t)cu_k) & 3u || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
     for (const znni_heads* h : {q, k, v, out})
         if (!heads_aligned(h, type)) return ZNNI_ERR_ALIGN;
-    const AttnArgs a = {Hq, Hk, D, cu_q, cu_k, {left, right, sinks}, scale};
+    const AttnPlan p = attn_plan(type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    float* parts = (float*)workspace;
+    const AttnArgs a = {Hq, Hk, D, cu_q, cu_k, {left, right, sinks}, scale, B, max_q, p.tiles, p.splits, p.tile_rows, parts,
+                        (float2*)(parts + p.rows * D)};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
-        case ZNNI_F32: return launch_attn<float>(a, B, max_q, q, k, v, out, st);
-        case ZNNI_BF16: return launch_attn<bf16>(a, B, max_q, q, k, v, out, st);
-        default: return launch_attn<f16>(a, B, max_q, q, k, v, out, st);
+        case ZNNI_F32: return launch_attn<float>(a, max_q, p, q, k, v, out, st);
+        case ZNNI_BF16: return launch_attn<bf16>(a, max_q, p, q, k, v, out, st);
+        default: return launch_attn<f16>(a, max_q, p, q, k, v, out, st);
     }
 }
 

@@ -9,6 +9,7 @@
 //   through LDS before the waves join.
 // Codes become bf16 (exact: 4 significant bits); queries and weights are sums of as many bf16 as their type has bits
 // for, so products are exact and only sums round, in fp32.
+#include "attn_join.h"
 #include "kv8.h"
 
 namespace znni {
@@ -26,7 +27,8 @@ struct Kv8Args {
     const int* lens;
     Window w;
     float scale;
-    float* parts;        // [B][Hk][row tile][splits][16 rows][D], then as many [16 rows][2]: maximum (in powers of two) and sum
+    float* parts;        // [B][Hk][row tile][splits][16 rows][D]
+    float2* stats;       // [B][Hk][row tile][splits][16 rows]: maximum (in powers of two) and sum of weights
 };
 
 constexpr int KV8_WAVES = 8, KV8_ROWS = 16;
@@ -309,7 +311,6 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8(Kv8Args a, Heads<const T
     for (int x = 0; x < NX; ++x) *(f32x4*)&acc_s[wave][r][16 * x + 4 * u] = acc[x];
     __syncthreads();
     const long long block = (((long long)b * a.Hk + hk) * tiles + tile) * a.splits + split_id;
-    const long long blocks = (long long)gridDim.z * gridDim.y * a.splits;
     for (int i = threadIdx.x; i < KV8_ROWS * DP; i += 64 * KV8_WAVES) {
         const int rr = i / DP, d = i % DP, row_r = tile * KV8_ROWS + rr;
         if (row_r >= rows || d >= a.D) continue;
@@ -327,39 +328,9 @@ __global__ __launch_bounds__(64 * KV8_WAVES) void k_kv8(Kv8Args a, Heads<const T
             out.row((long long)b * a.Lq + row_r / G, hk * G + row_r % G)[d] = (T)(n == 0.f ? 0.f : o / n);
         } else {
             a.parts[(block * KV8_ROWS + rr) * a.D + d] = o;
-            if (d == 0) *(float2*)(a.parts + blocks * KV8_ROWS * a.D + (block * KV8_ROWS + rr) * 2) = make_float2(m, n);
+            if (d == 0) a.stats[block * KV8_ROWS + rr] = make_float2(m, n);
         }
     }
-}
-
-// Joins the parts of a row: one wave a row, elements over its lanes.
-template <typename T>
-__global__ __launch_bounds__(256) void k_kv8_join(Kv8Args a, int B, Heads<T> out)
-{
-    const int G = a.Hq / a.Hk, tiles = (a.Lq * G + KV8_ROWS - 1) / KV8_ROWS, rows = a.Lq * G;
-    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), all = (long long)B * a.Hk * rows;
-    if (id >= all) return;
-    const int row = (int)(id % rows), l = threadIdx.x & 63;
-    const long long bh = id / rows;
-    const int hk = (int)(bh % a.Hk), b = (int)(bh / a.Hk);
-    const long long first = (bh * tiles + row / KV8_ROWS) * a.splits, blocks = (long long)B * a.Hk * tiles * a.splits;
-    const float* stats = a.parts + blocks * KV8_ROWS * a.D;
-    float m = -INFINITY;
-    for (int s = l; s < a.splits; s += 64) m = fmaxf(m, stats[((first + s) * KV8_ROWS + row % KV8_ROWS) * 2]);
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float z = m == -INFINITY ? 0.f : m;
-    float n = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const long long at = (first + s) * KV8_ROWS + row % KV8_ROWS;
-        const float2 st = *(const float2*)(stats + at * 2);
-        const float f = __builtin_amdgcn_exp2f(st.x - z);
-        n += f * st.y;
-        if (l < a.D) o0 += f * a.parts[at * a.D + l];
-        if (l + 64 < a.D) o1 += f * a.parts[at * a.D + l + 64];
-    }
-    T* y = out.row((long long)b * a.Lq + row / G, hk * G + row % G);
-    if (l < a.D) y[l] = (T)(n == 0.f ? 0.f : o0 / n);
-    if (l + 64 < a.D) y[l + 64] = (T)(n == 0.f ? 0.f : o1 / n);
 }
 
 // How many workgroups share a sequence's pages.  A call whose waves have two pages at most is not split, which saves the
@@ -378,11 +349,10 @@ static int kv8_splits(int B, int Lq, int Hq, int Hk, int max_len, int left, int 
     return (int)(n < most ? n : most);
 }
 
-static size_t kv8_parts(int B, int Lq, int Hq, int Hk, int D, int splits)
+static size_t kv8_part_rows(int B, int Lq, int Hq, int Hk, int splits)
 {
-    if (splits == 1) return 0;
     const size_t tiles = ((size_t)Lq * (Hq / Hk) + KV8_ROWS - 1) / KV8_ROWS;
-    return tiles * Hk * B * splits * KV8_ROWS * (D + 2) * sizeof(float);
+    return splits == 1 ? 0 : tiles * Hk * B * splits * KV8_ROWS;
 }
 
 template <typename T, int NC>
@@ -406,11 +376,9 @@ static znni_status launch_kv8(const Kv8Args& a, int B, const znni_heads* q, cons
         default: launch_steps<T, 4>(a, grid, qi, o, st); break;
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    if (a.splits > 1) {
-        k_kv8_join<T><<<dim3((unsigned)((rows * a.Hk * B + 3) / 4)), dim3(256), 0, st>>>(a, B, o);
-        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    }
-    return ZNNI_OK;
+    if (a.splits == 1) return ZNNI_OK;
+    const JoinArgs j = {a.Hq, a.Hk, a.D, a.splits, (int)tiles, KV8_ROWS, (int)rows, nullptr, a.Lq, a.parts, a.stats};
+    return launch_join<T>(j, B, o, st);
 }
 
 }  // namespace znni
@@ -428,7 +396,7 @@ znni_status znni_kv8_attn_workspace(int type, int B, int Lq, int Hq, int Hk, int
     if (rc) return rc;
     // row tiles of all heads ride in a launch dimension
     if (((long long)Lq * (Hq / Hk) + KV8_ROWS - 1) / KV8_ROWS * Hk > 65535) return ZNNI_ERR_SHAPE;
-    *bytes = B && Lq ? kv8_parts(B, Lq, Hq, Hk, D, kv8_splits(B, Lq, Hq, Hk, max_len, left, sinks)) : 0;
+    *bytes = B && Lq ? kv8_part_rows(B, Lq, Hq, Hk, kv8_splits(B, Lq, Hq, Hk, max_len, left, sinks)) * (D + 2) * sizeof(float) : 0;
     return ZNNI_OK;
 }
 
@@ -449,8 +417,10 @@ znni_status znni_kv8_attn(int type, int B, int Lq, int Hq, int Hk, int D, const 
     if (!heads_aligned(q, type) || !heads_aligned(out, type) || !cache_aligned(kcodes, vcodes, scales) ||
         (((uintptr_t)lens | (uintptr_t)table) & 3u) || (need && ((uintptr_t)workspace & 255u)))
         return ZNNI_ERR_ALIGN;
-    const Kv8Args a = {Lq, Hq, Hk, D, pages, width, kv8_splits(B, Lq, Hq, Hk, max_len, left, sinks), kcodes, vcodes, scales, table, lens,
-                       {left, 0, sinks}, scale, (float*)workspace};
+    const int splits = kv8_splits(B, Lq, Hq, Hk, max_len, left, sinks);
+    float* parts = (float*)workspace;
+    const Kv8Args a = {Lq, Hq, Hk, D, pages, width, splits, kcodes, vcodes, scales, table, lens, {left, 0, sinks}, scale, parts,
+                       (float2*)(parts + kv8_part_rows(B, Lq, Hq, Hk, splits) * D)};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
         case ZNNI_F32: return launch_kv8<float>(a, B, q, out, st);
