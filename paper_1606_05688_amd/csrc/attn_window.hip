@@ -46,9 +46,23 @@ struct AttnTile {
     }
 };
 
-__device__ inline void to_lds(const void* src, void* dst)
+// 16 bytes a lane from memory to LDS, 1024 bytes of a wave from `lds` on.  As assembly, since the compiler, which sees one
+// array in LDS, waits for such a load before any read of it: wait_and_meet() is what waits for these.
+__device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+__device__ inline void to_lds(const void* from, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// Four elements of one column of four rows: lanes 4r .. 4r + 3 of sixteen bring row r, lane c of them gets column c.
+template <typename V4>
+__device__ inline V4 transposed(const char* p)
+{
+    return __builtin_bit_cast(V4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
 
 __device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -142,6 +156,8 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const T* kp = k.row(k0, hk);
     const T* vp = v.row(k0, hk);
     const bool near = k.token >= 0 && v.token >= 0 && k.token < (1 << 22) && v.token < (1 << 22);
+    constexpr unsigned TILE = BN * RS * sizeof(T);
+    const unsigned k_lds = lds_address(ks) + wave * 1024, v_lds = lds_address(vs) + wave * 1024;
     unsigned ko[PER], vo[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -150,15 +166,22 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         vo[i] = ((unsigned)j * (unsigned)v.token + (c ^ G::swizzle_v(j)) * EC) * (unsigned)sizeof(T);
     }
     auto bring = [&](int buf, int j0) {
-        const bool fast = near && j0 + BN <= nk;
+        if (near && a.D == RS && j0 + BN <= nk) {
+            const char* kt = (const char*)(kp + j0 * k.token);
+            const char* vt = (const char*)(vp + j0 * v.token);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                to_lds(kt, ko[i], k_lds + buf * TILE + i * 4096);
+                to_lds(vt, vo[i], v_lds + buf * TILE + i * 4096);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = (i * 4 + wave) * 64, slot = at + l, j = slot / CR, ck = slot % CR ^ G::swizzle_k(j), cv = slot % CR ^ G::swizzle_v(j);
+            const int slot = (i * 4 + wave) * 64 + l, j = slot / CR, ck = slot % CR ^ G::swizzle_k(j), cv = slot % CR ^ G::swizzle_v(j);
             const long long jj = min(j0 + j, nk - 1);
-            const T* ks_src = fast ? (const T*)((const char*)(kp + j0 * k.token) + ko[i]) : kp + jj * k.token + ck * EC;
-            const T* vs_src = fast ? (const T*)((const char*)(vp + j0 * v.token) + vo[i]) : vp + jj * v.token + cv * EC;
-            if (ck * EC < a.D) to_lds(ks_src, &ks[buf][at * EC]);
-            if (cv * EC < a.D) to_lds(vs_src, &vs[buf][at * EC]);
+            if (ck * EC < a.D) to_lds(kp + jj * k.token + ck * EC, k_lds + buf * TILE + i * 4096);
+            if (cv * EC < a.D) to_lds(vp + jj * v.token + cv * EC, v_lds + buf * TILE + i * 4096);
         }
     };
     // chunks past a head's end are never brought: zero
@@ -182,6 +205,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             else
 #pragma unroll
                 for (int e = 0; e < EC; ++e) qf[c][e] = (T)0.f;
+            // a negative scale turns the queries, so that the largest product is the largest score
+            if (a.scale < 0.f)
+#pragma unroll
+                for (int e = 0; e < EC; ++e) qf[c][e] = -qf[c][e];
         }
     }
 
@@ -191,7 +218,13 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
     float top = -INFINITY, sum = 0.f;
-    const float by = a.scale * 1.44269504088896340736f;
+    const float by = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * 1.44269504088896340736f;       // of 0: what is masked stays so
+
+    // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
+    const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
+    int k_at = (c32 * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T);
+    int v_at = F32 ? (4 * h * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)
+                   : ((4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
 
     for (int it = begin; it < end; ++it) {
         const int buf = (it - begin) & 1, j0 = tiles.base(it);
@@ -218,17 +251,20 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         }
         if (!any_sees(p0, p1, j0, BN, a.w)) continue;
 
+        // (worked out again for every tile: kept, the addresses of all steps would take the registers)
+        asm volatile("" : "+v"(k_at), "+v"(v_at));
+        const char* kb = (const char*)ks[buf];
+        const char* vb = (const char*)vs[buf];
         f32x16 s[KT];
 #pragma unroll
-        for (int n = 0; n < KT; ++n) {
+        for (int n = 0; n < KT; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
-            const int j = n * 32 + c32;
-            const T* kr = &ks[buf][j * RS];
-            const int z = G::swizzle_k(j);
 #pragma unroll
-            for (int c = 0; c < QS; ++c) {
-                const typename M::V x = *(const typename M::V*)(kr + ((2 * c + h) ^ z) * EC);
+        for (int c = 0; c < QS; ++c)
+#pragma unroll
+            for (int n = 0; n < KT; ++n) {
+                const typename M::V x = *(const typename M::V*)(kb + (k_at ^ c * 32) + n * 32 * RS * (int)sizeof(T));
                 if constexpr (F32) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[n] = M::mul(x[e], qf[c][e], s[n]);
@@ -236,71 +272,66 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     s[n] = M::mul(x, qf[c], s[n]);
                 }
             }
+        if (!(all_see(p0, p1, j0, BN, a.w) && j0 + BN <= nk)) {
+#pragma unroll
+            for (int n = 0; n < KT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = j0 + n * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                    s[n][i] = j <= hi && (j >= lo || j < a.w.sinks) ? s[n][i] : -INFINITY;
+                }
         }
-        float mx = -INFINITY;
-        const bool whole = all_see(p0, p1, j0, BN, a.w) && j0 + BN <= nk;
+        float mx = top;
 #pragma unroll
         for (int n = 0; n < KT; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[n][i] *= by;
-                if (!whole) {
-                    const int j = j0 + n * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                    if (!(j <= hi && (j >= lo || j < a.w.sinks))) s[n][i] = -INFINITY;
-                }
-                mx = fmaxf(mx, s[n][i]);
-            }
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+            for (int i = 0; i < 16; i += 2) mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx, s[n][i]), s[n][i + 1]);
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32));
         if (__any(mx > top)) {
-            const float now = fmaxf(top, mx), old = __builtin_amdgcn_exp2f(top - (now == -INFINITY ? 0.f : now));
+            const float old = __builtin_amdgcn_exp2f((top - (mx == -INFINITY ? 0.f : mx)) * by);
             sum *= old;
 #pragma unroll
             for (int x = 0; x < NC; ++x) acc[x] *= old;
-            top = now;
+            top = mx;
         }
+        // weights 2^(by (s - top)): as one multiply-add, unless by * top is so large that its rounding would leave the range of
+        // the type (it is the same for all keys of a row and cancels)
         const float zero = top == -INFINITY ? 0.f : top;
-        float part[4] = {0.f, 0.f, 0.f, 0.f};
+        float shift = -zero * by;
+        if (__any(!(fabsf(shift) < 0x1p26f))) {
 #pragma unroll
-        for (int n = 0; n < KT; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - zero);
-                part[i & 3] += s[n][i];
-            }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
-
+            for (int n = 0; n < KT; ++n) s[n] -= zero;
+            shift = 0.f;
+        }
+        float part[2] = {0.f, 0.f};
         if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int j = 8 * (i / 4) + 4 * h + i % 4;
-                const T* vr = &vs[buf][j * RS];
-                const int z = G::swizzle_v(j) * EC;
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, shift));
+                part[i & 1] += w;
 #pragma unroll
-                for (int x = 0; x < NC; ++x) acc[x] = M::mul(vr[(32 * x + c32) ^ z], s[0][i], acc[x]);
+                for (int x = 0; x < NC; ++x)
+                    acc[x] = M::mul(*(const T*)(vb + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), w, acc[x]);
             }
         } else {
-            const int r = l >> 2 & 3, cc = l & 3, g = l >> 4 & 1;
 #pragma unroll
             for (int n = 0; n < 2 * KT; ++n) {
                 typename M::V w;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (T)s[n / 2][8 * (n & 1) + e];
+                for (int e = 0; e < 8; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, shift));
+                    part[e & 1] += p;
+                    w[e] = (T)p;
+                }
 #pragma unroll
                 for (int x = 0; x < NC; ++x) {
-                    typename M::V y;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int j = 16 * n + 8 * e + 4 * h + r, c = 4 * x + 2 * g + (cc >> 1);
-                        const s16x4 p = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) s16x4*)&vs[buf][j * RS + (c ^ G::swizzle_v(j)) * EC + (cc & 1) * 4]);
-                        const typename M::V4 f = __builtin_bit_cast(typename M::V4, p);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[4 * e + i] = f[i];
-                    }
-                    acc[x] = M::mul(y, w, acc[x]);
+                    const char* from = vb + (v_at ^ x * 64) + 16 * n * RS * (int)sizeof(T);
+                    const typename M::V4 y0 = transposed<typename M::V4>(from), y1 = transposed<typename M::V4>(from + 8 * RS * (int)sizeof(T));
+                    acc[x] = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[x]);
                 }
             }
         }
+        sum += part[0] + part[1];
         if (odd)
             for (int j = j0; j < min(j0 + BN, nk); ++j) {
                 const bool see = j <= hi && (j >= lo || j < a.w.sinks);
@@ -335,7 +366,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             }
     } else {
         const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wave * 32 + c32;
-        if (h == 0) a.stats[at] = make_float2(top, sum);
+        if (h == 0) a.stats[at] = make_float2(top * by, sum);
         float* y = a.parts + at * a.D;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
