@@ -26,7 +26,7 @@ struct AttnArgs {
     float2* stats;
 };
 
-constexpr int BM = 128, ATTN_THREADS = 256;
+constexpr int BM = 128, ATTN_THREADS = 256, RUN = 8;
 
 template <typename T, int NC>
 struct AttnTile {
@@ -93,31 +93,32 @@ struct Mfma<float> {
     __device__ static unsigned cleared(unsigned x) { return odd(x) ? 0u : x; }
 };
 
-// Key tiles that rows at positions p0 .. p1 see: those of sinks alone, then those of the window.
+// What rows at positions p0 .. p1 (none if p1 < p0) see of nk keys: the first row's keys go from lo0 to hi0, the last one's from lo1
+// to hi1, besides sinks.
+struct Sight {
+    int lo0, hi0, lo1, hi1, sinks;
+    __device__ Sight(long long p0, long long p1, int nk, const Window& w) : sinks(w.sinks)
+    {
+        window_of(p0, nk, w, &lo0, &hi0);
+        window_of(p1, nk, w, &lo1, &hi1);
+        if (p1 < p0) hi0 = hi1 = -1;
+    }
+    __device__ bool all(int j0, int n) const { return j0 + n - 1 <= hi0 && (j0 >= lo1 || j0 + n <= sinks); }
+    __device__ bool any(int j0, int n) const { return j0 <= hi1 && (j0 + n - 1 >= lo0 || j0 < sinks); }
+};
+
+// Their key tiles: those of sinks alone, then those of the window.
 template <int BN>
 struct KeyTiles {
     int sink_tiles, first, n;
-    __device__ KeyTiles(long long p0, long long p1, int nk, const Window& w)
+    __device__ KeyTiles(const Sight& s)
     {
-        int lo, hi, x, y;
-        window_of(p0, nk, w, &lo, &x);
-        window_of(p1, nk, w, &y, &hi);
-        first = lo / BN;
-        sink_tiles = min((min(w.sinks, hi + 1) + BN - 1) / BN, first);
-        n = hi < lo ? sink_tiles : sink_tiles + hi / BN - first + 1;
+        first = s.lo0 / BN;
+        sink_tiles = min((min(s.sinks, s.hi1 + 1) + BN - 1) / BN, first);
+        n = s.hi1 < s.lo0 ? sink_tiles : sink_tiles + s.hi1 / BN - first + 1;
     }
     __device__ int base(int i) const { return (i < sink_tiles ? i : first + i - sink_tiles) * BN; }
 };
-
-// Whether rows at p0 .. p1 all see keys j0 .. j0 + n - 1, and whether any sees any of them.
-__device__ inline bool all_see(long long p0, long long p1, int j0, int n, const Window& w)
-{
-    return j0 + n - 1 <= p0 + w.right && (j0 >= p1 - w.left || j0 + n <= w.sinks);
-}
-__device__ inline bool any_sees(long long p0, long long p1, int j0, int n, const Window& w)
-{
-    return p1 >= p0 && j0 <= p1 + w.right && (j0 + n - 1 >= p0 - w.left || j0 < w.sinks);
-}
 
 template <typename T, int NC>
 __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
@@ -129,7 +130,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     __shared__ __align__(1024) T ks[2][BN * RS];
     __shared__ __align__(1024) T vs[2][BN * RS];
 
+    // Workgroups go to the eight XCDs in turn, each with an L2 of its own: runs of RUN neighbouring row tiles, which see nearly the same
+    // keys, to the same one.
     int id = blockIdx.x;
+    if (id < (int)gridDim.x / (8 * RUN) * (8 * RUN)) id = (id / (8 * RUN) * 8 + id % 8) * RUN + id / 8 % RUN;
     const int split = id % a.splits; id /= a.splits;
     const int tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
     const int hk = id % a.Hk, b = id / a.Hk;
@@ -139,17 +143,16 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     if (row0 >= rows) return;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
     const long long base = (long long)nk - nq, last = min(row0 + BM, rows) - 1;
-    const long long pb0 = base + row0 / group, pb1 = base + last / group;              // positions of the workgroup
-    const long long wrow0 = row0 + wave * 32, wlast = min(wrow0 + 31, rows - 1);
-    const bool has = wrow0 < rows;
-    const long long p0 = has ? base + wrow0 / group : 0, p1 = has ? base + wlast / group : -1;       // of the wave
+    const long long wrow0 = row0 + wave * 32;
+    const Sight all_rows(base + row0 / group, base + last / group, nk, a.w);
+    const Sight wave_rows(base + wrow0 / group, wrow0 < rows ? base + min(wrow0 + 31, last) / group : LLONG_MIN, nk, a.w);
     const long long row = min(wrow0 + c32, rows - 1);
     const long long pos = base + row / group;                                          // of the lane
     int lo, hi;
     window_of(pos, nk, a.w, &lo, &hi);
     const int qh = hk * group + (int)(row % group);
 
-    const KeyTiles<BN> tiles(pb0, pb1, nk, a.w);
+    const KeyTiles<BN> tiles(all_rows);
     const int per = (tiles.n + a.splits - 1) / a.splits, begin = split * per, end = min(tiles.n, begin + per);
 
     // what this thread brings of a tile: PER chunks of keys and of values, 64 consecutive ones a wave
@@ -217,9 +220,11 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     for (int x = 0; x < NC; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
-    float top = -INFINITY, sum = 0.f;
+    float top = -INFINITY, sum = 0.f, shift = 0.f;
+    bool wild = false, odd = false;
     const float by = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * 1.44269504088896340736f;       // of 0: what is masked stays so
 
+    const float ahead = 8.f / by;
     // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
     int k_at = (c32 * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T);
@@ -230,17 +235,16 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         const int buf = (it - begin) & 1, j0 = tiles.base(it);
         wait_and_meet();
         if (it + 1 < end) bring(buf ^ 1, tiles.base(it + 1));
-        // values that are not finite, where some rows do not see them: out of the product, into the rows that do
-        bool odd = false;
-        if (!all_see(pb0, pb1, j0, BN, a.w) || j0 + BN > nk) {
+        // values that are not finite, where some rows do not see them: out of the product, into the rows that do at the end
+        if (!all_rows.all(j0, BN)) {
             bool x = false;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
                 x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
             }
-            odd = __syncthreads_or(x);
-            if (odd) {
+            if (__syncthreads_or(x)) {
+                odd = true;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
                     uint4* y = (uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 __syncthreads();
             }
         }
-        if (!any_sees(p0, p1, j0, BN, a.w)) continue;
+        if (!wave_rows.any(j0, BN)) continue;
 
         // (worked out again for every tile: kept, the addresses of all steps would take the registers)
         asm volatile("" : "+v"(k_at), "+v"(v_at));
@@ -272,7 +276,16 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     s[n] = M::mul(x, qf[c], s[n]);
                 }
             }
-        if (!(all_see(p0, p1, j0, BN, a.w) && j0 + BN <= nk)) {
+        // reads run four ahead of the products (left alone, the compiler waits for each)
+        if constexpr (!F32) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int n = 0; n < QS * KT; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+        }
+        if (!wave_rows.all(j0, BN)) {
 #pragma unroll
             for (int n = 0; n < KT; ++n)
 #pragma unroll
@@ -281,33 +294,38 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     s[n][i] = j <= hi && (j >= lo || j < a.w.sinks) ? s[n][i] : -INFINITY;
                 }
         }
-        float mx = top;
+        float mx[4];
 #pragma unroll
-        for (int n = 0; n < KT; ++n)
+        for (int x = 0; x < 4; ++x) {
+            mx[x] = s[0][x];
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx, s[n][i]), s[n][i + 1]);
-        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32));
-        if (__any(mx > top)) {
-            const float old = __builtin_amdgcn_exp2f((top - (mx == -INFINITY ? 0.f : mx)) * by);
+            for (int i = 1; i < 4 * KT; ++i) mx[x] = __builtin_elementwise_maximum(mx[x], s[i / 4][4 * (i % 4) + x]);
+        }
+        float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]));
+        // Weights are 2^(by (s - top)), as one multiply-add.  `top` follows the maximum when that is 2^8 ahead: weights stay in
+        // the range of every type, and most tiles have nothing to rescale.  by * top may be so large that its rounding would
+        // leave that range (it is the same for all keys of a row and cancels): then the difference comes first.
+        float offset = shift;
+        if (wild || __any(most > top + ahead)) {
+            most = fmaxf(fmaxf(most, __shfl_xor(most, 32)), top);
+            const float zero = most == -INFINITY ? 0.f : most, old = __builtin_amdgcn_exp2f((top - zero) * by);
             sum *= old;
 #pragma unroll
             for (int x = 0; x < NC; ++x) acc[x] *= old;
-            top = mx;
-        }
-        // weights 2^(by (s - top)): as one multiply-add, unless by * top is so large that its rounding would leave the range of
-        // the type (it is the same for all keys of a row and cancels)
-        const float zero = top == -INFINITY ? 0.f : top;
-        float shift = -zero * by;
-        if (__any(!(fabsf(shift) < 0x1p26f))) {
+            top = most;
+            offset = shift = -zero * by;
+            wild = __any(!(fabsf(shift) < 0x1p26f));
+            if (wild) {
 #pragma unroll
-            for (int n = 0; n < KT; ++n) s[n] -= zero;
-            shift = 0.f;
+                for (int n = 0; n < KT; ++n) s[n] -= zero;
+                offset = 0.f;
+            }
         }
         float part[2] = {0.f, 0.f};
         if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, shift));
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, offset));
                 part[i & 1] += w;
 #pragma unroll
                 for (int x = 0; x < NC; ++x)
@@ -319,7 +337,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 typename M::V w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, shift));
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, offset));
                     part[e & 1] += p;
                     w[e] = (T)p;
                 }
@@ -332,7 +350,11 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             }
         }
         sum += part[0] + part[1];
-        if (odd)
+    }
+    if (odd)
+        for (int it = begin; it < end; ++it) {
+            const int j0 = tiles.base(it);
+            if (all_rows.all(j0, BN)) continue;
             for (int j = j0; j < min(j0 + BN, nk); ++j) {
                 const bool see = j <= hi && (j >= lo || j < a.w.sinks);
                 const T* vr = vp + (long long)j * v.token;
@@ -345,7 +367,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                         if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
                     }
             }
-    }
+        }
     sum += __shfl_xor(sum, 32);
     if (wrow0 + c32 >= rows) return;
     if (a.splits == 1) {
@@ -366,7 +388,8 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             }
     } else {
         const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wave * 32 + c32;
-        if (h == 0) a.stats[at] = make_float2(top * by, sum);
+        const float in_range = top == -INFINITY ? top : fminf(fmaxf(top * by, -3.402823466e38f), 3.402823466e38f);
+        if (h == 0) a.stats[at] = make_float2(in_range, sum);
         float* y = a.parts + at * a.D;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
