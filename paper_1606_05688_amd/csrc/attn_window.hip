@@ -7,133 +7,25 @@
 //   exchange; the weights as they stand are the right operand of  out^T [D][32 rows] += V^T W^T.
 // V^T's operand: 16-bit types by transposing LDS reads, fp32 (products of fp32) by plain ones, keys permuted to match.
 // Rows in LDS are permuted by 16-byte chunks so that neither kind of read meets a bank twice.
-#include "attn_common.h"
 #include "attn_join.h"
+#include "attn_tile.h"
 
 namespace znni {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
+constexpr int BM = 128, ATTN_THREADS = 256;
 
-struct AttnArgs {
-    int Hq, Hk, D;
-    const int* cu_q;
-    const int* cu_k;
-    Window w;
-    float scale;
-    int B, max_q, tiles, splits, tile_rows;     // row tiles of a sequence, workgroups that share a tile's keys, rows of a tile in `parts`
-    float* parts;
-    float2* stats;
-};
-
-constexpr int BM = 128, ATTN_THREADS = 256, RUN = 8;
-
-template <typename T, int NC>
-struct AttnTile {
-    static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int BN = F32 ? 32 : 64;                       // keys
-    static constexpr int EC = 16 / sizeof(T);                      // elements of a 16-byte chunk
-    static constexpr int RS = NC == 3 ? 128 : 32 * NC;             // elements of a row in LDS
-    static constexpr int CR = RS / EC;                             // its chunks
-    static constexpr int PER = BN * CR / ATTN_THREADS;             // chunks a thread brings
-    // Chunk c of key j lies at c ^ swizzle(j).  Scores read one chunk of 32 keys, 16 bytes a lane: 256 bytes of
-    // consecutive keys get different places; values read, 16-bit: four keys, 64 bytes each, fp32: two keys four apart, 128 bytes each.
-    __device__ static int swizzle_k(int j) { return CR >= 16 ? j & 15 : CR == 8 ? j >> 1 & 7 : j >> 2 & 3; }
-    __device__ static int swizzle_v(int j)
-    {
-        if (F32) return CR >= 16 ? (j >> 2 & 1) << 3 : 0;
-        return CR == 16 ? (j & 3) << 2 : CR == 8 ? (j >> 1 & 1) << 2 : 0;
-    }
-};
-
-// 16 bytes a lane from memory to LDS, 1024 bytes of a wave from `lds` on.  As assembly, since the compiler, which sees one
-// array in LDS, waits for such a load before any read of it: wait_and_meet() is what waits for these.
-__device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
-}
-__device__ inline void to_lds(const void* from, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
-}
-__device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
-
-// Four elements of one column of four rows: lanes 4r .. 4r + 3 of sixteen bring row r, lane c of them gets column c.
-template <typename V4>
-__device__ inline V4 transposed(const char* p)
-{
-    return __builtin_bit_cast(V4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
-}
-
-__device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-template <typename T>
-struct Mfma;
-template <>
-struct Mfma<bf16> {
-    typedef bf16 V __attribute__((ext_vector_type(8)));
-    typedef bf16 V4 __attribute__((ext_vector_type(4)));
-    __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u); }
-};
-template <>
-struct Mfma<f16> {
-    typedef f16 V __attribute__((ext_vector_type(8)));
-    typedef f16 V4 __attribute__((ext_vector_type(4)));
-    __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
-    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7c00u) == 0x7c00u ? 0u : x & 0xffffu) | ((x & 0x7c000000u) == 0x7c000000u ? 0u : x & 0xffff0000u); }
-};
-template <>
-struct Mfma<float> {
-    typedef float V __attribute__((ext_vector_type(4)));
-    __device__ static f32x16 mul(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u; }
-    __device__ static unsigned cleared(unsigned x) { return odd(x) ? 0u : x; }
-};
-
-// What rows at positions p0 .. p1 (none if p1 < p0) see of nk keys: the first row's keys go from lo0 to hi0, the last one's from lo1
-// to hi1, besides sinks.
-struct Sight {
-    int lo0, hi0, lo1, hi1, sinks;
-    __device__ Sight(long long p0, long long p1, int nk, const Window& w) : sinks(w.sinks)
-    {
-        window_of(p0, nk, w, &lo0, &hi0);
-        window_of(p1, nk, w, &lo1, &hi1);
-        if (p1 < p0) hi0 = hi1 = -1;
-    }
-    __device__ bool all(int j0, int n) const { return j0 + n - 1 <= hi0 && (j0 >= lo1 || j0 + n <= sinks); }
-    __device__ bool any(int j0, int n) const { return j0 <= hi1 && (j0 + n - 1 >= lo0 || j0 < sinks); }
-};
-
-// Their key tiles: those of sinks alone, then those of the window.
-template <int BN>
-struct KeyTiles {
-    int sink_tiles, first, n;
-    __device__ KeyTiles(const Sight& s)
-    {
-        first = s.lo0 / BN;
-        sink_tiles = min((min(s.sinks, s.hi1 + 1) + BN - 1) / BN, first);
-        n = s.hi1 < s.lo0 ? sink_tiles : sink_tiles + s.hi1 / BN - first + 1;
-    }
-    __device__ int base(int i) const { return (i < sink_tiles ? i : first + i - sink_tiles) * BN; }
-};
 
 template <typename T, int NC>
 __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
 {
-    using G = AttnTile<T, NC>;
+    using G = AttnTile<T, NC, ATTN_THREADS>;
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
     constexpr int BN = G::BN, KT = BN / 32, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
     __shared__ __align__(1024) T ks[2][BN * RS];
     __shared__ __align__(1024) T vs[2][BN * RS];
 
-    // Workgroups go to the eight XCDs in turn, each with an L2 of its own: runs of RUN neighbouring row tiles, which see nearly the same
-    // keys, to the same one.
-    int id = blockIdx.x;
-    if (id < (int)gridDim.x / (8 * RUN) * (8 * RUN)) id = (id / (8 * RUN) * 8 + id % 8) * RUN + id / 8 % RUN;
+    int id = in_runs(blockIdx.x, gridDim.x);
     const int split = id % a.splits; id /= a.splits;
     const int tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
     const int hk = id % a.Hk, b = id / a.Hk;
