@@ -96,7 +96,7 @@ def lib():
         for fn in (L.znni_mpf, L.znni_maxpool):
             fn.restype = i
             fn.argtypes = [i, i, i3, i3, vp, vp, vp]
-        hp, ip = ctypes.POINTER(_Heads), ctypes.POINTER(ctypes.c_int)
+        hp, ip = vp, ctypes.POINTER(ctypes.c_int)          # (znni_heads *: several lie in one array)
         L.znni_rope_axes.restype = i
         L.znni_rope_axes.argtypes = [i, i, i, i, i, hp, hp, vp, vp, i, ip, hp, hp, u, vp]
         L.znni_attn_window_workspace.restype = i
@@ -361,25 +361,28 @@ def znni_copy_probe(dst, src, stream=None):
 
 
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_DESCRIPTORS = {n: ctypes.c_longlong * (3 * n) for n in range(1, 5)}
+_byref = ctypes.byref
 
 
-def _heads(x):
-    """A [tokens, heads, D] tensor whose last index is contiguous, as a znni_heads."""
-    assert x.is_cuda and x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1), "tensors of heads are [tokens, heads, D], D contiguous"
-    # the stride of an axis of one element (or of none) says nothing, and torch may report any
-    return _Heads(x.data_ptr() if x.numel() else None, x.stride(0) if x.shape[0] > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
+def _heads(*tensors):
+    """References to the znni_heads of [tokens, heads, D] tensors of one type and device, whose last index is contiguous."""
+    first = tensors[0]
+    dtype, device, values = first.dtype, first.get_device(), []
+    assert first.is_cuda and dtype in _TYPES, "heads are float32, bfloat16 or float16 tensors on the GPU"
+    for x in tensors:
+        assert x.dtype == dtype and x.get_device() == device, "all tensors of heads have one type and device"
+        (tokens, heads, _), (token, head, unit) = x.shape, x.stride()
+        assert unit == 1, "tensors of heads are [tokens, heads, D], D contiguous"
+        # the stride of an axis of one element (or of none) says nothing, and torch may report any
+        values += (x.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
+    d = _DESCRIPTORS[len(tensors)](*values)
+    return [_byref(d, 24 * i) for i in range(len(tensors))]
 
 
 def _ints(x, *shape):
-    assert x.is_cuda and x.dtype == torch.int32 and x.is_contiguous() and tuple(x.shape) == shape, f"need contiguous int32 {shape}"
+    assert x.is_cuda and x.dtype == torch.int32 and x.shape == shape and x.is_contiguous(), f"need contiguous int32 {shape}"
     return x.data_ptr()
-
-
-def _same(x, *others):
-    assert x.dtype in _TYPES, "heads are float32, bfloat16 or float16"
-    for o in others:
-        assert o.dtype == x.dtype and o.device == x.device, "all tensors of heads have one type and device"
-    return _TYPES[x.dtype]
 
 
 def _window(v):
@@ -389,55 +392,62 @@ def _window(v):
 def _on(stream, x, *made):
     """The stream to launch on; tensors allocated here for this call stay alive until it has used them."""
     if stream is None:
-        return torch.cuda.current_stream(x.device).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(x.get_device())
     for m in made:
         if m is not None:
             m.record_stream(stream)
     return stream.cuda_stream
 
 
-def _scratch(nbytes, x):
-    return torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+def _scratch(need, workspace, x):
+    """(address, bytes) of the caller's workspace or of one made here, and the latter."""
+    if workspace is None:
+        if not need:
+            return None, 0, None
+        workspace = made = torch.empty(need, dtype=torch.uint8, device=x.device)
+        return made.data_ptr(), need, made
+    assert workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    return workspace.data_ptr(), workspace.numel(), None
 
 
-def _room(workspace, made):
-    w = made if workspace is None else workspace
-    if w is None:
-        return None, 0
-    assert w.is_cuda and w.dtype == torch.uint8 and w.is_contiguous()
-    return w.data_ptr(), w.numel()
+def _like(x):
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_k=None, stream=None):
     """Rotary positions with several axes on q [T, Hq, D] and k [T, Hk, D] (k may be None): pair j is turned by
     pos[t, a] * freq[j], a the axis whose section holds j.  pairing: "halves" (j, R + j) or "neighbours" (2j, 2j + 1), R the sum
     of sections.  pos int32 [T, axes], signed; freq float32 [R].  out_q, out_k may be q and k.  Returns (out_q, out_k)."""
-    type = _same(q, *([] if k is None else [k]))
     T, Hq, D = q.shape
-    sections = [int(n) for n in sections]
+    axes = len(sections)
     made_q = made_k = None
     if out_q is None:
-        out_q = made_q = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
-    if k is not None and out_k is None:
-        out_k = made_k = torch.empty(tuple(k.shape), dtype=k.dtype, device=k.device)
-    _same(q, out_q, *([] if k is None else [out_k]))
-    assert tuple(out_q.shape) == (T, Hq, D)
-    assert k is None or (k.shape[0] == T and k.shape[2] == D and out_k.shape == k.shape)
-    assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.numel() == sum(sections)
-    p = _ints(pos, T, len(sections))
-    ref = ctypes.byref
-    _check(lib().znni_rope_axes(type, T, Hq, 0 if k is None else k.shape[1], D, ref(_heads(q)), None if k is None else ref(_heads(k)), p,
-                                freq.data_ptr(), len(sections), (ctypes.c_int * max(1, len(sections)))(*sections), ref(_heads(out_q)),
-                                None if k is None else ref(_heads(out_k)), {"halves": 0, "neighbours": ROPE_NEIGHBOURS}[pairing],
+        out_q = made_q = _like(q)
+    assert out_q.shape == q.shape
+    Hk, dk, do_k = 0, None, None
+    if k is None:
+        dq, do_q = _heads(q, out_q)
+    else:
+        Hk = k.shape[1]
+        if out_k is None:
+            out_k = made_k = _like(k)
+        assert k.shape == (T, Hk, D) and out_k.shape == k.shape
+        dq, dk, do_q, do_k = _heads(q, k, out_q, out_k)
+    assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
+    _check(lib().znni_rope_axes(_TYPES[q.dtype], T, Hq, Hk, D, dq, dk, _ints(pos, T, axes), freq.data_ptr(), axes,
+                                (ctypes.c_int * max(1, axes))(*sections), do_q, do_k, {"halves": 0, "neighbours": ROPE_NEIGHBOURS}[pairing],
                                 _on(stream, q, made_q, made_k)))
     return out_q, out_k
 
 
-def znni_attn_window_workspace(dtype, B, Hq, Hk, D, max_q, max_k, left=None, right=0, sinks=0):
+def _attn_window_need(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks):
     b = ctypes.c_size_t(0)
-    _check(lib().znni_attn_window_workspace(_TYPES[dtype], int(B), int(Hq), int(Hk), int(D), int(max_q), int(max_k), _window(left),
-                                            _window(right), int(sinks), ctypes.byref(b)))
-    return int(b.value)
+    _check(lib().znni_attn_window_workspace(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks, _byref(b)))
+    return b.value
+
+
+def znni_attn_window_workspace(dtype, B, Hq, Hk, D, max_q, max_k, left=None, right=0, sinks=0):
+    return _attn_window_need(_TYPES[dtype], int(B), int(Hq), int(Hk), int(D), int(max_q), int(max_k), _window(left), _window(right), int(sinks))
 
 
 def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sinks=0, scale=None, out=None, workspace=None,
@@ -445,24 +455,21 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     """Attention over B sequences one behind the other: q [Tq, Hq, D], k and v [Tk, Hk, D], cu_q and cu_k int32 [B + 1] their
     starts.  The last query of a sequence stands at its last key; a row at position p sees keys p - left .. p + right (None:
     without an end) and, up to p + right, the first `sinks` keys.  Rows that see nothing are zero.  scale: D ** -0.5."""
-    type = _same(q, k, v)
     Tq, Hq, D = q.shape
-    Hk, B = k.shape[1], cu_q.numel() - 1
+    Tk, Hk, _ = k.shape
+    B = cu_q.numel() - 1
     assert k.shape == v.shape and k.shape[2] == D
-    left, right = _window(left), _window(right)
-    max_q, max_k = int(max_q) if Tq else 0, int(max_k) if k.shape[0] else 0          # tensors of no tokens have no address
-    need = znni_attn_window_workspace(q.dtype, B, Hq, Hk, D, max_q, max_k, left, right, sinks)
-    made = None if workspace is not None else _scratch(need, q)
+    left, right, sinks = _window(left), _window(right), int(sinks)
+    max_q, max_k = int(max_q) if Tq else 0, int(max_k) if Tk else 0          # tensors of no tokens have no address
     made_out = None
     if out is None:
-        out = made_out = torch.empty((Tq, Hq, D), dtype=q.dtype, device=q.device)
-    _same(q, out)
-    assert tuple(out.shape) == (Tq, Hq, D)
-    w, n = _room(workspace, made)
-    ref = ctypes.byref
-    _check(lib().znni_attn_window(type, B, Hq, Hk, D, ref(_heads(q)), ref(_heads(k)), ref(_heads(v)), _ints(cu_q, B + 1), _ints(cu_k, B + 1),
-                                  int(max_q), int(max_k), left, right, int(sinks), float(D ** -0.5 if scale is None else scale),
-                                  ref(_heads(out)), w, n, _on(stream, q, made, made_out)))
+        out = made_out = _like(q)
+    assert out.shape == q.shape
+    dq, dk, dv, do = _heads(q, k, v, out)
+    type = _TYPES[q.dtype]
+    w, n, made = _scratch(_attn_window_need(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
+    _check(lib().znni_attn_window(type, B, Hq, Hk, D, dq, dk, dv, _ints(cu_q, B + 1), _ints(cu_k, B + 1), max_q, max_k, left, right, sinks,
+                                  D ** -0.5 if scale is None else scale, do, w, n, _on(stream, q, made, made_out)))
     return out
 
 
@@ -475,56 +482,52 @@ def kv8_alloc(pages, Hk, D, device="cuda"):
 
 
 def _cache(kcodes, vcodes, scales, Hk, D):
-    for c in (kcodes, vcodes):
-        assert c.is_cuda and c.dtype == torch.uint8 and c.is_contiguous() and c.dim() == 4
+    """Addresses of a cache's three tensors, and its pages."""
     pages = kcodes.shape[0]
-    assert tuple(kcodes.shape) == (pages, Hk, KV8_PAGE, D) and tuple(vcodes.shape) == (pages, Hk, D, KV8_PAGE)
-    assert scales.is_cuda and scales.dtype == torch.float32 and scales.is_contiguous() and tuple(scales.shape) == (pages, Hk, 2)
-    return pages
+    assert kcodes.dtype == vcodes.dtype == torch.uint8 and scales.dtype == torch.float32
+    assert kcodes.is_cuda and kcodes.is_contiguous() and vcodes.is_cuda and vcodes.is_contiguous() and scales.is_cuda and scales.is_contiguous()
+    assert kcodes.shape == (pages, Hk, KV8_PAGE, D) and vcodes.shape == (pages, Hk, D, KV8_PAGE) and scales.shape == (pages, Hk, 2)
+    return kcodes.data_ptr(), vcodes.data_ptr(), scales.data_ptr(), pages
 
 
 def znni_kv8_append(kcodes, vcodes, scales, k, v, table, cu, start, max_new, stream=None):
     """Puts k, v [T, Hk, D] (cu int32 [B + 1]: where each sequence's tokens start) into the cache behind the start[b] tokens
     that sequence b holds; table int32 [B, width] names its pages.  max_new: no sequence gets more."""
-    type = _same(k, v)
-    Hk, D = k.shape[1:]
-    B = start.numel()
+    T, Hk, D = k.shape
+    B, width = table.shape
     assert k.shape == v.shape
-    pages = _cache(kcodes, vcodes, scales, Hk, D)
-    ref = ctypes.byref
-    _check(lib().znni_kv8_append(type, B, Hk, D, ref(_heads(k)), ref(_heads(v)), _ints(cu, B + 1), _ints(start, B), int(max_new) if k.shape[0] else 0,
-                                 kcodes.data_ptr(), vcodes.data_ptr(), scales.data_ptr(), pages, _ints(table, B, table.shape[1]),
-                                 table.shape[1], _on(stream, k)))
+    dk, dv = _heads(k, v)
+    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
+    _check(lib().znni_kv8_append(_TYPES[k.dtype], B, Hk, D, dk, dv, _ints(cu, B + 1), _ints(start, B), int(max_new) if T else 0, kc, vc, sc,
+                                 pages, _ints(table, B, width), width, _on(stream, k)))
+
+
+def _kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks):
+    b = ctypes.c_size_t(0)
+    _check(lib().znni_kv8_attn_workspace(type, B, Lq, Hq, Hk, D, max_len, left, sinks, _byref(b)))
+    return b.value
 
 
 def znni_kv8_attn_workspace(dtype, B, Lq, Hq, Hk, D, max_len, left=None, sinks=0):
-    b = ctypes.c_size_t(0)
-    _check(lib().znni_kv8_attn_workspace(_TYPES[dtype], int(B), int(Lq), int(Hq), int(Hk), int(D), int(max_len), _window(left), int(sinks),
-                                         ctypes.byref(b)))
-    return int(b.value)
+    return _kv8_attn_need(_TYPES[dtype], int(B), int(Lq), int(Hq), int(Hk), int(D), int(max_len), _window(left), int(sinks))
 
 
 def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, sinks=0, scale=None, out=None, workspace=None,
                   stream=None):
     """Attention of the last Lq tokens of each of B sequences, q [B, Lq, Hq, D], over the 8-bit cache.  lens int32 [B]: tokens
     of each sequence, the last Lq among them; max_len: no sequence is longer.  Visibility as for znni_attn_window, right = 0."""
-    type = _same(q)
     B, Lq, Hq, D = q.shape
-    Hk = kcodes.shape[1]
-    pages = _cache(kcodes, vcodes, scales, Hk, D)
-    left = _window(left)
-    need = znni_kv8_attn_workspace(q.dtype, B, Lq, Hq, Hk, D, max_len, left, sinks)
-    made = None if workspace is not None else _scratch(need, q)
+    Hk, width = kcodes.shape[1], table.shape[1]
+    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
+    left, sinks, max_len = _window(left), int(sinks), int(max_len)
     made_out = None
     if out is None:
-        out = made_out = torch.empty((B, Lq, Hq, D), dtype=q.dtype, device=q.device)
-    _same(q, out)
-    assert tuple(out.shape) == (B, Lq, Hq, D) and out.is_contiguous()
-    w, n = _room(workspace, made)
+        out = made_out = _like(q)
+    assert out.shape == q.shape and out.is_contiguous()
     rows = q.reshape(B * Lq, Hq, D)                  # a copy where tokens are not evenly spaced
-    ref = ctypes.byref
-    _check(lib().znni_kv8_attn(type, B, Lq, Hq, Hk, D, ref(_heads(rows)), kcodes.data_ptr(), vcodes.data_ptr(),
-                               scales.data_ptr(), pages, _ints(table, B, table.shape[1]), table.shape[1], _ints(lens, B), int(max_len),
-                               left, int(sinks), float(D ** -0.5 if scale is None else scale), ref(_heads(out.view(B * Lq, Hq, D))), w, n,
-                               _on(stream, q, made, made_out, rows)))
+    dq, do = _heads(rows, out.view(B * Lq, Hq, D))
+    type = _TYPES[q.dtype]
+    w, n, made = _scratch(_kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
+    _check(lib().znni_kv8_attn(type, B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, B, width), width, _ints(lens, B), max_len, left,
+                               sinks, D ** -0.5 if scale is None else scale, do, w, n, _on(stream, q, made, made_out, rows)))
     return out
