@@ -1,8 +1,9 @@
 // kv8.hip -- filling the 8-bit cache of keys and values.
 //
-// A workgroup has one page and head: it reads the tokens that come to the page (16 bytes a thread and load, kept in
-// registers), takes their largest magnitude, decides the scale and writes codes, keys as they come and values through LDS
-// with the tokens innermost.  Bound by memory for prompts, by the chain of dependent reads (start, table, scale, tokens) for single tokens.
+// A workgroup has one page and head.  A thread has four tokens of eight elements, of keys and of values, all loaded at once;
+// the largest magnitudes meet in LDS, then codes go out: keys as they come (lanes along the head), values with the tokens innermost
+// (lanes along the tokens: four codes of an element are a word, sixteen lanes a row of the page).  Bound by memory for prompts, by the
+// chain of dependent reads (start, tokens, scale) for single tokens.
 #include "kv8.h"
 
 namespace znni {
@@ -18,7 +19,8 @@ struct AppendArgs {
 };
 
 constexpr int APPEND_THREADS = 256;
-constexpr int CHUNKS = PAGE * ATTN_DMAX / 8 / APPEND_THREADS;     // of eight values, for a thread
+constexpr int GROUPS = PAGE / 4;         // of four tokens
+static_assert(GROUPS * ATTN_DMAX / 8 <= APPEND_THREADS, "a unit for every thread");
 
 // The least E >= -126 for which a <= 448 * 2^E = 1.75 * 2^(E + 8), a finite and not negative.
 __device__ inline int exponent_of(float a)
@@ -51,129 +53,118 @@ __device__ inline float largest(float a, float x)
     return m <= 3.402823466e38f ? fmaxf(a, m) : a;       // infinities and NaN do not count
 }
 
-__device__ inline float block_max(float a, float* red)
-{
-    for (int o = 32; o; o >>= 1) a = fmaxf(a, __shfl_xor(a, o));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-    __syncthreads();
-    for (int w = 0; w < APPEND_THREADS / 64; ++w) a = fmaxf(a, red[w]);
-    return a;
-}
-
+// Eight elements as they lie in memory.
 template <typename T>
 struct Eight {
-    T x[8];
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+    V v[sizeof(T) / 2];
+    __device__ void load(const T* p)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = ((const V*)p)[i];
+    }
+    __device__ float at(int e) const { return (float)v[e * sizeof(T) / 16][e % (16 / (int)sizeof(T))]; }
 };
 
-template <typename T>
-__device__ inline void load8(const T* p, float* f)
+// The scale of the page after these tokens; *grown is what older codes are multiplied by.
+__device__ inline float new_scale(float top, float was, bool has_old, float* grown)
 {
-    struct alignas(16) { Eight<T> e; } v;
-    const uint4* s = (const uint4*)p;
-    uint4* d = (uint4*)&v;
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) d[i] = s[i];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)v.e.x[i];
+    int E = exponent_of(top);
+    *grown = 1.f;
+    if (has_old) {
+        const int before = (int)(__float_as_uint(was) >> 23 & 255) - 127;
+        if (before >= E) E = before;
+        else *grown = power_of_two(before - E > -126 ? before - E : -126);
+    }
+    return power_of_two(E);
 }
+
+__device__ inline float inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }     // of 2^-126 .. 2^120
 
 template <typename T>
 __global__ __launch_bounds__(APPEND_THREADS) void k_append(AppendArgs a, Heads<const T> k, Heads<const T> v)
 {
-    __shared__ __align__(16) unsigned char turned[ATTN_DMAX * PAGE];
-    __shared__ float red[APPEND_THREADS / 64];
+    __shared__ float2 red[APPEND_THREADS / 64];
     const int b = blockIdx.z, h = blockIdx.y, t = threadIdx.x;
     const int c0 = a.cu[b], n = a.cu[b + 1] - c0, start = a.start[b];
     const long long index = (long long)start / PAGE + blockIdx.x, base = index * PAGE;
     const int s0 = (int)(start > base ? start - base : 0);                       // slots s0 .. s1 are new, those before s0 old
     const int s1 = (int)min((long long)PAGE, (long long)start + n - base);
     if (s0 >= s1 || start < 0 || index >= a.width) return;
+    const int per = a.D / 8;
+    const bool has = t < GROUPS * per;
+    const int kd = t % per * 8, ks = t / per * 4, vd = t / GROUPS * 8, vs = t % GROUPS * 4;      // first element and slot of the units
+    const long long token = c0 + base - start;
+    // (slots of a unit that are not new: some new one, which counts once more and is not written; no branch for each, so that
+    // all loads go out at once)
+    Eight<T> x[4] = {}, y[4] = {};
+    float2 top = {0.f, 0.f};
+    if (has && ks < s1 && ks + 4 > s0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].load(k.row(token + min(max(ks + i, s0), s1 - 1), h) + kd);
+    if (has && vs < s1 && vs + 4 > s0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i].load(v.row(token + min(max(vs + i, s0), s1 - 1), h) + vd);
     const int page = a.table[(long long)b * a.width + index];
     if (page < 0 || page >= a.pages) return;
-    const long long at = ((long long)page * a.Hk + h), token = c0 + base - start;
+    const long long at = (long long)page * a.Hk + h;
+    float2* scale = (float2*)a.scales + at;
+    const float2 was = *scale;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            top.x = largest(top.x, x[i].at(e));
+            top.y = largest(top.y, y[i].at(e));
+        }
+    for (int o = 32; o; o >>= 1) {
+        top.x = fmaxf(top.x, __shfl_xor(top.x, o));
+        top.y = fmaxf(top.y, __shfl_xor(top.y, o));
+    }
+    if ((t & 63) == 0) red[t >> 6] = top;
+    __syncthreads();                          // (every thread has read the old scale, too)
+#pragma unroll
+    for (int w = 0; w < APPEND_THREADS / 64; ++w) {
+        top.x = fmaxf(top.x, red[w].x);
+        top.y = fmaxf(top.y, red[w].y);
+    }
+    float kg, vg;
+    const float kscale = new_scale(top.x, was.x, s0 > 0, &kg), vscale = new_scale(top.y, was.y, s0 > 0, &vg);
+    if (t == 0) *scale = make_float2(kscale, vscale);
+    if (!has) return;
+    const float kby = inverse(kscale), vby = inverse(vscale);
     unsigned char* kc = a.kcodes + at * PAGE * a.D;
     unsigned char* vc = a.vcodes + at * PAGE * a.D;
-    const int per = a.D / 8, chunks = (s1 - s0) * per;
-    // Keys, then values: at most four chunks of eight values a thread.
-    for (int which = 0; which < 2; ++which) {
-        const Heads<const T>& src = which ? v : k;
-        float x[CHUNKS][8], top = 0.f;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int i = t + c * APPEND_THREADS;
-            if (i < chunks) {
-                const int slot = s0 + i / per, d = i % per * 8;
-                load8(src.row(token + slot, h) + d, x[c]);
+    for (int i = 0; i < 4; ++i) {
+        uint2* to = (uint2*)(kc + (ks + i) * a.D + kd);
+        const Eight<T>& f = x[i];
+        if (ks + i >= s1) continue;
+        if (ks + i >= s0) *to = make_uint2(codes_of(f.at(0) * kby, f.at(1) * kby, f.at(2) * kby, f.at(3) * kby), codes_of(f.at(4) * kby, f.at(5) * kby, f.at(6) * kby, f.at(7) * kby));
+        else if (kg != 1.f) *to = make_uint2(rescaled(to->x, kg), rescaled(to->y, kg));
+    }
+    // values: slots vs .. vs + 3 of eight elements
+    if (vs >= s1 || (vs + 4 <= s0 && vg == 1.f)) return;
+    unsigned fresh = 0;                       // bytes that are new, and that are older tokens'
+    unsigned older = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = largest(top, x[c][e]);
-            }
-        }
-        int E = exponent_of(block_max(top, red));
-        float grown = 1.f;
-        if (s0) {
-            const float was = a.scales[at * 2 + which];
-            const int before = (int)(__float_as_uint(was) >> 23 & 255) - 127;
-            if (before >= E) E = before;
-            else grown = power_of_two(before - E > -126 ? before - E : -126);
-        }
-        // every thread has read the old scale before it changes
-        __syncthreads();
-        if (t == 0) a.scales[at * 2 + which] = power_of_two(E);
-        const float up = power_of_two(-E);          // E <= 120
-        if (!which) {
-            if (grown != 1.f)
-                for (int i = t; i < s0 * per * 2; i += APPEND_THREADS) ((unsigned*)kc)[i] = rescaled(((unsigned*)kc)[i], grown);
+    for (int i = 0; i < 4; ++i) {
+        if (vs + i >= s0 && vs + i < s1) fresh |= 255u << (8 * i);
+        if (vs + i < s0) older |= 255u << (8 * i);
+    }
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const int i = t + c * APPEND_THREADS;
-                if (i < chunks) {
-                    float* y = x[c];
+    for (int e = 0; e < 8; ++e) {
+        unsigned* to = (unsigned*)(vc + (vd + e) * PAGE + vs);
+        unsigned w = codes_of(y[0].at(e) * vby, y[1].at(e) * vby, y[2].at(e) * vby, y[3].at(e) * vby);
+        if (fresh == ~0u) {
+            *to = w;
+        } else if (vg == 1.f) {               // bytes of their own: nothing to read first
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= up;
-                    *(uint2*)(kc + (s0 + i / per) * a.D + i % per * 8) =
-                        make_uint2(codes_of(y[0], y[1], y[2], y[3]), codes_of(y[4], y[5], y[6], y[7]));
-                }
-            }
+            for (int i = 0; i < 4; ++i)
+                if (fresh >> (8 * i) & 1) ((unsigned char*)to)[i] = (unsigned char)(w >> (8 * i));
         } else {
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                const int i = t + c * APPEND_THREADS;
-                if (i < chunks) {
-                    const int slot = s0 + i / per, d = i % per * 8;
-                    float* y = x[c];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= up;
-                    const unsigned lo = codes_of(y[0], y[1], y[2], y[3]), hi = codes_of(y[4], y[5], y[6], y[7]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) turned[(d + e) * PAGE + slot] = (unsigned char)((e < 4 ? lo : hi) >> (e % 4 * 8));
-                }
-            }
-            __syncthreads();
-            // sixteen slots of one element of the head: old ones stay (or are rescaled), new ones are set
-            for (int i = t; i < a.D * (PAGE / 16); i += APPEND_THREADS) {
-                const int d = i / (PAGE / 16), g = i % (PAGE / 16) * 16;
-                if (g >= s1 || (g + 16 <= s0 && grown == 1.f)) continue;
-                uint4* dst = (uint4*)(vc + d * PAGE + g);
-                uint4 w = *(const uint4*)(turned + d * PAGE + g);
-                if (g < s0 || g + 16 > s1) {
-                    const uint4 old = *dst;
-                    const unsigned o[4] = {old.x, old.y, old.z, old.w};
-                    unsigned* y = (unsigned*)&w;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned kept = grown != 1.f ? rescaled(o[e], grown) : o[e];
-                        unsigned r = 0;
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            const int slot = g + e * 4 + f;
-                            r |= (slot < s0 ? kept : slot < s1 ? y[e] : o[e]) & (255u << (8 * f));
-                        }
-                        y[e] = r;
-                    }
-                }
-                *dst = w;
-            }
+            const unsigned had = *to;
+            *to = (w & fresh) | (rescaled(had, vg) & older) | (had & ~(fresh | older));
         }
     }
 }
