@@ -169,13 +169,11 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 }
             }
         // reads run four ahead of the products (left alone, the compiler waits for each)
-        if constexpr (!F32) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, F32 ? 2 : 4, 0);
 #pragma unroll
-            for (int n = 0; n < QS * KT; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
+        for (int n = 0; n < QS * KT; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 : 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         if (!wave_rows.all(j0, BN)) {
 #pragma unroll
@@ -222,6 +220,13 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 #pragma unroll
                 for (int x = 0; x < NC; ++x)
                     acc[x] = M::mul(*(const T*)(vb + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), w, acc[x]);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int n = 0; n < 16 * NC; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
         } else {
 #pragma unroll
