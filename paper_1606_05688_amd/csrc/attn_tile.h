@@ -25,7 +25,8 @@ struct AttnTile {
     static constexpr int EC = 16 / sizeof(T);                      // elements of a 16-byte chunk
     static constexpr int RS = NC == 3 ? 128 : 32 * NC;             // elements of a row in LDS
     static constexpr int CR = RS / EC;                             // its chunks
-    static constexpr int PER = BN * CR / THREADS;             // chunks a thread brings
+    static constexpr int PER = BN * CR / THREADS;                  // chunks a thread brings
+    static constexpr int STAGES = NC == 1 ? 4 : NC == 2 ? 3 : 2;   // tiles in LDS: what leaves two workgroups a compute unit, or three
     // Chunk c of key j lies at c ^ swizzle(j).  Scores read one chunk of 32 keys, 16 bytes a lane: 256 bytes of
     // consecutive keys get different places; values read, 16-bit: four keys, 64 bytes each, fp32: two keys four apart, 128 bytes each.
     __device__ static int swizzle_k(int j) { return CR >= 16 ? j & 15 : CR == 8 ? j >> 1 & 7 : j >> 2 & 3; }
@@ -37,14 +38,14 @@ struct AttnTile {
 };
 
 // 16 bytes a lane from memory to LDS, 1024 bytes of a wave from `lds` on.  As assembly, since the compiler, which sees one
-// array in LDS, waits for such a load before any read of it: wait_and_meet() is what waits for these.
+// array in LDS, waits for such a load before any read of it: wait_but_and_meet() is what waits for these.
 __device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
 }
 __device__ inline void to_lds(const void* from, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "memory");
 }
 __device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
@@ -55,7 +56,12 @@ __device__ inline V4 transposed(const char* p)
     return __builtin_bit_cast(V4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
 
-__device__ inline void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All loads but the LEFT newest have come, for all waves.
+template <int LEFT>
+__device__ inline void wait_but_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 
 template <typename T>
 struct Mfma;

@@ -7,6 +7,8 @@
 //   exchange; the weights as they stand are the right operand of  out^T [D][32 rows] += V^T W^T.
 // V^T's operand: 16-bit types by transposing LDS reads, fp32 (products of fp32) by plain ones, keys permuted to match.
 // Rows in LDS are permuted by 16-byte chunks so that neither kind of read meets a bank twice.
+#include <type_traits>
+
 #include "attn_join.h"
 #include "attn_tile.h"
 
@@ -22,8 +24,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
     constexpr int BN = G::BN, KT = BN / 32, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
-    __shared__ __align__(1024) T ks[2][BN * RS];
-    __shared__ __align__(1024) T vs[2][BN * RS];
+    constexpr int STAGES = G::STAGES, ONE = STAGES > 2 ? 2 * PER : 0, TWO = STAGES > 3 ? 4 * PER : 0;      // loads of tiles behind the present one
+    __shared__ __align__(1024) T ks[STAGES][BN * RS];
+    __shared__ __align__(1024) T vs[STAGES][BN * RS];
+    __shared__ int again;
 
     int id = in_runs(blockIdx.x, gridDim.x);
     const int split = id % a.splits; id /= a.splits;
@@ -34,6 +38,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const long long rows = (long long)min(nq, a.max_q) * group, row0 = (long long)tile * BM;
     if (row0 >= rows) return;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
+    if (t == 0) again = 0;
     const long long base = (long long)nk - nq, last = min(row0 + BM, rows) - 1;
     const long long wrow0 = row0 + wave * 32;
     const Sight all_rows(base + row0 / group, base + last / group, nk, a.w);
@@ -60,7 +65,9 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         ko[i] = ((unsigned)j * (unsigned)k.token + (c ^ G::swizzle_k(j)) * EC) * (unsigned)sizeof(T);
         vo[i] = ((unsigned)j * (unsigned)v.token + (c ^ G::swizzle_v(j)) * EC) * (unsigned)sizeof(T);
     }
-    auto bring = [&](int buf, int j0) {
+    // (every wave has 2 PER loads a tile in flight, whichever way: some of its lanes have a chunk of the head)
+    auto bring = [&](int it) {
+        const int buf = (it - begin) % STAGES, j0 = tiles.base(it);
         if (near && a.D == RS && j0 + BN <= nk) {
             const char* kt = (const char*)(kp + j0 * k.token);
             const char* vt = (const char*)(vp + j0 * v.token);
@@ -81,12 +88,18 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     };
     // chunks past a head's end are never brought: zero
     if (a.D < RS)
-        for (int i = t; i < 2 * BN * CR; i += ATTN_THREADS) {
+        for (int i = t; i < STAGES * BN * CR; i += ATTN_THREADS) {
             const int slot = i % (BN * CR), j = slot / CR;
             if ((slot % CR ^ G::swizzle_k(j)) * EC >= a.D) *(uint4*)&ks[i / (BN * CR)][slot * EC] = make_uint4(0, 0, 0, 0);
             if ((slot % CR ^ G::swizzle_v(j)) * EC >= a.D) *(uint4*)&vs[i / (BN * CR)][slot * EC] = make_uint4(0, 0, 0, 0);
         }
-    if (begin < end) bring(0, tiles.base(begin));
+
+    auto bring_first = [&] {
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (begin + i < end) bring(begin + i);
+    };
+    bring_first();
 
     // queries: the right operand of the scores
     constexpr int QS = F32 ? 4 * NC : 2 * NC;          // steps of 8 (4 a lane, in fp32) or 16 elements (8 a lane)
@@ -107,13 +120,6 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         }
     }
 
-    f32x16 acc[NC];
-#pragma unroll
-    for (int x = 0; x < NC; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
-    float top = -INFINITY, sum = 0.f, shift = 0.f;
-    bool wild = false, odd = false;
     const float by = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * 1.44269504088896340736f;       // of 0: what is masked stays so
 
     const float ahead = 8.f / by;
@@ -123,19 +129,38 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     int v_at = F32 ? (4 * h * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)
                    : ((4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
 
+    f32x16 acc[NC];
+    float top, sum;
+    // Values that are not finite leave their mark on rows that do not see them (their weight is zero, and zero times those is NaN).
+    // So the walk over the keys takes place without a thought for them, and where a result is not finite once more, carefully: such values
+    // are taken out of the tiles that only some rows see, and given to those at the end.
+    auto walk = [&](auto carefully) {
+    constexpr bool careful = decltype(carefully)::value;
+    bool odd = false;
+#pragma unroll
+    for (int x = 0; x < NC; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
+    top = -INFINITY;
+    sum = 0.f;
+    float shift = 0.f;
+    bool wild = false;
+    if constexpr (careful) bring_first();
     for (int it = begin; it < end; ++it) {
-        const int buf = (it - begin) & 1, j0 = tiles.base(it);
-        wait_and_meet();
-        if (it + 1 < end) bring(buf ^ 1, tiles.base(it + 1));
-        // values that are not finite, where some rows do not see them: out of the product, into the rows that do at the end
-        if (!all_rows.all(j0, BN)) {
+        const int buf = (it - begin) % STAGES, j0 = tiles.base(it);
+        // this tile is there, the ones behind it may be on their way
+        if (STAGES > 3 && it + 2 < end) wait_but_and_meet<TWO>();
+        else if (STAGES > 2 && it + 1 < end) wait_but_and_meet<ONE>();
+        else wait_but_and_meet<0>();
+        if (it + STAGES - 1 < end) bring(it + STAGES - 1);
+        if constexpr (careful) if (!all_rows.all(j0, BN)) {
             bool x = false;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
                 x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
             }
-            if (__syncthreads_or(x)) {
+            if (__builtin_amdgcn_readfirstlane(__syncthreads_or(x))) {
                 odd = true;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
@@ -157,7 +182,8 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
 #pragma unroll
-        for (int c = 0; c < QS; ++c)
+        for (int c = 0; c < QS; ++c) {
+            if (F32 && 8 * c >= a.D) continue;           // (256 cycles a step; in 16-bit types 32, which a branch would cost)
 #pragma unroll
             for (int n = 0; n < KT; ++n) {
                 const typename M::V x = *(const typename M::V*)(kb + (k_at ^ c * 32) + n * 32 * RS * (int)sizeof(T));
@@ -168,12 +194,15 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     s[n] = M::mul(x, qf[c], s[n]);
                 }
             }
+        }
         // reads run four ahead of the products (left alone, the compiler waits for each)
-        __builtin_amdgcn_sched_group_barrier(0x100, F32 ? 2 : 4, 0);
+        if constexpr (!F32) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-        for (int n = 0; n < QS * KT; ++n) {
-            __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 : 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            for (int n = 0; n < QS * KT; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
         }
         if (!wave_rows.all(j0, BN)) {
 #pragma unroll
@@ -265,6 +294,16 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     }
             }
         }
+    };
+    walk(std::false_type());
+    bool fine = true;
+#pragma unroll
+    for (int x = 0; x < NC; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[x][i]) <= 3.402823466e38f;
+    if (__any(!fine)) again = 1;                     // (set to zero before the first barrier; without a tile all is fine)
+    __syncthreads();
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) walk(std::true_type());
     sum += __shfl_xor(sum, 32);
     if (wrow0 + c32 >= rows) return;
     if (a.splits == 1) {
