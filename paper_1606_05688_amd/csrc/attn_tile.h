@@ -37,11 +37,19 @@ struct AttnTile {
     }
 };
 
+// An address that is the same for all lanes, in scalar registers.
+__device__ inline const void* uniform(const void* p)
+{
+    const unsigned long long x = (unsigned long long)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)(x >> 32));
+    return (const void*)((unsigned long long)hi << 32 | lo);
+}
+
 // 16 bytes a lane from memory to LDS, 1024 bytes of a wave from `lds` on.  As assembly, since the compiler, which sees one
 // array in LDS, waits for such a load before any read of it: wait_but_and_meet() is what waits for these.
 __device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(uniform(base)) : "memory");
 }
 __device__ inline void to_lds(const void* from, unsigned lds)
 {
