@@ -5,6 +5,7 @@ There is no fallback: if the compiled library is missing, loading raises.
 """
 import ctypes
 import os
+import struct
 
 import torch  # imported before the library so both share one HIP runtime
 
@@ -31,13 +32,9 @@ F32, BF16, F16 = 0, 1, 2
 ALL = 2147483647
 KV8_PAGE = 64
 ROPE_NEIGHBOURS = 1
+_PAIRINGS = {"halves": 0, "neighbours": ROPE_NEIGHBOURS}
 
 _lib = None
-
-
-class _Heads(ctypes.Structure):
-    """znni_heads: element (token, head, d) at data[token * token_stride + head * head_stride + d]."""
-    _fields_ = [("data", ctypes.c_void_p), ("token", ctypes.c_longlong), ("head", ctypes.c_longlong)]
 
 
 class ZnniError(RuntimeError):
@@ -96,7 +93,7 @@ def lib():
         for fn in (L.znni_mpf, L.znni_maxpool):
             fn.restype = i
             fn.argtypes = [i, i, i3, i3, vp, vp, vp]
-        hp, ip = vp, ctypes.POINTER(ctypes.c_int)          # (znni_heads *: several lie in one array)
+        hp = ip = vp                     # znni_heads *, int *: bytes that hold them
         L.znni_rope_axes.restype = i
         L.znni_rope_axes.argtypes = [i, i, i, i, i, hp, hp, vp, vp, i, ip, hp, hp, u, vp]
         L.znni_attn_window_workspace.restype = i
@@ -361,23 +358,31 @@ def znni_copy_probe(dst, src, stream=None):
 
 
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-_DESCRIPTORS = {n: ctypes.c_longlong * (3 * n) for n in range(1, 5)}
 _byref = ctypes.byref
+_descriptor = struct.Struct("Pqq").pack          # a znni_heads (data, token stride, head stride) as bytes
 
 
-def _heads(*tensors):
-    """References to the znni_heads of [tokens, heads, D] tensors of one type and device, whose last index is contiguous."""
-    first = tensors[0]
-    dtype, device, values = first.dtype, first.get_device(), []
-    assert first.is_cuda and dtype in _TYPES, "heads are float32, bfloat16 or float16 tensors on the GPU"
-    for x in tensors:
-        assert x.dtype == dtype and x.get_device() == device, "all tensors of heads have one type and device"
-        (tokens, heads, _), (token, head, unit) = x.shape, x.stride()
-        assert unit == 1, "tensors of heads are [tokens, heads, D], D contiguous"
-        # the stride of an axis of one element (or of none) says nothing, and torch may report any
-        values += (x.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
-    d = _DESCRIPTORS[len(tensors)](*values)
-    return [_byref(d, 24 * i) for i in range(len(tensors))]
+def _kind(x):
+    """(znni_type, dtype, device) of a tensor of heads."""
+    assert x.is_cuda and x.dtype in _TYPES, "heads are float32, bfloat16 or float16 tensors on the GPU"
+    return _TYPES[x.dtype], x.dtype, x.get_device()
+
+
+def _heads(x, shape, kind):
+    """The znni_heads of a [tokens, heads, D] tensor of this shape and kind whose last index is contiguous."""
+    assert x.shape == shape and x.dtype == kind[1] and x.get_device() == kind[2], f"need {kind[1]} heads {tuple(shape)} on GPU {kind[2]}"
+    token, head, unit = x.stride()
+    assert unit == 1, "tensors of heads are [tokens, heads, D], D contiguous"
+    # the stride of an axis of one element (or of none) says nothing, and torch may report any
+    return _descriptor(x.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
+
+
+def _result(like, given, shape, kind):
+    """(tensor for a result like this one of that shape and kind, its znni_heads, the tensor again if it was made here)."""
+    if given is not None:
+        return given, _heads(given, shape, kind), None
+    out = torch.empty_like(like) if like.is_contiguous() else torch.empty_like(like, memory_format=torch.contiguous_format)
+    return out, _descriptor(out.data_ptr(), shape[1] * shape[2], shape[2]), out
 
 
 def _ints(x, *shape):
@@ -410,33 +415,24 @@ def _scratch(need, workspace, x):
     return workspace.data_ptr(), workspace.numel(), None
 
 
-def _like(x):
-    return torch.empty_like(x, memory_format=torch.contiguous_format)
-
-
 def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_k=None, stream=None):
     """Rotary positions with several axes on q [T, Hq, D] and k [T, Hk, D] (k may be None): pair j is turned by
     pos[t, a] * freq[j], a the axis whose section holds j.  pairing: "halves" (j, R + j) or "neighbours" (2j, 2j + 1), R the sum
     of sections.  pos int32 [T, axes], signed; freq float32 [R].  out_q, out_k may be q and k.  Returns (out_q, out_k)."""
-    T, Hq, D = q.shape
+    kind = _kind(q)
+    T, Hq, D = shape = q.shape
     axes = len(sections)
-    made_q = made_k = None
-    if out_q is None:
-        out_q = made_q = _like(q)
-    assert out_q.shape == q.shape
-    Hk, dk, do_k = 0, None, None
-    if k is None:
-        dq, do_q = _heads(q, out_q)
-    else:
-        Hk = k.shape[1]
-        if out_k is None:
-            out_k = made_k = _like(k)
-        assert k.shape == (T, Hk, D) and out_k.shape == k.shape
-        dq, dk, do_q, do_k = _heads(q, k, out_q, out_k)
+    out_q, do_q, made_q = _result(q, out_q, shape, kind)
+    Hk, dk, do_k, made_k = 0, None, None, None
+    if k is not None:
+        kshape = k.shape
+        Hk = kshape[1]
+        assert kshape == (T, Hk, D)
+        dk = _heads(k, kshape, kind)
+        out_k, do_k, made_k = _result(k, out_k, kshape, kind)
     assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
-    _check(lib().znni_rope_axes(_TYPES[q.dtype], T, Hq, Hk, D, dq, dk, _ints(pos, T, axes), freq.data_ptr(), axes,
-                                (ctypes.c_int * max(1, axes))(*sections), do_q, do_k, {"halves": 0, "neighbours": ROPE_NEIGHBOURS}[pairing],
-                                _on(stream, q, made_q, made_k)))
+    _check(lib().znni_rope_axes(kind[0], T, Hq, Hk, D, _heads(q, shape, kind), dk, _ints(pos, T, axes), freq.data_ptr(), axes,
+                                struct.pack("%di" % axes, *sections), do_q, do_k, _PAIRINGS[pairing], _on(stream, q, made_q, made_k)))
     return out_q, out_k
 
 
@@ -461,14 +457,11 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     assert k.shape == v.shape and k.shape[2] == D
     left, right, sinks = _window(left), _window(right), int(sinks)
     max_q, max_k = int(max_q) if Tq else 0, int(max_k) if Tk else 0          # tensors of no tokens have no address
-    made_out = None
-    if out is None:
-        out = made_out = _like(q)
-    assert out.shape == q.shape
-    dq, dk, dv, do = _heads(q, k, v, out)
-    type = _TYPES[q.dtype]
-    w, n, made = _scratch(_attn_window_need(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
-    _check(lib().znni_attn_window(type, B, Hq, Hk, D, dq, dk, dv, _ints(cu_q, B + 1), _ints(cu_k, B + 1), max_q, max_k, left, right, sinks,
+    kind = _kind(q)
+    out, do, made_out = _result(q, out, q.shape, kind)
+    w, n, made = _scratch(_attn_window_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
+    _check(lib().znni_attn_window(kind[0], B, Hq, Hk, D, _heads(q, q.shape, kind), _heads(k, k.shape, kind), _heads(v, k.shape, kind),
+                                  _ints(cu_q, B + 1), _ints(cu_k, B + 1), max_q, max_k, left, right, sinks,
                                   D ** -0.5 if scale is None else scale, do, w, n, _on(stream, q, made, made_out)))
     return out
 
@@ -495,11 +488,10 @@ def znni_kv8_append(kcodes, vcodes, scales, k, v, table, cu, start, max_new, str
     that sequence b holds; table int32 [B, width] names its pages.  max_new: no sequence gets more."""
     T, Hk, D = k.shape
     B, width = table.shape
-    assert k.shape == v.shape
-    dk, dv = _heads(k, v)
+    kind = _kind(k)
     kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
-    _check(lib().znni_kv8_append(_TYPES[k.dtype], B, Hk, D, dk, dv, _ints(cu, B + 1), _ints(start, B), int(max_new) if T else 0, kc, vc, sc,
-                                 pages, _ints(table, B, width), width, _on(stream, k)))
+    _check(lib().znni_kv8_append(kind[0], B, Hk, D, _heads(k, k.shape, kind), _heads(v, k.shape, kind), _ints(cu, B + 1), _ints(start, B),
+                                 int(max_new) if T else 0, kc, vc, sc, pages, _ints(table, B, width), width, _on(stream, k)))
 
 
 def _kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks):
@@ -520,14 +512,21 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
     Hk, width = kcodes.shape[1], table.shape[1]
     kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
     left, sinks, max_len = _window(left), int(sinks), int(max_len)
+    kind = _kind(q)
+    shape, rows = (B * Lq, Hq, D), q
     made_out = None
     if out is None:
-        out = made_out = _like(q)
-    assert out.shape == q.shape and out.is_contiguous()
-    rows = q.reshape(B * Lq, Hq, D)                  # a copy where tokens are not evenly spaced
-    dq, do = _heads(rows, out.view(B * Lq, Hq, D))
-    type = _TYPES[q.dtype]
-    w, n, made = _scratch(_kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
-    _check(lib().znni_kv8_attn(type, B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, B, width), width, _ints(lens, B), max_len, left,
-                               sinks, D ** -0.5 if scale is None else scale, do, w, n, _on(stream, q, made, made_out, rows)))
+        out = made_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.get_device() == kind[2] and out.is_contiguous()
+    token, head, unit = q.stride()[1:]
+    if unit != 1 or (B > 1 and Lq > 1 and q.stride(0) != Lq * token):
+        rows = q.contiguous()                        # tokens that are not evenly spaced
+        token, head = Hq * D, D
+    elif Lq == 1:
+        token = q.stride(0)
+    dq = _descriptor(rows.data_ptr(), token if shape[0] > 1 else 0, head if Hq > 1 else 0)
+    w, n, made = _scratch(_kv8_attn_need(kind[0], B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
+    _check(lib().znni_kv8_attn(kind[0], B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, B, width), width, _ints(lens, B), max_len, left,
+                               sinks, D ** -0.5 if scale is None else scale, _descriptor(out.data_ptr(), Hq * D, D), w, n,
+                               _on(stream, q, made, made_out, rows)))
     return out

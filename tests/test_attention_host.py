@@ -14,7 +14,7 @@ NULL, SHAPE, SIZE, WORKSPACE, FLAGS, ALIGN, TYPE = -1, -2, -3, -4, -5, -7, -8
 
 
 def heads(data=P, token=256, head=64):
-    return ctypes.byref(B._Heads(data, token, head))
+    return B._descriptor(data or 0, token, head)
 
 
 def rope(type=B.BF16, T=4, Hq=2, Hk=1, D=64, q=True, k=True, pos=P, freq=P, axes=3, sections=(8, 8, 8), qo=True, ko=True, flags=0):
