@@ -1,12 +1,18 @@
 // attn_window.hip -- attention with a sliding window and first tokens that stay visible, over sequences of any lengths.
 //
-// A workgroup has 128 rows of one key and value head: tokens times the query heads that share it, so that keys and values
-// are read once for all of them; a wave has 32 rows.  It walks the key tiles that any row sees (sinks, then the window),
-// double-buffered in LDS, loads going from memory to LDS without registers in between.  Per tile, on 32x32 products:
+// A workgroup has 128 rows of one key and value head (64, where there are few): tokens times the query heads that share it, so that
+// keys and values are read once for all of them; a wave has 32 rows.  It walks the key tiles that any row sees (sinks, then the
+// window), two to four of them in LDS, loads going from memory to LDS without registers in between.  Per tile, on 32x32 products:
 //   scores^T [keys][32 rows] = K Q^T: a lane has one row, half of its scores; maximum and weights are lane-local but for one
 //   exchange; the weights as they stand are the right operand of  out^T [D][32 rows] += V^T W^T.
 // V^T's operand: 16-bit types by transposing LDS reads, fp32 (products of fp32) by plain ones, keys permuted to match.
 // Rows in LDS are permuted by 16-byte chunks so that neither kind of read meets a bank twice.
+// Rounded: 16-bit weights to their type before the second product (at most 2^8 times a row's largest then), sums stay fp32.
+//
+// bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 530 to 600 us, 800 to 910 TFLOP/s, against 1090 of a large bf16 product.  Bound by
+// the LDS reads of a wave (32 KB a tile, each used for 32 rows), the weights' instructions between the products, and the clock, which falls to
+// 2.2 GHz.  fp32, 2744 tokens, heads 5 x 40: 48 us, matrix units busy for a third.  16-bit calls of few rows: one wave's chain of a
+// tile, 1.1 us.
 #include <type_traits>
 
 #include "attn_join.h"
@@ -16,14 +22,17 @@ namespace znni {
 
 constexpr int BM = 128, ATTN_THREADS = 256;
 
+// The x lowest bits.
+__device__ inline unsigned lowest(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
 
-template <typename T, int NC>
+// SHARE waves share 32 rows, each with its part of a tile's keys: 128 / SHARE rows a workgroup.
+template <typename T, int NC, int SHARE>
 __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
 {
     using G = AttnTile<T, NC, ATTN_THREADS>;
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
-    constexpr int BN = G::BN, KT = BN / 32, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
+    constexpr int ROWS = BM / SHARE, BN = G::BN, KT = BN / 32 / SHARE, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
     constexpr int STAGES = G::STAGES, ONE = STAGES > 2 ? 2 * PER : 0, TWO = STAGES > 3 ? 4 * PER : 0;      // loads of tiles behind the present one
     __shared__ __align__(1024) T ks[STAGES][BN * RS];
     __shared__ __align__(1024) T vs[STAGES][BN * RS];
@@ -35,12 +44,13 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const int hk = id % a.Hk, b = id / a.Hk;
     const int q0 = a.cu_q[b], nq = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
     const int group = a.Hq / a.Hk;
-    const long long rows = (long long)min(nq, a.max_q) * group, row0 = (long long)tile * BM;
+    const long long rows = (long long)min(nq, a.max_q) * group, row0 = (long long)tile * ROWS;
     if (row0 >= rows) return;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
     if (t == 0) again = 0;
-    const long long base = (long long)nk - nq, last = min(row0 + BM, rows) - 1;
-    const long long wrow0 = row0 + wave * 32;
+    const long long base = (long long)nk - nq, last = min(row0 + ROWS, rows) - 1;
+    const int part = wave % SHARE, wrow = wave / SHARE * 32;
+    const long long wrow0 = row0 + wrow;
     const Sight all_rows(base + row0 / group, base + last / group, nk, a.w);
     const Sight wave_rows(base + wrow0 / group, wrow0 < rows ? base + min(wrow0 + 31, last) / group : LLONG_MIN, nk, a.w);
     const long long row = min(wrow0 + c32, rows - 1);
@@ -125,9 +135,9 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const float ahead = 8.f / by;
     // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
-    int k_at = (c32 * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T);
-    int v_at = F32 ? (4 * h * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)
-                   : ((4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
+    int k_at = ((part * KT * 32 + c32) * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T);
+    int v_at = F32 ? ((part * KT * 32 + 4 * h) * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)
+                   : ((part * KT * 32 + 4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
 
     f32x16 acc[NC];
     float top, sum;
@@ -135,165 +145,170 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     // So the walk over the keys takes place without a thought for them, and where a result is not finite once more, carefully: such values
     // are taken out of the tiles that only some rows see, and given to those at the end.
     auto walk = [&](auto carefully) {
-    constexpr bool careful = decltype(carefully)::value;
-    bool odd = false;
+        constexpr bool careful = decltype(carefully)::value;
+        bool odd = false;                        // (in here: known outside, it costs the loop 5 % of its time)
 #pragma unroll
-    for (int x = 0; x < NC; ++x)
+        for (int x = 0; x < NC; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
-    top = -INFINITY;
-    sum = 0.f;
-    float shift = 0.f;
-    bool wild = false;
-    if constexpr (careful) bring_first();
-    for (int it = begin; it < end; ++it) {
-        const int buf = (it - begin) % STAGES, j0 = tiles.base(it);
-        // this tile is there, the ones behind it may be on their way
-        if (STAGES > 3 && it + 2 < end) wait_but_and_meet<TWO>();
-        else if (STAGES > 2 && it + 1 < end) wait_but_and_meet<ONE>();
-        else wait_but_and_meet<0>();
-        if (it + STAGES - 1 < end) bring(it + STAGES - 1);
-        if constexpr (careful) if (!all_rows.all(j0, BN)) {
-            bool x = false;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
-                x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
-            }
-            if (__builtin_amdgcn_readfirstlane(__syncthreads_or(x))) {
-                odd = true;
+            for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
+        top = -INFINITY;
+        sum = 0.f;
+        float shift = 0.f;
+        bool wild = false;
+        if constexpr (careful) bring_first();
+        for (int it = begin; it < end; ++it) {
+            const int buf = (it - begin) % STAGES, j0 = tiles.base(it);
+            // this tile is there, the ones behind it may be on their way
+            if (STAGES > 3 && it + 2 < end) wait_but_and_meet<TWO>();
+            else if (STAGES > 2 && it + 1 < end) wait_but_and_meet<ONE>();
+            else wait_but_and_meet<0>();
+            if (it + STAGES - 1 < end) bring(it + STAGES - 1);
+            if constexpr (careful) if (!all_rows.all(j0, BN)) {
+                bool x = false;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    uint4* y = (uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
-                    *y = make_uint4(M::cleared(y->x), M::cleared(y->y), M::cleared(y->z), M::cleared(y->w));
+                    const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
+                    x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
                 }
-                __syncthreads();
+                if (__builtin_amdgcn_readfirstlane(__syncthreads_or(x))) {
+                    odd = true;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        uint4* y = (uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
+                        *y = make_uint4(M::cleared(y->x), M::cleared(y->y), M::cleared(y->z), M::cleared(y->w));
+                    }
+                    __syncthreads();
+                }
             }
-        }
-        if (!wave_rows.any(j0, BN)) continue;
+            const int wj0 = j0 + part * KT * 32;             // of the wave
+            if (!wave_rows.any(wj0, 32 * KT)) continue;
 
-        // (worked out again for every tile: kept, the addresses of all steps would take the registers)
-        asm volatile("" : "+v"(k_at), "+v"(v_at));
-        const char* kb = (const char*)ks[buf];
-        const char* vb = (const char*)vs[buf];
-        f32x16 s[KT];
-#pragma unroll
-        for (int n = 0; n < KT; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
-#pragma unroll
-        for (int c = 0; c < QS; ++c) {
-            if (F32 && 8 * c >= a.D) continue;           // (256 cycles a step; in 16-bit types 32, which a branch would cost)
-#pragma unroll
-            for (int n = 0; n < KT; ++n) {
-                const typename M::V x = *(const typename M::V*)(kb + (k_at ^ c * 32) + n * 32 * RS * (int)sizeof(T));
-                if constexpr (F32) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[n] = M::mul(x[e], qf[c][e], s[n]);
-                } else {
-                    s[n] = M::mul(x, qf[c], s[n]);
-                }
-            }
-        }
-        // reads run four ahead of the products (left alone, the compiler waits for each)
-        if constexpr (!F32) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-            for (int n = 0; n < QS * KT; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-        }
-        if (!wave_rows.all(j0, BN)) {
+            // (worked out again for every tile: kept, the addresses of all steps would take the registers)
+            asm volatile("" : "+v"(k_at), "+v"(v_at));
+            const char* kb = (const char*)ks[buf];
+            const char* vb = (const char*)vs[buf];
+            f32x16 s[KT];
 #pragma unroll
             for (int n = 0; n < KT; ++n)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int j = j0 + n * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                    s[n][i] = j <= hi && (j >= lo || j < a.w.sinks) ? s[n][i] : -INFINITY;
-                }
-        }
-        float mx[4];
+                for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            mx[x] = s[0][x];
+            for (int c = 0; c < QS; ++c) {
+                if (F32 && 8 * c >= a.D) continue;           // (256 cycles a step; in 16-bit types 32, which a branch would cost)
 #pragma unroll
-            for (int i = 1; i < 4 * KT; ++i) mx[x] = __builtin_elementwise_maximum(mx[x], s[i / 4][4 * (i % 4) + x]);
-        }
-        float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]));
-        // Weights are 2^(by (s - top)), as one multiply-add.  `top` follows the maximum when that is 2^8 ahead: weights stay in
-        // the range of every type, and most tiles have nothing to rescale.  by * top may be so large that its rounding would
-        // leave that range (it is the same for all keys of a row and cancels): then the difference comes first.
-        float offset = shift;
-        if (wild || __any(most > top + ahead)) {
-            most = fmaxf(fmaxf(most, __shfl_xor(most, 32)), top);
-            const float zero = most == -INFINITY ? 0.f : most, old = __builtin_amdgcn_exp2f((top - zero) * by);
-            sum *= old;
+                for (int n = 0; n < KT; ++n) {
+                    const typename M::V x = *(const typename M::V*)(kb + (k_at ^ c * 32) + n * 32 * RS * (int)sizeof(T));
+                    if constexpr (F32) {
 #pragma unroll
-            for (int x = 0; x < NC; ++x) acc[x] *= old;
-            top = most;
-            offset = shift = -zero * by;
-            wild = __any(!(fabsf(shift) < 0x1p26f));
-            if (wild) {
-#pragma unroll
-                for (int n = 0; n < KT; ++n) s[n] -= zero;
-                offset = 0.f;
-            }
-        }
-        float part[2] = {0.f, 0.f};
-        if constexpr (F32) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, offset));
-                part[i & 1] += w;
-#pragma unroll
-                for (int x = 0; x < NC; ++x)
-                    acc[x] = M::mul(*(const T*)(vb + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), w, acc[x]);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-            for (int n = 0; n < 16 * NC; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < 2 * KT; ++n) {
-                typename M::V w;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, offset));
-                    part[e & 1] += p;
-                    w[e] = (T)p;
-                }
-#pragma unroll
-                for (int x = 0; x < NC; ++x) {
-                    const char* from = vb + (v_at ^ x * 64) + 16 * n * RS * (int)sizeof(T);
-                    const typename M::V4 y0 = transposed<typename M::V4>(from), y1 = transposed<typename M::V4>(from + 8 * RS * (int)sizeof(T));
-                    acc[x] = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[x]);
+                        for (int e = 0; e < 4; ++e) s[n] = M::mul(x[e], qf[c][e], s[n]);
+                    } else {
+                        s[n] = M::mul(x, qf[c], s[n]);
+                    }
                 }
             }
-        }
-        sum += part[0] + part[1];
-    }
-    if (odd)
-        for (int it = begin; it < end; ++it) {
-            const int j0 = tiles.base(it);
-            if (all_rows.all(j0, BN)) continue;
-            for (int j = j0; j < min(j0 + BN, nk); ++j) {
-                const bool see = j <= hi && (j >= lo || j < a.w.sinks);
-                const T* vr = vp + (long long)j * v.token;
+            // reads run four ahead of the products (left alone, the compiler waits for each)
+            if constexpr (!F32) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-                for (int x = 0; x < NC; ++x)
+                for (int n = 0; n < QS * KT; ++n) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+            if (!wave_rows.all(wj0, 32 * KT)) {
+#pragma unroll
+                for (int n = 0; n < KT; ++n) {
+                    // one bit for each of 32 keys: two instructions a score
+                    const int j = wj0 + n * 32;
+                    const unsigned see = lowest(hi + 1 - j) & (~lowest(lo - j) | lowest(a.w.sinks - j)), mine = see >> 4 * h;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int d = 32 * x + 8 * (i / 4) + 4 * h + i % 4;
-                        const float y = d < a.D ? (float)vr[d] : 0.f;
-                        if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
+                        const int m = (int)(mine << (31 - 8 * (i / 4) - i % 4)) >> 31;
+                        s[n][i] = __int_as_float((__float_as_int(s[n][i]) & m) | (0xff800000 & ~m));
                     }
+                }
             }
+            float mx[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                mx[x] = s[0][x];
+#pragma unroll
+                for (int i = 1; i < 4 * KT; ++i) mx[x] = __builtin_elementwise_maximum(mx[x], s[i / 4][4 * (i % 4) + x]);
+            }
+            float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]));
+            // Weights are 2^(by (s - top)), as one multiply-add.  `top` follows the maximum when that is 2^8 ahead: weights stay in
+            // the range of every type, and most tiles have nothing to rescale.  by * top may be so large that its rounding would
+            // leave that range (it is the same for all keys of a row and cancels): then the difference comes first.
+            float offset = shift;
+            if (wild || __any(most > top + ahead)) {
+                most = fmaxf(fmaxf(most, __shfl_xor(most, 32)), top);
+                const float zero = most == -INFINITY ? 0.f : most, old = __builtin_amdgcn_exp2f((top - zero) * by);
+                sum *= old;
+#pragma unroll
+                for (int x = 0; x < NC; ++x) acc[x] *= old;
+                top = most;
+                offset = shift = -zero * by;
+                wild = __any(!(fabsf(shift) < 0x1p26f));
+                if (wild) {
+#pragma unroll
+                    for (int n = 0; n < KT; ++n) s[n] -= zero;
+                    offset = 0.f;
+                }
+            }
+            float part[2] = {0.f, 0.f};
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, offset));
+                    part[i & 1] += w;
+#pragma unroll
+                    for (int x = 0; x < NC; ++x)
+                        acc[x] = M::mul(*(const T*)(vb + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), w, acc[x]);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+                for (int n = 0; n < 16 * NC; ++n) {
+                    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 2 * KT; ++n) {
+                    typename M::V w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, offset));
+                        part[e & 1] += p;
+                        w[e] = (T)p;
+                    }
+#pragma unroll
+                    for (int x = 0; x < NC; ++x) {
+                        const char* from = vb + (v_at ^ x * 64) + 16 * n * RS * (int)sizeof(T);
+                        const typename M::V4 y0 = transposed<typename M::V4>(from), y1 = transposed<typename M::V4>(from + 8 * RS * (int)sizeof(T));
+                        acc[x] = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[x]);
+                    }
+                }
+            }
+            sum += part[0] + part[1];
         }
+        if (odd)
+            for (int it = begin; it < end; ++it) {
+                const int j0 = tiles.base(it);
+                if (all_rows.all(j0, BN)) continue;
+                for (int j = j0 + part * KT * 32; j < min(j0 + (part + 1) * KT * 32, nk); ++j) {
+                    const bool see = j <= hi && (j >= lo || j < a.w.sinks);
+                    const T* vr = vp + (long long)j * v.token;
+#pragma unroll
+                    for (int x = 0; x < NC; ++x)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int d = 32 * x + 8 * (i / 4) + 4 * h + i % 4;
+                            const float y = d < a.D ? (float)vr[d] : 0.f;
+                            if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
+                        }
+                }
+            }
     };
     walk(std::false_type());
     bool fine = true;
@@ -305,6 +320,38 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     __syncthreads();
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) walk(std::true_type());
     sum += __shfl_xor(sum, 32);
+    if constexpr (SHARE == 2) {
+        // the second wave's sums by way of the tiles' memory
+        float4* const sums = (float4*)&ks[0][0] + wrow / 32 * NC * 256;
+        float2* const stat = (float2*)&vs[0][0] + wrow / 32 * 64;
+        __syncthreads();
+        if (part) {
+            stat[l] = make_float2(top, sum);
+#pragma unroll
+            for (int x = 0; x < NC; ++x)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) sums[(x * 4 + i / 4) * 64 + l] = make_float4(acc[x][i], acc[x][i + 1], acc[x][i + 2], acc[x][i + 3]);
+        }
+        __syncthreads();
+        if (part) return;
+        const float2 theirs = stat[l];
+        const float most = fmaxf(top, theirs.x), zero = most == -INFINITY ? 0.f : most;
+        // (not zero, which would make NaN of a sum that is infinite)
+        const float f0 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((top - zero) * by), 0x1p-126f);
+        const float f1 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((theirs.x - zero) * by), 0x1p-126f);
+        top = most;
+        sum = f0 * sum + f1 * theirs.y;
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const float4 y = sums[(x * 4 + i / 4) * 64 + l];
+                acc[x][i] = f0 * acc[x][i] + f1 * y.x;
+                acc[x][i + 1] = f0 * acc[x][i + 1] + f1 * y.y;
+                acc[x][i + 2] = f0 * acc[x][i + 2] + f1 * y.z;
+                acc[x][i + 3] = f0 * acc[x][i + 3] + f1 * y.w;
+            }
+    }
     if (wrow0 + c32 >= rows) return;
     if (a.splits == 1) {
         T* y = out.row(q0 + row / group, qh);
@@ -323,7 +370,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 }
             }
     } else {
-        const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wave * 32 + c32;
+        const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wrow + c32;
         const float in_range = top == -INFINITY ? top : fminf(fmaxf(top * by, -3.402823466e38f), 3.402823466e38f);
         if (h == 0) a.stats[at] = make_float2(in_range, sum);
         float* y = a.parts + at * a.D;
@@ -338,23 +385,25 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 }
 
 struct AttnPlan {
-    int tiles, splits, tile_rows;
+    int share, tiles, splits, tile_rows;
     long long groups;                  // workgroups without splitting
     size_t rows;                       // rows of parts
 };
 
 // Few row tiles over many keys: workgroups share the keys of a tile until the chip has two for every compute unit, each with four
 // tiles at least.
-static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
+static AttnPlan attn_plan(int share, int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
 {
     AttnPlan p;
+    const int bm = BM / share;
+    p.share = share;
     const long long rows = (long long)max_q * (Hq / Hk);
-    const long long tiles = (rows + BM - 1) / BM;
+    const long long tiles = (rows + bm - 1) / bm;
     p.tiles = (int)(tiles < INT_MAX ? tiles : INT_MAX);
     p.groups = tiles * Hk * B;
-    p.tile_rows = (int)(rows < BM ? rows : BM);
+    p.tile_rows = (int)(rows < bm ? rows : bm);
     const int bn = type == ZNNI_F32 ? 32 : 64;
-    const long long tokens = (rows < BM ? max_q : BM / (Hq / Hk) + 2);
+    const long long tokens = (rows < bm ? max_q : bm / (Hq / Hk) + 2);
     long long seen = (long long)left + right + tokens + (sinks < max_k ? sinks : max_k);
     if (seen > max_k) seen = max_k;
     const long long most = (seen + bn - 1) / bn / 4;
@@ -365,6 +414,16 @@ static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k,
     return p;
 }
 
+// With up to three workgroups for two compute units a wave has a SIMD nearly to itself and waits for its own instructions: two share
+// the rows (16-bit types; an fp32 tile has 32 keys).  fp16, heads 8 x 64, 300 queries, window of 100, with 128 and with 64 rows a
+// workgroup: 24 workgroups 10.8 and 9.4 us, 288: 13.8 and 11.9, 384: 14.1 and 13.3, 480: 14.6 and 17.7, 768: 18.2 and 23.0; bf16, heads
+// 16 of 4 x 128, 2048 queries, 256 workgroups: 61.6 and 54.7 us.
+static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
+{
+    const AttnPlan p = attn_plan(1, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    return type != ZNNI_F32 && p.groups <= 384 ? attn_plan(2, type, B, Hq, Hk, max_q, max_k, left, right, sinks) : p;
+}
+
 template <typename T>
 static znni_status launch_attn(const AttnArgs& a, int max_q, const AttnPlan& p, const znni_heads* q, const znni_heads* k, const znni_heads* v,
                                const znni_heads* out, hipStream_t st)
@@ -372,11 +431,20 @@ static znni_status launch_attn(const AttnArgs& a, int max_q, const AttnPlan& p, 
     const dim3 grid((unsigned)(p.groups * p.splits)), block(ATTN_THREADS);
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v);
     const Heads<T> o = heads_of<T>(out);
-    switch ((a.D + 31) / 32) {
-        case 1: k_attn<T, 1><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-        case 2: k_attn<T, 2><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-        case 3: k_attn<T, 3><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-        default: k_attn<T, 4><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+    auto launch = [&](auto share) {
+        constexpr int SHARE = decltype(share)::value;
+        switch ((a.D + 31) / 32) {
+            case 1: k_attn<T, 1, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            case 2: k_attn<T, 2, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            case 3: k_attn<T, 3, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            default: k_attn<T, 4, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+        }
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (p.share == 2) launch(std::integral_constant<int, 2>());
+        else launch(std::integral_constant<int, 1>());
+    } else {
+        launch(std::integral_constant<int, 1>());
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;

@@ -67,6 +67,43 @@ def test_against_the_definition(dtype, case):
     assert torch.equal(got, again)
 
 
+def _many(x, n, copies):
+    """The sequences of n tokens, one behind the other, so many times over."""
+    return x.repeat(copies, 1, 1), n * copies
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", [c for c in CASES if sum(c[3]) < 400], ids=lambda c: "-".join(str(x) for x in c[:3]) + f"-{len(c[3])}x{c[3][0]}")
+def test_many_sequences(dtype, case):
+    """So many row tiles that no keys are shared out: every copy of a sequence has the definition's result, and the same one."""
+    Hq, Hk, D, nq, nk, left, right, sinks = case
+    copies = 400 // (Hk * len(nq)) + 1
+    print(f"[attn many] {dtype} {case} {copies}", flush=True)
+    q, k, v = _inputs(sum(nq) + D + 1, nq, nk, Hq, Hk, D, dtype)
+    ref = _reference(q, k, v, nq, nk, left, right, sinks, D ** -0.5)
+    (qs, nqs), (ks, nks), (vs, _) = _many(q, nq, copies), _many(k, nk, copies), _many(v, nk, copies)
+    got = _run(qs.to(DEV), ks.to(DEV), vs.to(DEV), nqs, nks, left, right, sinks).view(copies, sum(nq), Hq, D)
+    assert torch.equal(got, got[:1].expand_as(got))
+    R.check(got[0], ref[0], R.bound(dtype, *ref), str(case))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("copies", [1, 210])
+def test_values_that_are_not_finite_in_both_halves_of_a_tile(dtype, copies):
+    """Infinities that some rows of a tile see and others do not, few rows (two waves share them) and many."""
+    Hq, Hk, D, n, left = 2, 2, 64, 90, 20
+    q, k, v = _inputs(12, [n], [n], Hq, Hk, D, dtype)
+    for j, e in ((3, 0), (40, 9), (50, 33), (70, 63), (89, 5)):
+        v[j, j % 2, e] = float("inf") if j % 4 else float("-inf")
+    ref = _reference(q, k, v, [n], [n], left, 0, 2, D ** -0.5)
+    (qs, nq), (ks, nk), (vs, _) = _many(q, [n], copies), _many(k, [n], copies), _many(v, [n], copies)
+    got = _run(qs.to(DEV), ks.to(DEV), vs.to(DEV), nq, nk, left, 0, 2).view(copies, n, Hq, D)
+    assert torch.equal(got, got[:1].expand_as(got))
+    clean = torch.isfinite(ref[0])
+    assert clean.any() and not clean.all() and not torch.isnan(ref[0]).any()
+    R.check(got[0], ref[0], torch.where(clean, R.bound(dtype, *ref), torch.ones_like(ref[0])))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_long_sequences_and_sharp_weights(dtype):
     """Many tiles, scores far apart: the running maximum moves late in the sequence, most weights vanish."""
