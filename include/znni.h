@@ -1,5 +1,5 @@
 /*
- * znni.h -- C ABI of the pruned-FFT 3D convolutional layer for AMD MI355X (gfx950).
+ * znni.h -- C ABI of the pruned-FFT 3D convolutional layer for AMD MI355X (gfx950), and of attention over its voxels.
  *
  * The layer (paper Section IV): a batch of S inputs, each a tuple of f images of n^3 voxels, is turned into
  * S tuples of f' images of n'^3 voxels, n' = n - k + 1, by
@@ -38,7 +38,8 @@
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*; NULL = the default stream) and the call
  *     returns without synchronising, except znni_conv3d_fft_profile, which synchronises the stream.
  *   - Results are deterministic: no floating-point atomics, fixed summation order.
- *   - Tensors are dense, row-major, last index fastest.  All values and sums are fp32; some kernels form products
+ *   - Tensors are dense, row-major, last index fastest (attention: strided heads of three types, its own conventions below).
+ *     All values and sums are fp32; some kernels form products
  *     of fp32 values on fp16 matrix instructions, each value split in two scaled halves (22 bits and a sign), with results
  *     as close to the 64-bit ones as fp32 products give for values of ordinary spread: a value down to 2^-17 of the
  *     largest that shares its scale keeps 22 bits, one below it has an absolute error of 2^-40 of that largest value.
@@ -335,6 +336,7 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *
  * Conventions, besides those at the top of this file:
  *   - `type` is a znni_type, the type of all tensors of heads of a call; scores, softmax statistics and sums are fp32.
+ *     znni_attn_window rounds weights to a 16-bit type before they meet the values; znni_kv8_attn keeps 16 bits of them and more.
  *   - A tensor of heads is a znni_heads: element (token t, head h, d) lies at data[t * token + h * head + d], strides in
  *     elements.  Data 16-byte aligned, strides multiples of 16 bytes (zero and negative ones included for what is read),
  *     D a multiple of 8.  ZNNI_ERR_ALIGN, ZNNI_ERR_UNSUPPORTED_SIZE.
@@ -344,8 +346,8 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *     values that a row does not see, infinities and NaN included, has no influence on it.  A row that sees nothing, or whose weights
  *     are all zero, is zero.
  *   - Lengths of zero are fine; a call without tokens launches nothing.
- *   - Results are deterministic; a row's depends on how many keys its call says there may be at most (max_k, max_len), by
- *     rounding only.
+ *   - Results are deterministic; a row's depends on how many sequences, rows and keys its call says there may be (B, max_q,
+ *     max_k, max_len), by rounding only.
  */
 typedef enum { ZNNI_F32 = 0, ZNNI_BF16 = 1, ZNNI_F16 = 2 } znni_type;
 
@@ -415,7 +417,8 @@ znni_status znni_kv8_append(int type, int B, int Hk, int D, const znni_heads* k,
 /*
  * Attention of the last Lq tokens of each of B sequences over the cache: q [B*Lq][Hq][D] -> out, token i of sequence b at
  * position p = lens[b] - Lq + i (rows before the first token are zero), visibility with right = 0.  lens [B] device, counted
- * as at most width * ZNNI_KV8_PAGE; max_len: no sequence is longer (host; the launch is made for it).  Keys and values are taken as they stand in the cache.
+ * as at most width * ZNNI_KV8_PAGE; max_len: no sequence is longer (host; the launch is made for it).  Keys and
+ * values are taken as they stand in the cache.
  * Other arguments as for znni_attn_window and znni_kv8_append.
  */
 znni_status znni_kv8_attn_workspace(int type, int B, int Lq, int Hq, int Hk, int D, int max_len, int left, int sinks, size_t* bytes);

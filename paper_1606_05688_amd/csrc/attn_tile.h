@@ -49,7 +49,8 @@ __device__ inline const void* uniform(const void* p)
 // array in LDS, waits for such a load before any read of it: wait_but_and_meet() is what waits for these.
 __device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(uniform(base)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset),
+                 "s"(uniform(base)) : "memory");
 }
 __device__ inline void to_lds(const void* from, unsigned lds)
 {
@@ -79,7 +80,10 @@ struct Mfma<bf16> {
     typedef bf16 V4 __attribute__((ext_vector_type(4)));
     __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     __device__ static bool odd(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u); }
+    __device__ static unsigned cleared(unsigned x)
+    {
+        return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+    }
 };
 template <>
 struct Mfma<f16> {
@@ -87,7 +91,10 @@ struct Mfma<f16> {
     typedef f16 V4 __attribute__((ext_vector_type(4)));
     __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     __device__ static bool odd(unsigned x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
-    __device__ static unsigned cleared(unsigned x) { return ((x & 0x7c00u) == 0x7c00u ? 0u : x & 0xffffu) | ((x & 0x7c000000u) == 0x7c000000u ? 0u : x & 0xffff0000u); }
+    __device__ static unsigned cleared(unsigned x)
+    {
+        return ((x & 0x7c00u) == 0x7c00u ? 0u : x & 0xffffu) | ((x & 0x7c000000u) == 0x7c000000u ? 0u : x & 0xffff0000u);
+    }
 };
 template <>
 struct Mfma<float> {

