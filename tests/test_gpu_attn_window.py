@@ -119,6 +119,19 @@ def test_long_sequences_and_sharp_weights(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [8, 40, 64, 72, 128])
+@pytest.mark.parametrize("n", [600, 1100, 2500])
+def test_keys_shared_by_workgroups(dtype, D, n):
+    """Two to twenty parts a row, of heads of all widths; one sequence is so short that most of its parts are empty."""
+    Hq, Hk, nq, nk = 6, 2, [33, 1, 2], [n, n - 100, 2]
+    print(f"[attn parts] {dtype} {D} {n}", flush=True)
+    q, k, v = _inputs(n + D, nq, nk, Hq, Hk, D, dtype)
+    for left, sinks in ((ALL, 0), (n // 2, 70)):
+        ref = _reference(q, k, v, nq, nk, left, 0, sinks, D ** -0.5)
+        R.check(_run(q.to(DEV), k.to(DEV), v.to(DEV), nq, nk, left, 0, sinks), ref[0], R.bound(dtype, *ref), f"{left} {sinks}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("nq", [1, 70])
 def test_what_a_row_does_not_see_has_no_influence(dtype, nq):
     """NaN and infinities in keys and values behind a row's window, before it and beside the sequence; rows that see one take it."""
