@@ -343,8 +343,8 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *   - Query head h reads key and value head h / (Hq / Hk); Hk divides Hq.  ZNNI_ERR_SHAPE.
  *   - A row at position p sees key j if j <= p + right and (j >= p - left or j < sinks): the window, and the first tokens,
  *     which stay visible to all rows that come after them.  ZNNI_ALL for left or right: no end.  What lies in keys and
- *     values that a row does not see, infinities and NaN included, has no influence on it.  A row that sees nothing, or whose weights
- *     are all zero, is zero.
+ *     values that a row does not see, infinities and NaN included, has no influence on it.  A row that sees nothing, or whose
+ *     weights are all zero, is zero.
  *   - Lengths of zero are fine; a call without tokens launches nothing.
  *   - Results are deterministic; a row's depends on how many sequences, rows and keys its call says there may be (B, max_q,
  *     max_k, max_len), by rounding only.
@@ -402,11 +402,11 @@ znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_
  * and their table entries may be anything; an entry outside [0, pages) that is reached counts as a page that no row sees.
  *
  * znni_kv8_append puts k, v [cu[B]][Hk][D] behind the start[b] tokens that sequence b holds already (cu [B+1], start [B],
- * device; max_new: no sequence gets more).  scale = 2^E with the least E for which the largest finite magnitude among the page's
- * tokens is at most 448 * 2^E, E >= -126, by the tokens that are there: a page that is filled further keeps its scale if the new
- * tokens fit and else gets the larger one, its older codes rounded once more (exact above the type's subnormals).  Rounding
- * to nearest, ties to even; infinities become the largest code, NaN stay.  No page may be named twice by what a call writes.
- * Tokens past the table's width or in pages outside [0, pages) are dropped.
+ * device; max_new: no sequence gets more, at most 2^23 pages).  scale = 2^E with the least E for which the largest finite
+ * magnitude among the page's tokens is at most 448 * 2^E, E >= -126, by the tokens that are there: a page that is filled further
+ * keeps its scale if the new tokens fit and else gets the larger one, its older codes rounded once more (exact above the type's
+ * subnormals).  Rounding to nearest, ties to even; infinities become the largest code, NaN stay.  No page may be named twice by
+ * what a call writes.  Tokens past the table's width or in pages outside [0, pages) are dropped.
  */
 #define ZNNI_KV8_PAGE 64
 

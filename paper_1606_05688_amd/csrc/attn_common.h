@@ -48,6 +48,15 @@ __host__ __device__ inline bool sees(long long p, int j, const Window& w)
     return j <= p + w.right && (j >= p - w.left || j < w.sinks);
 }
 
+// A dimension of a launch has fewer than 2^32 threads: workgroups (of up to 256) past this many go on in the second dimension.
+constexpr unsigned LAUNCH_X = 1u << 23;
+static inline dim3 launch_of(long long groups)
+{
+    const unsigned x = groups < LAUNCH_X ? (unsigned)groups : LAUNCH_X;
+    return dim3(x, (unsigned)((groups + x - 1) / x));
+}
+__device__ inline long long group_id() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Host-side checks that the operators share.
 static inline bool type_ok(int type) { return type == ZNNI_F32 || type == ZNNI_BF16 || type == ZNNI_F16; }
 static inline int type_size(int type) { return type == ZNNI_F32 ? 4 : 2; }

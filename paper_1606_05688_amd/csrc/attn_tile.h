@@ -13,7 +13,8 @@ struct AttnArgs {
     const int* cu_k;
     Window w;
     float scale;
-    int B, max_q, tiles, splits, tile_rows;     // row tiles of a sequence, workgroups that share a tile's keys, rows of a tile in `parts`
+    int groups, max_q;
+    int tiles, splits, tile_rows;     // row tiles of a sequence, workgroups that share a tile's keys, rows of a tile in `parts`
     float* parts;
     float2* stats;
 };

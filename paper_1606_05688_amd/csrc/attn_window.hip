@@ -11,8 +11,8 @@
 //
 // bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 530 to 600 us, 800 to 910 TFLOP/s, against 1090 of a large bf16 product.  Bound by
 // the LDS reads of a wave (32 KB a tile, each used for 32 rows), the weights' instructions between the products, and the clock, which falls to
-// 2.2 GHz.  fp32, 2744 tokens, heads 5 x 40: 40 us and 4 for the join, matrix units busy for a third.  16-bit calls of few rows: one wave's chain of a
-// tile, 1.1 us.
+// 2.2 GHz.  fp32, 2744 tokens, heads 5 x 40: 40 us and 4 for the join, matrix units busy for a third.  16-bit calls of few rows: one
+// wave's chain of a tile, 1.1 us.
 #include <type_traits>
 
 #include "attn_join.h"
@@ -38,26 +38,28 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     __shared__ __align__(1024) T vs[STAGES][BN * RS];
     __shared__ int again;
 
-    int id = in_runs(blockIdx.x, gridDim.x);
+    const long long group = group_id();
+    if (group >= a.groups) return;
+    int id = in_runs((int)group, a.groups);
     const int split = id % a.splits; id /= a.splits;
     const int tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
     const int hk = id % a.Hk, b = id / a.Hk;
     const int q0 = a.cu_q[b], nq = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
-    const int group = a.Hq / a.Hk;
-    const long long rows = (long long)min(nq, a.max_q) * group, row0 = (long long)tile * ROWS;
+    const int shared = a.Hq / a.Hk;
+    const long long rows = (long long)min(nq, a.max_q) * shared, row0 = (long long)tile * ROWS;
     if (row0 >= rows) return;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
     if (t == 0) again = 0;
     const long long base = (long long)nk - nq, last = min(row0 + ROWS, rows) - 1;
     const int part = wave % SHARE, wrow = wave / SHARE * 32;
     const long long wrow0 = row0 + wrow;
-    const Sight all_rows(base + row0 / group, base + last / group, nk, a.w);
-    const Sight wave_rows(base + wrow0 / group, wrow0 < rows ? base + min(wrow0 + 31, last) / group : LLONG_MIN, nk, a.w);
+    const Sight all_rows(base + row0 / shared, base + last / shared, nk, a.w);
+    const Sight wave_rows(base + wrow0 / shared, wrow0 < rows ? base + min(wrow0 + 31, last) / shared : LLONG_MIN, nk, a.w);
     const long long row = min(wrow0 + c32, rows - 1);
-    const long long pos = base + row / group;                                          // of the lane
+    const long long pos = base + row / shared;                                         // of the lane
     int lo, hi;
     window_of(pos, nk, a.w, &lo, &hi);
-    const int qh = hk * group + (int)(row % group);
+    const int qh = hk * shared + (int)(row % shared);
 
     const KeyTiles<BN> tiles(all_rows);
     const int per = (tiles.n + a.splits - 1) / a.splits, begin = split * per, end = min(tiles.n, begin + per);
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     constexpr int QS = F32 ? 4 * NC : 2 * NC;          // steps of 8 (4 a lane, in fp32) or 16 elements (8 a lane)
     typename M::V qf[QS];
     {
-        const T* p = q.row(q0 + row / group, qh);
+        const T* p = q.row(q0 + row / shared, qh);
 #pragma unroll
         for (int c = 0; c < QS; ++c) {
             const int d = (2 * c + h) * EC;
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     }
     if (wrow0 + c32 >= rows) return;
     if (a.splits == 1) {
-        T* y = out.row(q0 + row / group, qh);
+        T* y = out.row(q0 + row / shared, qh);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
@@ -425,10 +427,10 @@ static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k,
 }
 
 template <typename T>
-static znni_status launch_attn(const AttnArgs& a, int max_q, const AttnPlan& p, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const AttnPlan& p, const znni_heads* q, const znni_heads* k, const znni_heads* v,
                                const znni_heads* out, hipStream_t st)
 {
-    const dim3 grid((unsigned)(p.groups * p.splits)), block(ATTN_THREADS);
+    const dim3 grid = launch_of(a.groups), block(ATTN_THREADS);
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v);
     const Heads<T> o = heads_of<T>(out);
     auto launch = [&](auto share) {
@@ -449,7 +451,7 @@ static znni_status launch_attn(const AttnArgs& a, int max_q, const AttnPlan& p, 
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;
     const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, a.parts, a.stats};
-    return launch_join<T>(j, a.B, o, st);
+    return launch_join<T>(j, B, o, st);
 }
 
 static znni_status attn_shape(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
@@ -496,13 +498,13 @@ znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_
         if (!heads_aligned(h, type)) return ZNNI_ERR_ALIGN;
     const AttnPlan p = attn_plan(type, B, Hq, Hk, max_q, max_k, left, right, sinks);
     float* parts = (float*)workspace;
-    const AttnArgs a = {Hq, Hk, D, cu_q, cu_k, {left, right, sinks}, scale, B, max_q, p.tiles, p.splits, p.tile_rows, parts,
+    const AttnArgs a = {Hq, Hk, D, cu_q, cu_k, {left, right, sinks}, scale, (int)(p.groups * p.splits), max_q, p.tiles, p.splits, p.tile_rows, parts,
                         (float2*)(parts + p.rows * D)};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
-        case ZNNI_F32: return launch_attn<float>(a, max_q, p, q, k, v, out, st);
-        case ZNNI_BF16: return launch_attn<bf16>(a, max_q, p, q, k, v, out, st);
-        default: return launch_attn<f16>(a, max_q, p, q, k, v, out, st);
+        case ZNNI_F32: return launch_attn<float>(a, B, max_q, p, q, k, v, out, st);
+        case ZNNI_BF16: return launch_attn<bf16>(a, B, max_q, p, q, k, v, out, st);
+        default: return launch_attn<f16>(a, B, max_q, p, q, k, v, out, st);
     }
 }
 

@@ -176,8 +176,9 @@ template <typename T>
 static znni_status launch_append(const AppendArgs& a, int B, int max_new, const znni_heads* k, const znni_heads* v, hipStream_t st)
 {
     // tokens that begin anywhere in a page reach this many
-    const int reach = (int)(((long long)max_new + PAGE - 2) / PAGE + 1);
-    k_append<T><<<dim3((unsigned)reach, (unsigned)a.Hk, (unsigned)B), dim3(APPEND_THREADS), 0, st>>>(a, heads_of<const T>(k), heads_of<const T>(v));
+    const long long reach = ((long long)max_new + PAGE - 2) / PAGE + 1, pages = reach < a.width ? reach : a.width;
+    if (pages > LAUNCH_X) return ZNNI_ERR_SHAPE;
+    k_append<T><<<dim3((unsigned)pages, (unsigned)a.Hk, (unsigned)B), dim3(APPEND_THREADS), 0, st>>>(a, heads_of<const T>(k), heads_of<const T>(v));
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }
 

@@ -33,7 +33,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeArgs a, Heads<const T
 {
     typedef T V __attribute__((ext_vector_type(VEC)));
     __shared__ float2 table[ROPE_TABLE];
-    const long long t0 = (long long)blockIdx.x * a.tokens;
+    const long long t0 = group_id() * a.tokens;
+    if (t0 >= a.T) return;
     const int nt = (int)min((long long)a.tokens, a.T - t0);
     for (int i = threadIdx.x; i < nt * a.R; i += ROPE_THREADS) {
         const int tok = i / a.R, j = i - tok * a.R;
@@ -95,10 +96,10 @@ static znni_status launch_rope(RopeArgs a, bool neighbours, const znni_heads* q,
     const int units = (a.Hq + a.Hk) * a.D / WIDE;
     const int want = (2 * ROPE_THREADS + units - 1) / units;
     if (a.tokens > want) a.tokens = want;
-    const int spread = (a.T + 1023) / 1024;                          // at least 1024 workgroups if there are tokens for them
+    const int spread = (int)((a.T + 1023LL) / 1024);                          // at least 1024 workgroups if there are tokens for them
     if (a.tokens > spread) a.tokens = spread;
     if (a.tokens < 1) a.tokens = 1;
-    const dim3 grid((unsigned)((a.T + a.tokens - 1) / a.tokens)), block(ROPE_THREADS);
+    const dim3 grid = launch_of(((long long)a.T + a.tokens - 1) / a.tokens), block(ROPE_THREADS);
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k);
     const Heads<T> oq = heads_of<T>(qo), ok = heads_of<T>(ko);
     // Every row starts at a multiple of 16 bytes, and so does its second half unless the turned part ends inside a vector.

@@ -87,6 +87,16 @@ def test_many_sequences(dtype, case):
     R.check(got[0], ref[0], R.bound(dtype, *ref), str(case))
 
 
+def test_more_workgroups_than_a_dimension_of_a_launch_holds():
+    """Many sequences under a bound on their length that is far too large: most workgroups have nothing to do."""
+    n, D = 65535, 8
+    q, k, v = (x.to(DEV) for x in _inputs(5, [n], [n], 1, 1, D, torch.bfloat16))
+    cu = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    few = B.znni_attn_window(q, k, v, cu, cu, 1, 1)
+    assert torch.equal(few, v)                      # a row's only key is its own
+    assert torch.equal(B.znni_attn_window(q, k, v, cu, cu, 128 * 130, 1), few)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("copies", [1, 210])
 def test_values_that_are_not_finite_in_both_halves_of_a_tile(dtype, copies):
