@@ -73,6 +73,9 @@ __device__ inline void wait_but_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
+// What this wave wrote to LDS is there for all (loads into LDS go on).
+__device__ inline void wait_and_meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <typename T>
 struct Mfma;
 template <>

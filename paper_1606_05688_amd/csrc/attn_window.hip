@@ -1,6 +1,6 @@
 // attn_window.hip -- attention with a sliding window and first tokens that stay visible, over sequences of any lengths.
 //
-// A workgroup has 128 rows of one key and value head (64, where there are few): tokens times the query heads that share it, so that
+// A workgroup has 128 rows of one key and value head (64 or 32, where there are few): tokens times the query heads that share it, so that
 // keys and values are read once for all of them; a wave has 32 rows.  It walks the key tiles that any row sees (sinks, then the
 // window), two to four of them in LDS, loads going from memory to LDS without registers in between.  Per tile, on 32x32 products:
 //   scores^T [keys][32 rows] = K Q^T: a lane has one row, half of its scores; maximum and weights are lane-local but for one
@@ -25,21 +25,37 @@ constexpr int BM = 128, ATTN_THREADS = 256;
 // The x lowest bits.
 __device__ inline unsigned lowest(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
 
-// SHARE waves share 32 rows, each with its part of a tile's keys: 128 / SHARE rows a workgroup.
+// SHARE waves share 32 rows, 128 / SHARE rows a workgroup.  Two: each has half of a tile's keys, their sums are joined at the end.  Four (fp32, whose
+// tile has no more keys than a product): each has a quarter of the head's elements, in the scores, whose parts are added through LDS, and
+// in the results; softmax statistics are the same in all four.
 template <typename T, int NC, int SHARE>
 __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
 {
     using G = AttnTile<T, NC, ATTN_THREADS>;
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
-    constexpr int ROWS = BM / SHARE, BN = G::BN, KT = BN / 32 / SHARE, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
+    constexpr bool BY_D = F32 && SHARE == 4;
+    constexpr int BN = G::BN, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER;
+    constexpr int ROWS = BM / SHARE, KT = BY_D ? 1 : BN / 32 / SHARE, NA = BY_D ? 1 : NC;
     constexpr int STAGES = G::STAGES, ONE = STAGES > 2 ? 2 * PER : 0, TWO = STAGES > 3 ? 4 * PER : 0;      // loads of tiles behind the present one
     __shared__ __align__(1024) T ks[STAGES][BN * RS];
     __shared__ __align__(1024) T vs[STAGES][BN * RS];
-    __shared__ int again;
+    __shared__ float4 partial[BY_D ? 4 * 4 * 64 : 1];          // scores of a wave's elements; a flag
 
     const long long group = group_id();
     if (group >= a.groups) return;
+    // whether x holds anywhere in the workgroup
+    auto any_of_all = [&](bool x) {
+        int* const flag = (int*)partial;
+        __syncthreads();
+        if (threadIdx.x == 0) *flag = 0;
+        __syncthreads();
+        if (__any(x) && (threadIdx.x & 63) == 0) *flag = 1;
+        __syncthreads();
+        const int y = __builtin_amdgcn_readfirstlane(*flag);
+        __syncthreads();
+        return y;
+    };
     int id = in_runs((int)group, a.groups);
     const int split = id % a.splits; id /= a.splits;
     const int tile = a.tiles - 1 - id % a.tiles; id /= a.tiles;
@@ -49,9 +65,8 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const long long rows = (long long)min(nq, a.max_q) * shared, row0 = (long long)tile * ROWS;
     if (row0 >= rows) return;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
-    if (t == 0) again = 0;
     const long long base = (long long)nk - nq, last = min(row0 + ROWS, rows) - 1;
-    const int part = wave % SHARE, wrow = wave / SHARE * 32;
+    const int part = wave % SHARE, wrow = wave / SHARE * 32, key_part = BY_D ? 0 : part * KT * 32;
     const long long wrow0 = row0 + wrow;
     const Sight all_rows(base + row0 / shared, base + last / shared, nk, a.w);
     const Sight wave_rows(base + wrow0 / shared, wrow0 < rows ? base + min(wrow0 + 31, last) / shared : LLONG_MIN, nk, a.w);
@@ -114,13 +129,14 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     bring_first();
 
     // queries: the right operand of the scores
-    constexpr int QS = F32 ? 4 * NC : 2 * NC;          // steps of 8 (4 a lane, in fp32) or 16 elements (8 a lane)
+    constexpr int QS = BY_D ? RS / 32 : F32 ? 4 * NC : 2 * NC;       // steps of 8 (4 a lane, in fp32) or 16 elements (8 a lane)
+    const int q_part = BY_D ? part * QS : 0, d_part = BY_D ? part * 32 : 0;       // the wave's first step, its first element of results
     typename M::V qf[QS];
     {
         const T* p = q.row(q0 + row / shared, qh);
 #pragma unroll
         for (int c = 0; c < QS; ++c) {
-            const int d = (2 * c + h) * EC;
+            const int d = (2 * (q_part + c) + h) * EC;
             if (d < a.D) qf[c] = *(const typename M::V*)(p + d);
             else
 #pragma unroll
@@ -137,11 +153,11 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const float ahead = 8.f / by;
     // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
-    int k_at = ((part * KT * 32 + c32) * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T);
-    int v_at = F32 ? ((part * KT * 32 + 4 * h) * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)
-                   : ((part * KT * 32 + 4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
+    int k_at = (((key_part + c32) * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T)) ^ q_part * 32;
+    int v_at = F32 ? (((key_part + 4 * h) * RS + (c32 ^ G::swizzle_v(4 * h) * EC)) * (int)sizeof(T)) ^ d_part * 4
+                   : ((key_part + 4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
 
-    f32x16 acc[NC];
+    f32x16 acc[NA];
     float top, sum;
     // Values that are not finite leave their mark on rows that do not see them (their weight is zero, and zero times those is NaN).
     // So the walk over the keys takes place without a thought for them, and where a result is not finite once more, carefully: such values
@@ -150,7 +166,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         constexpr bool careful = decltype(carefully)::value;
         bool odd = false;                        // (in here: known outside, it costs the loop 5 % of its time)
 #pragma unroll
-        for (int x = 0; x < NC; ++x)
+        for (int x = 0; x < NA; ++x)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
         top = -INFINITY;
@@ -172,7 +188,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
                     x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
                 }
-                if (__builtin_amdgcn_readfirstlane(__syncthreads_or(x))) {
+                if (any_of_all(x)) {
                     odd = true;
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
@@ -182,7 +198,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     __syncthreads();
                 }
             }
-            const int wj0 = j0 + part * KT * 32;             // of the wave
+            const int wj0 = j0 + key_part;                   // of the wave
             if (!wave_rows.any(wj0, 32 * KT)) continue;
 
             // (worked out again for every tile: kept, the addresses of all steps would take the registers)
@@ -196,7 +212,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < QS; ++c) {
-                if (F32 && 8 * c >= a.D) continue;           // (256 cycles a step; in 16-bit types 32, which a branch would cost)
+                if (F32 && 8 * (q_part + c) >= a.D) continue;           // (256 cycles a step; in 16-bit types 32, which a branch would cost)
 #pragma unroll
                 for (int n = 0; n < KT; ++n) {
                     const typename M::V x = *(const typename M::V*)(kb + (k_at ^ c * 32) + n * 32 * RS * (int)sizeof(T));
@@ -216,6 +232,23 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
+            }
+            if constexpr (BY_D) {
+                // so far of this wave's elements of the head
+                float4* const mine = partial + part * 256 + l;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mine[i * 64] = make_float4(s[0][4 * i], s[0][4 * i + 1], s[0][4 * i + 2], s[0][4 * i + 3]);
+                wait_and_meet();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4* const p = partial + i * 64 + l;
+                    const float4 y0 = p[0], y1 = p[256], y2 = p[512], y3 = p[768];
+                    s[0][4 * i] = (y0.x + y1.x) + (y2.x + y3.x);
+                    s[0][4 * i + 1] = (y0.y + y1.y) + (y2.y + y3.y);
+                    s[0][4 * i + 2] = (y0.z + y1.z) + (y2.z + y3.z);
+                    s[0][4 * i + 3] = (y0.w + y1.w) + (y2.w + y3.w);
+                }
+                if (d_part >= a.D) continue;
             }
             if (!wave_rows.all(wj0, 32 * KT)) {
 #pragma unroll
@@ -247,7 +280,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 const float zero = most == -INFINITY ? 0.f : most, old = __builtin_amdgcn_exp2f((top - zero) * by);
                 sum *= old;
 #pragma unroll
-                for (int x = 0; x < NC; ++x) acc[x] *= old;
+                for (int x = 0; x < NA; ++x) acc[x] *= old;
                 top = most;
                 offset = shift = -zero * by;
                 wild = __any(!(fabsf(shift) < 0x1p26f));
@@ -264,12 +297,12 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], by, offset));
                     part[i & 1] += w;
 #pragma unroll
-                    for (int x = 0; x < NC; ++x)
+                    for (int x = 0; x < NA; ++x)
                         acc[x] = M::mul(*(const T*)(vb + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), w, acc[x]);
                 }
                 __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-                for (int n = 0; n < 16 * NC; ++n) {
+                for (int n = 0; n < 16 * NA; ++n) {
                     __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -285,7 +318,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                         w[e] = (T)p;
                     }
 #pragma unroll
-                    for (int x = 0; x < NC; ++x) {
+                    for (int x = 0; x < NA; ++x) {
                         const char* from = vb + (v_at ^ x * 64) + 16 * n * RS * (int)sizeof(T);
                         const typename M::V4 y0 = transposed<typename M::V4>(from), y1 = transposed<typename M::V4>(from + 8 * RS * (int)sizeof(T));
                         acc[x] = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[x]);
@@ -298,14 +331,14 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             for (int it = begin; it < end; ++it) {
                 const int j0 = tiles.base(it);
                 if (all_rows.all(j0, BN)) continue;
-                for (int j = j0 + part * KT * 32; j < min(j0 + (part + 1) * KT * 32, nk); ++j) {
+                for (int j = j0 + key_part; j < min(j0 + key_part + 32 * KT, nk); ++j) {
                     const bool see = j <= hi && (j >= lo || j < a.w.sinks);
                     const T* vr = vp + (long long)j * v.token;
 #pragma unroll
-                    for (int x = 0; x < NC; ++x)
+                    for (int x = 0; x < NA; ++x)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int d = 32 * x + 8 * (i / 4) + 4 * h + i % 4;
+                            const int d = d_part + 32 * x + 8 * (i / 4) + 4 * h + i % 4;
                             const float y = d < a.D ? (float)vr[d] : 0.f;
                             if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
                         }
@@ -315,12 +348,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     walk(std::false_type());
     bool fine = true;
 #pragma unroll
-    for (int x = 0; x < NC; ++x)
+    for (int x = 0; x < NA; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[x][i]) <= 3.402823466e38f;
-    if (__any(!fine)) again = 1;                     // (set to zero before the first barrier; without a tile all is fine)
-    __syncthreads();
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane(again), 0)) walk(std::true_type());
+    if (__builtin_expect(any_of_all(!fine && d_part < a.D), 0)) walk(std::true_type());
     sum += __shfl_xor(sum, 32);
     if constexpr (SHARE == 2) {
         // the second wave's sums by way of the tiles' memory
@@ -330,7 +361,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         if (part) {
             stat[l] = make_float2(top, sum);
 #pragma unroll
-            for (int x = 0; x < NC; ++x)
+            for (int x = 0; x < NA; ++x)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) sums[(x * 4 + i / 4) * 64 + l] = make_float4(acc[x][i], acc[x][i + 1], acc[x][i + 2], acc[x][i + 3]);
         }
@@ -344,7 +375,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         top = most;
         sum = f0 * sum + f1 * theirs.y;
 #pragma unroll
-        for (int x = 0; x < NC; ++x)
+        for (int x = 0; x < NA; ++x)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const float4 y = sums[(x * 4 + i / 4) * 64 + l];
@@ -359,10 +390,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         T* y = out.row(q0 + row / shared, qh);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-        for (int x = 0; x < NC; ++x)
+        for (int x = 0; x < NA; ++x)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int d = 32 * x + 2 * i + 4 * h;
+                const int d = d_part + 32 * x + 2 * i + 4 * h;
                 if (d < a.D) {
                     typedef T T4 __attribute__((ext_vector_type(4)));
                     T4 o;
@@ -374,13 +405,13 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     } else {
         const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wrow + c32;
         const float in_range = top == -INFINITY ? top : fminf(fmaxf(top * by, -3.402823466e38f), 3.402823466e38f);
-        if (h == 0) a.stats[at] = make_float2(in_range, sum);
+        if (h == 0 && d_part == 0) a.stats[at] = make_float2(in_range, sum);
         float* y = a.parts + at * a.D;
 #pragma unroll
-        for (int x = 0; x < NC; ++x)
+        for (int x = 0; x < NA; ++x)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int d = 32 * x + 2 * i + 4 * h;
+                const int d = d_part + 32 * x + 2 * i + 4 * h;
                 if (d < a.D) *(float4*)(y + d) = make_float4(acc[x][i], acc[x][i + 1], acc[x][i + 2], acc[x][i + 3]);
             }
     }
@@ -416,14 +447,18 @@ static AttnPlan attn_plan(int share, int type, int B, int Hq, int Hk, int max_q,
     return p;
 }
 
-// With up to three workgroups for two compute units a wave has a SIMD nearly to itself and waits for its own instructions: two share
-// the rows (16-bit types; an fp32 tile has 32 keys).  fp16, heads 8 x 64, 300 queries, window of 100, with 128 and with 64 rows a
-// workgroup: 24 workgroups 10.8 and 9.4 us, 288: 13.8 and 11.9, 384: 14.1 and 13.3, 480: 14.6 and 17.7, 768: 18.2 and 23.0; bf16, heads
-// 16 of 4 x 128, 2048 queries, 256 workgroups: 61.6 and 54.7 us.
+// 16-bit types: with up to three workgroups for two compute units a wave has a SIMD nearly to itself and waits for its own
+// instructions: two share the rows.  fp16, heads 8 x 64, 300 queries, window of 100, with 128 and with 64 rows a workgroup: 24 workgroups
+// 10.8 and 9.4 us, 288: 13.8 and 11.9, 384: 14.1 and 13.3, 480: 14.6 and 17.7, 768: 18.2 and 23.0; bf16, heads 16 of 4 x 128, 2048
+// queries, 256 workgroups: 61.6 and 54.7 us.
+// fp32: where one wave's rows are all, the other three would wait for its products (heads 16 of 4 x 128, one query, 8 sequences of 8192
+// keys: 89 us with one wave at work, 60 with four; of 500: 27 and 16); and where workgroups are very few (heads 5 x 40, 200 queries: 20.9
+// and 16.8, 400: 19.5 and 16.2, 700, 30 workgroups: 21.1 and 24.0; 16 of 4 x 128, 100 queries: 24.6 and 13.0, 256 of 4000 keys: 89 and 105).
 static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
 {
     const AttnPlan p = attn_plan(1, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
-    return type != ZNNI_F32 && p.groups <= 384 ? attn_plan(2, type, B, Hq, Hk, max_q, max_k, left, right, sinks) : p;
+    const int share = type != ZNNI_F32 ? (p.groups <= 384 ? 2 : 1) : p.groups <= 20 || (long long)max_q * (Hq / Hk) <= 32 ? 4 : 1;
+    return share == 1 ? p : attn_plan(share, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
 }
 
 template <typename T>
@@ -446,7 +481,8 @@ static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const AttnPl
         if (p.share == 2) launch(std::integral_constant<int, 2>());
         else launch(std::integral_constant<int, 1>());
     } else {
-        launch(std::integral_constant<int, 1>());
+        if (p.share == 4) launch(std::integral_constant<int, 4>());
+        else launch(std::integral_constant<int, 1>());
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;

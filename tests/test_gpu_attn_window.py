@@ -87,6 +87,20 @@ def test_many_sequences(dtype, case):
     R.check(got[0], ref[0], R.bound(dtype, *ref), str(case))
 
 
+@pytest.mark.parametrize("D", [8, 32, 40, 72, 96, 104, 128])
+@pytest.mark.parametrize("nq,Hq", [(1, 1), (1, 8), (7, 4), (33, 1), (129, 3), (450, 5)])
+def test_few_rows_in_fp32(nq, Hq, D):
+    """Workgroups whose waves share the elements of a head, and (450 rows of five heads) those whose waves do not."""
+    nk, left, sinks = [nq + 301], 150, 5
+    print(f"[attn few] {nq} {Hq} {D}", flush=True)
+    q, k, v = _inputs(nq + D, [nq], nk, Hq, 1, D, torch.float32)
+    v[nq // 2, 0, D - 1] = float("inf")             # seen by some rows of long ones, by none of a single one
+    ref = _reference(q, k, v, [nq], nk, left, 2, sinks, D ** -0.5)
+    clean = torch.isfinite(ref[0])
+    got = _run(q.to(DEV), k.to(DEV), v.to(DEV), [nq], nk, left, 2, sinks)
+    R.check(got, ref[0], torch.where(clean, R.bound(torch.float32, *ref), torch.ones_like(ref[0])))
+
+
 def test_more_workgroups_than_a_dimension_of_a_launch_holds():
     """Many sequences under a bound on their length that is far too large: most workgroups have nothing to do."""
     n, D = 65535, 8
