@@ -49,8 +49,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeArgs a, Heads<const T
     const int turned = NEIGHBOURS ? a.D / VEC : a.R / VEC;
     const int units = NEIGHBOURS ? turned : turned + (a.D - 2 * a.R) / VEC;
     const int heads = a.Hq + a.Hk, n = nt * heads * units;
+    // (one thread's unit, head and token move on by the same steps: no division for each)
+    const int rows = ROPE_THREADS / units, du = ROPE_THREADS - rows * units, dtok = rows / heads, dh = rows - dtok * heads;
+    int u = threadIdx.x % units, h = threadIdx.x / units % heads, tok = threadIdx.x / units / heads;
     for (int i = threadIdx.x; i < n; i += ROPE_THREADS) {
-        const int row = i / units, u = i - row * units, tok = row / heads, h = row - tok * heads;
         const T* x = h < a.Hq ? q.row(t0 + tok, h) : k.row(t0 + tok, h - a.Hq);
         T* y = h < a.Hq ? qo.row(t0 + tok, h) : ko.row(t0 + tok, h - a.Hq);
         const float2* cs = table + tok * a.R;
@@ -83,6 +85,11 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeArgs a, Heads<const T
             const int at = 2 * a.R + (u - turned) * VEC;
             *(V*)(y + at) = *(const V*)(x + at);
         }
+        u += du;
+        h += dh;
+        tok += dtok;
+        if (u >= units) { u -= units; ++h; }
+        if (h >= heads) { h -= heads; ++tok; }
     }
 }
 
@@ -102,9 +109,12 @@ static znni_status launch_rope(RopeArgs a, bool neighbours, const znni_heads* q,
     const dim3 grid = launch_of(((long long)a.T + a.tokens - 1) / a.tokens), block(ROPE_THREADS);
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k);
     const Heads<T> oq = heads_of<T>(qo), ok = heads_of<T>(ko);
-    // Every row starts at a multiple of 16 bytes, and so does its second half unless the turned part ends inside a vector.
+    // Every row starts at a multiple of 16 bytes; its second half, and what passes, at a multiple of the widest vector that divides R.
+    // (Wide vectors from wherever the half starts, the last one element by element, are slower: R = 44 148 us against 83, 45 200 and 178.)
     if (neighbours) k_rope<T, WIDE, true><<<grid, block, 0, st>>>(a, qi, ki, pos, freq, oq, ok);
     else if (a.R % WIDE == 0) k_rope<T, WIDE, false><<<grid, block, 0, st>>>(a, qi, ki, pos, freq, oq, ok);
+    else if (WIDE > 4 && a.R % 4 == 0) k_rope<T, 4, false><<<grid, block, 0, st>>>(a, qi, ki, pos, freq, oq, ok);
+    else if (a.R % 2 == 0) k_rope<T, 2, false><<<grid, block, 0, st>>>(a, qi, ki, pos, freq, oq, ok);
     else k_rope<T, 1, false><<<grid, block, 0, st>>>(a, qi, ki, pos, freq, oq, ok);
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }

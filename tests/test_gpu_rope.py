@@ -84,3 +84,22 @@ def test_negative_positions_turn_back_and_are_the_gradient():
         down, _ = B.znni_rope_axes(x - 0.5 * d, None, p, f, (10, 10, 12))
         slope = ((up.double() - down.double()) * y.double()).sum()
         assert abs(slope - (grad.double() * d.double()).sum()) <= 2.0 ** -18 * (y.abs().double() * 2 * (x.abs() + d.abs()).amax(-1, keepdim=True)).sum()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [16, 24, 40, 64])
+def test_turned_parts_of_any_width(dtype, D):
+    """Halves that begin anywhere: every number of pairs, into a new tensor and in place."""
+    for pairs in range(1, D // 2 + 1):
+        q, k, pos, freq = _case(pairs, 37, 3, 1, D, (pairs,), dtype)
+        exp = R.rope(q.double(), pos, freq, (pairs,), "halves")
+        dev = q.to(DEV)
+        got, _ = B.znni_rope_axes(dev, k.to(DEV), pos.to(DEV), freq.to(DEV), (pairs,))
+        B.znni_rope_axes(dev, None, pos.to(DEV), freq.to(DEV), (pairs,), out_q=dev)
+        assert torch.equal(got, dev)
+        assert torch.equal(got.cpu()[..., 2 * pairs:], q[..., 2 * pairs:])
+        # the two products and their sum in fp32, sines to 2^-21, one rounding to the type
+        size = q.double().abs()
+        u, v = size[..., :pairs], size[..., pairs:2 * pairs]
+        bound = R.UNIT[dtype] * exp[..., :2 * pairs].abs() + torch.cat([u + v, u + v], -1) * 2.0 ** -20 + 2.0 ** -25
+        assert ((got.cpu().double() - exp)[..., :2 * pairs].abs() <= bound).all(), (dtype, D, pairs)
