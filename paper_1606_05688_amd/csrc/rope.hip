@@ -49,10 +49,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeArgs a, Heads<const T
     const int turned = NEIGHBOURS ? a.D / VEC : a.R / VEC;
     const int units = NEIGHBOURS ? turned : turned + (a.D - 2 * a.R) / VEC;
     const int heads = a.Hq + a.Hk, n = nt * heads * units;
-    // (one thread's unit, head and token move on by the same steps: no division for each)
-    const int rows = ROPE_THREADS / units, du = ROPE_THREADS - rows * units, dtok = rows / heads, dh = rows - dtok * heads;
-    int u = threadIdx.x % units, h = threadIdx.x / units % heads, tok = threadIdx.x / units / heads;
     for (int i = threadIdx.x; i < n; i += ROPE_THREADS) {
+        const int row = i / units, u = i - row * units, tok = row / heads, h = row - tok * heads;
         const T* x = h < a.Hq ? q.row(t0 + tok, h) : k.row(t0 + tok, h - a.Hq);
         T* y = h < a.Hq ? qo.row(t0 + tok, h) : ko.row(t0 + tok, h - a.Hq);
         const float2* cs = table + tok * a.R;
@@ -85,11 +83,6 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope(RopeArgs a, Heads<const T
             const int at = 2 * a.R + (u - turned) * VEC;
             *(V*)(y + at) = *(const V*)(x + at);
         }
-        u += du;
-        h += dh;
-        tok += dtok;
-        if (u >= units) { u -= units; ++h; }
-        if (h >= heads) { h -= heads; ++tok; }
     }
 }
 
