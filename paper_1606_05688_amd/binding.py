@@ -378,11 +378,11 @@ def _heads(x, shape, kind):
 
 
 def _result(like, given, shape, kind):
-    """(tensor for a result like this one of that shape and kind, its znni_heads, the tensor again if it was made here)."""
+    """(tensor for a result like this one of that shape and kind, its znni_heads)."""
     if given is not None:
-        return given, _heads(given, shape, kind), None
+        return given, _heads(given, shape, kind)
     out = torch.empty_like(like) if like.is_contiguous() else torch.empty_like(like, memory_format=torch.contiguous_format)
-    return out, _descriptor(out.data_ptr(), shape[1] * shape[2], shape[2]), out
+    return out, _descriptor(out.data_ptr(), shape[1] * shape[2], shape[2])
 
 
 def _ints(x, *shape):
@@ -394,45 +394,55 @@ def _window(v):
     return ALL if v is None else int(v)
 
 
-def _on(stream, x, *made):
-    """The stream to launch on; tensors allocated here for this call stay alive until it has used them."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(x.get_device())
-    for m in made:
-        if m is not None:
-            m.record_stream(stream)
-    return stream.cuda_stream
+def _current(x):
+    """The stream to launch on: torch's current one."""
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
+
+
+def _on(stream, x, call, *args, **kw):
+    """`call` with `stream` as torch's current one: all that it copies and allocates is ordered with its launches.  Results belong to
+    that stream then, and stay until the caller's own stream has used them."""
+    assert stream.device == x.device, f"need a stream of {x.device}"
+    callers = torch.cuda.current_stream(x.device)
+    with torch.cuda.stream(stream):
+        results = call(*args, **kw)
+    for r in results if isinstance(results, tuple) else (results,):
+        if r is not None:
+            r.record_stream(callers)
+    return results
 
 
 def _scratch(need, workspace, x):
-    """(address, bytes) of the caller's workspace or of one made here, and the latter."""
+    """(address, bytes) of the caller's workspace or of one made here, and the tensor."""
     if workspace is None:
         if not need:
             return None, 0, None
-        workspace = made = torch.empty(need, dtype=torch.uint8, device=x.device)
-        return made.data_ptr(), need, made
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        return workspace.data_ptr(), need, workspace
     assert workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()
-    return workspace.data_ptr(), workspace.numel(), None
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
 def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_k=None, stream=None):
     """Rotary positions with several axes on q [T, Hq, D] and k [T, Hk, D] (k may be None): pair j is turned by
     pos[t, a] * freq[j], a the axis whose section holds j.  pairing: "halves" (j, R + j) or "neighbours" (2j, 2j + 1), R the sum
     of sections.  pos int32 [T, axes], signed; freq float32 [R].  out_q, out_k may be q and k.  Returns (out_q, out_k)."""
+    if stream is not None:
+        return _on(stream, q, znni_rope_axes, q, k, pos, freq, sections, pairing, out_q, out_k)
     kind = _kind(q)
     T, Hq, D = shape = q.shape
     axes = len(sections)
-    out_q, do_q, made_q = _result(q, out_q, shape, kind)
-    Hk, dk, do_k, made_k = 0, None, None, None
+    out_q, do_q = _result(q, out_q, shape, kind)
+    Hk, dk, do_k = 0, None, None
     if k is not None:
         kshape = k.shape
         Hk = kshape[1]
         assert kshape == (T, Hk, D)
         dk = _heads(k, kshape, kind)
-        out_k, do_k, made_k = _result(k, out_k, kshape, kind)
+        out_k, do_k = _result(k, out_k, kshape, kind)
     assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
     _check(lib().znni_rope_axes(kind[0], T, Hq, Hk, D, _heads(q, shape, kind), dk, _ints(pos, T, axes), freq.data_ptr(), axes,
-                                struct.pack("%di" % axes, *sections), do_q, do_k, _PAIRINGS[pairing], _on(stream, q, made_q, made_k)))
+                                struct.pack("%di" % axes, *sections), do_q, do_k, _PAIRINGS[pairing], _current(q)))
     return out_q, out_k
 
 
@@ -451,6 +461,8 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     """Attention over B sequences one behind the other: q [Tq, Hq, D], k and v [Tk, Hk, D], cu_q and cu_k int32 [B + 1] their
     starts.  The last query of a sequence stands at its last key; a row at position p sees keys p - left .. p + right (None:
     without an end) and, up to p + right, the first `sinks` keys.  Rows that see nothing are zero.  scale: D ** -0.5."""
+    if stream is not None:
+        return _on(stream, q, znni_attn_window, q, k, v, cu_q, cu_k, max_q, max_k, left, right, sinks, scale, out, workspace)
     Tq, Hq, D = q.shape
     Tk, Hk, _ = k.shape
     B = cu_q.numel() - 1
@@ -458,11 +470,11 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     left, right, sinks = _window(left), _window(right), int(sinks)
     max_q, max_k = int(max_q) if Tq else 0, int(max_k) if Tk else 0          # tensors of no tokens have no address
     kind = _kind(q)
-    out, do, made_out = _result(q, out, q.shape, kind)
-    w, n, made = _scratch(_attn_window_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
+    out, do = _result(q, out, q.shape, kind)
+    w, n, held = _scratch(_attn_window_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
     _check(lib().znni_attn_window(kind[0], B, Hq, Hk, D, _heads(q, q.shape, kind), _heads(k, k.shape, kind), _heads(v, k.shape, kind),
                                   _ints(cu_q, B + 1), _ints(cu_k, B + 1), max_q, max_k, left, right, sinks,
-                                  D ** -0.5 if scale is None else scale, do, w, n, _on(stream, q, made, made_out)))
+                                  D ** -0.5 if scale is None else scale, do, w, n, _current(q)))
     return out
 
 
@@ -486,12 +498,14 @@ def _cache(kcodes, vcodes, scales, Hk, D):
 def znni_kv8_append(kcodes, vcodes, scales, k, v, table, cu, start, max_new, stream=None):
     """Puts k, v [T, Hk, D] (cu int32 [B + 1]: where each sequence's tokens start) into the cache behind the start[b] tokens
     that sequence b holds; table int32 [B, width] names its pages.  max_new: no sequence gets more."""
+    if stream is not None:
+        return _on(stream, k, znni_kv8_append, kcodes, vcodes, scales, k, v, table, cu, start, max_new)
     T, Hk, D = k.shape
     B, width = table.shape
     kind = _kind(k)
     kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
     _check(lib().znni_kv8_append(kind[0], B, Hk, D, _heads(k, k.shape, kind), _heads(v, k.shape, kind), _ints(cu, B + 1), _ints(start, B),
-                                 int(max_new) if T else 0, kc, vc, sc, pages, _ints(table, B, width), width, _on(stream, k)))
+                                 int(max_new) if T else 0, kc, vc, sc, pages, _ints(table, B, width), width, _current(k)))
 
 
 def _kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks):
@@ -508,15 +522,16 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
                   stream=None):
     """Attention of the last Lq tokens of each of B sequences, q [B, Lq, Hq, D], over the 8-bit cache.  lens int32 [B]: tokens
     of each sequence, the last Lq among them; max_len: no sequence is longer.  Visibility as for znni_attn_window, right = 0."""
+    if stream is not None:
+        return _on(stream, q, znni_kv8_attn, q, kcodes, vcodes, scales, table, lens, max_len, left, sinks, scale, out, workspace)
     B, Lq, Hq, D = q.shape
     Hk, width = kcodes.shape[1], table.shape[1]
     kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
     left, sinks, max_len = _window(left), int(sinks), int(max_len)
     kind = _kind(q)
     shape, rows = (B * Lq, Hq, D), q
-    made_out = None
     if out is None:
-        out = made_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     assert out.shape == q.shape and out.dtype == q.dtype and out.get_device() == kind[2] and out.is_contiguous()
     token, head, unit = q.stride()[1:]
     if unit != 1 or (B > 1 and Lq > 1 and q.stride(0) != Lq * token):
@@ -525,8 +540,8 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
     elif Lq == 1:
         token = q.stride(0)
     dq = _descriptor(rows.data_ptr(), token if shape[0] > 1 else 0, head if Hq > 1 else 0)
-    w, n, made = _scratch(_kv8_attn_need(kind[0], B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
+    w, n, held = _scratch(_kv8_attn_need(kind[0], B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
     _check(lib().znni_kv8_attn(kind[0], B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, B, width), width, _ints(lens, B), max_len, left,
                                sinks, D ** -0.5 if scale is None else scale, _descriptor(out.data_ptr(), Hq * D, D), w, n,
-                               _on(stream, q, made, made_out, rows)))
+                               _current(q)))
     return out
