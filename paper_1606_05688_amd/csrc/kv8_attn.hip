@@ -432,7 +432,8 @@ znni_status znni_kv8_attn(int type, int B, int Lq, int Hq, int Hk, int D, const 
         return ZNNI_ERR_ALIGN;
     const int splits = kv8_splits(B, Lq, Hq, Hk, max_len, left, sinks);
     float* parts = (float*)workspace;
-    const Kv8Args a = {Lq, Hq, Hk, D, pages, width, splits, kcodes, vcodes, scales, table, lens, {left, 0, sinks}, scale, parts,
+    // (without pages no entry of the table is one: it is not read, and may be NULL)
+    const Kv8Args a = {Lq, Hq, Hk, D, pages, pages ? width : 0, splits, kcodes, vcodes, scales, table, lens, {left, 0, sinks}, scale, parts,
                        (float2*)(parts + kv8_part_rows(B, Lq, Hq, Hk, splits) * D)};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
