@@ -5,11 +5,12 @@
 namespace znni {
 
 // Part s of row r (of a batch entry and key head) of `rows` lies at ((bh * tiles + r / tile_rows) * splits + s) * tile_rows
-// + r % tile_rows: D weighted sums of values, and their maximum (in powers of two) and sum of weights in `stats`.
+// + r % tile_rows: D weighted sums of values, and their maximum (`by` times that in powers of two) and sum of weights in `stats`.
 struct JoinArgs {
     int Hq, Hk, D, splits, tiles, tile_rows, rows;
     const int* cu;              // starts of the sequences' queries; NULL: all have `queries`
     int queries;
+    float by;
     const float* parts;
     const float2* stats;
 };
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256) void k_join_few(JoinArgs a, unsigned all, Head
 #pragma unroll
     for (int i = 0; i < JOIN_FEW; ++i)
         if (i < a.splits) {
-            const float f = __builtin_amdgcn_exp2f(st[i].x - z);
+            const float f = __builtin_amdgcn_exp2f((st[i].x - z) * a.by);
             n += f * st[i].y;
             o.x += f * p[i].x;
             o.y += f * p[i].y;
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a, Heads<T> out)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (s0 + 4 * i >= a.splits) break;
-            const float f = __builtin_amdgcn_exp2f(st[i].x - z);
+            const float f = __builtin_amdgcn_exp2f((st[i].x - z) * a.by);
             n += f * st[i].y;
             o.x += f * p[i].x;
             o.y += f * p[i].y;

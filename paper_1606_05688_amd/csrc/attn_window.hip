@@ -22,6 +22,9 @@ namespace znni {
 
 constexpr int BM = 128, ATTN_THREADS = 256;
 
+// What a score is multiplied by to count powers of two (of a scale of 0: so little that what is masked stays so; queries have the sign).
+__host__ __device__ inline float powers_of(float scale) { return scale == 0.f ? 1e-37f : fabsf(scale) * 1.44269504088896340736f; }
+
 // The x lowest bits.
 __device__ inline unsigned lowest(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
 
@@ -148,8 +151,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         }
     }
 
-    const float by = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * 1.44269504088896340736f;       // of 0: what is masked stays so
-
+    const float by = powers_of(a.scale);
     const float ahead = 8.f / by;
     // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                    : ((key_part + 4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle_v(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
 
     f32x16 acc[NA];
-    float top, sum;
+    float top, sum, off;            // sums stand for weights of 2^(by (s - top) + off)
     // Values that are not finite leave their mark on rows that do not see them (their weight is zero, and zero times those is NaN).
     // So the walk over the keys takes place without a thought for them, and where a result is not finite once more, carefully: such values
     // are taken out of the tiles that only some rows see, and given to those at the end.
@@ -271,19 +273,23 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                 for (int i = 1; i < 4 * KT; ++i) mx[x] = __builtin_elementwise_maximum(mx[x], s[i / 4][4 * (i % 4) + x]);
             }
             float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx[0], mx[1]), __builtin_elementwise_maximum(mx[2], mx[3]));
-            // Weights are 2^(by (s - top)), as one multiply-add.  `top` follows the maximum when that is 2^8 ahead: weights stay in
-            // the range of every type, and most tiles have nothing to rescale.  by * top may be so large that its rounding would
-            // leave that range (it is the same for all keys of a row and cancels): then the difference comes first.
+            // Weights are 2^(by (s - top)), as one multiply-add of `shift` = -by top.  `top` follows the maximum when that is 2^8 ahead:
+            // weights stay in the range of every type, and most tiles have nothing to rescale.  What the rounding of by * top leaves, by * top +
+            // shift, is in all weights of a row until `top` moves, and is made good there and where sums are joined.  It may be so large that
+            // weights would leave the range of the type: then the difference comes first, which leaves nothing.
             float offset = shift;
             if (wild || __any(most > top + ahead)) {
                 most = fmaxf(fmaxf(most, __shfl_xor(most, 32)), top);
-                const float zero = most == -INFINITY ? 0.f : most, old = __builtin_amdgcn_exp2f((top - zero) * by);
+                const float zero = most == -INFINITY ? 0.f : most, now = -zero * by;
+                const bool far = __any(!(fabsf(now) < 0x1p26f));
+                const float was = wild ? 0.f : fmaf(top, by, shift), is = far ? 0.f : fmaf(zero, by, now);
+                const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - zero) * by + (is - was));
                 sum *= old;
 #pragma unroll
                 for (int x = 0; x < NA; ++x) acc[x] *= old;
                 top = most;
-                offset = shift = -zero * by;
-                wild = __any(!(fabsf(shift) < 0x1p26f));
+                wild = far;
+                offset = shift = now;
                 if (wild) {
 #pragma unroll
                     for (int n = 0; n < KT; ++n) s[n] -= zero;
@@ -327,6 +333,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             }
             sum += part[0] + part[1];
         }
+        off = wild || top == -INFINITY ? 0.f : fmaf(top, by, shift);
         if (odd)
             for (int it = begin; it < end; ++it) {
                 const int j0 = tiles.base(it);
@@ -356,10 +363,10 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     if constexpr (SHARE == 2) {
         // the second wave's sums by way of the tiles' memory
         float4* const sums = (float4*)&ks[0][0] + wrow / 32 * NC * 256;
-        float2* const stat = (float2*)&vs[0][0] + wrow / 32 * 64;
+        float3* const stat = (float3*)&vs[0][0] + wrow / 32 * 64;
         __syncthreads();
         if (part) {
-            stat[l] = make_float2(top, sum);
+            stat[l] = make_float3(top, sum, off);
 #pragma unroll
             for (int x = 0; x < NA; ++x)
 #pragma unroll
@@ -367,12 +374,13 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         }
         __syncthreads();
         if (part) return;
-        const float2 theirs = stat[l];
+        const float3 theirs = stat[l];
         const float most = fmaxf(top, theirs.x), zero = most == -INFINITY ? 0.f : most;
         // (not zero, which would make NaN of a sum that is infinite)
-        const float f0 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((top - zero) * by), 0x1p-126f);
-        const float f1 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((theirs.x - zero) * by), 0x1p-126f);
+        const float f0 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((top - zero) * by - off), 0x1p-126f);
+        const float f1 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((theirs.x - zero) * by - theirs.z), 0x1p-126f);
         top = most;
+        off = 0.f;
         sum = f0 * sum + f1 * theirs.y;
 #pragma unroll
         for (int x = 0; x < NA; ++x)
@@ -404,15 +412,15 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             }
     } else {
         const long long at = ((((long long)b * a.Hk + hk) * a.tiles + tile) * a.splits + split) * a.tile_rows + wrow + c32;
-        const float in_range = top == -INFINITY ? top : fminf(fmaxf(top * by, -3.402823466e38f), 3.402823466e38f);
-        if (h == 0 && d_part == 0) a.stats[at] = make_float2(in_range, sum);
+        const float even = __builtin_amdgcn_exp2f(-off);
+        if (h == 0 && d_part == 0) a.stats[at] = make_float2(top, even * sum);
         float* y = a.parts + at * a.D;
 #pragma unroll
         for (int x = 0; x < NA; ++x)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const int d = d_part + 32 * x + 2 * i + 4 * h;
-                if (d < a.D) *(float4*)(y + d) = make_float4(acc[x][i], acc[x][i + 1], acc[x][i + 2], acc[x][i + 3]);
+                if (d < a.D) *(float4*)(y + d) = make_float4(even * acc[x][i], even * acc[x][i + 1], even * acc[x][i + 2], even * acc[x][i + 3]);
             }
     }
 }
@@ -486,7 +494,7 @@ static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const AttnPl
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;
-    const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, a.parts, a.stats};
+    const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, powers_of(a.scale), a.parts, a.stats};
     return launch_join<T>(j, B, o, st);
 }
 

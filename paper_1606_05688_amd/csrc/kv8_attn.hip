@@ -390,7 +390,7 @@ static znni_status launch_kv8(const Kv8Args& a, int B, const znni_heads* q, cons
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (a.splits == 1) return ZNNI_OK;
-    const JoinArgs j = {a.Hq, a.Hk, a.D, a.splits, (int)tiles, KV8_ROWS, (int)rows, nullptr, a.Lq, a.parts, a.stats};
+    const JoinArgs j = {a.Hq, a.Hk, a.D, a.splits, (int)tiles, KV8_ROWS, (int)rows, nullptr, a.Lq, 1.f, a.parts, a.stats};
     return launch_join<T>(j, B, o, st);
 }
 
