@@ -22,8 +22,9 @@ namespace znni {
 
 constexpr int BM = 128, ATTN_THREADS = 256;
 
-// What a score is multiplied by to count powers of two (of a scale of 0: so little that what is masked stays so; queries have the sign).
-__host__ __device__ inline float powers_of(float scale) { return scale == 0.f ? 1e-37f : fabsf(scale) * 1.44269504088896340736f; }
+// What a score is multiplied by to count powers of two (queries have the sign).  Of a scale of 0: the least there is, with which scores of
+// 2^128 are 2^-21 and what is masked stays so.
+__host__ __device__ inline float powers_of(float scale) { return scale == 0.f ? 0x1p-149f : fabsf(scale) * 1.44269504088896340736f; }
 
 // The x lowest bits.
 __device__ inline unsigned lowest(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     }
 
     const float by = powers_of(a.scale);
-    const float ahead = 8.f / by;
+    const float ahead = fminf(8.f / by, 3.402823466e38f);          // (finite: minus infinity and this is minus infinity)
     // where this lane reads: keys row c32 (and 32 on), chunk h ^ ... of step 0, other steps by exclusive or; values likewise
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
     int k_at = (((key_part + c32) * RS + (h ^ G::swizzle_k(c32)) * EC) * (int)sizeof(T)) ^ q_part * 32;
