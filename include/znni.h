@@ -343,8 +343,9 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *   - Query head h reads key and value head h / (Hq / Hk); Hk divides Hq.  ZNNI_ERR_SHAPE.
  *   - A row at position p sees key j if j <= p + right and (j >= p - left or j < sinks): the window, and the first tokens,
  *     which stay visible to all rows that come after them.  ZNNI_ALL for left or right: no end.  What lies in keys and
- *     values that a row does not see, infinities and NaN included, has no influence on it.  A row that sees nothing, or whose
- *     weights are all zero, is zero.
+ *     values that a row does not see, infinities and NaN included, has no influence on it.  An infinite value that it sees makes
+ *     that element infinite, however small its weight (infinities of both signs: NaN).  A row that sees nothing, or whose weights are all
+ *     zero, is zero.
  *   - Lengths of zero are fine; a call without tokens launches nothing.
  *   - Results are deterministic; a row's depends on how many sequences, rows and keys its call says there may be (B, max_q,
  *     max_k, max_len), by rounding only.

@@ -31,6 +31,9 @@ struct JoinRow {
     }
 };
 
+// A part's sum times the part's factor.  An infinite one stays so: the row sees an infinity, and a factor that rounds to zero would make NaN of it.
+__device__ inline float share_of(float f, float sum) { return fabsf(sum) == INFINITY ? sum : f * sum; }
+
 constexpr int JOIN_FEW = 8;          // parts that a lane reads at once
 
 // Few parts: LANES lanes a row, four elements a lane, everything read at once (13720 rows of 4 parts of 40 elements, 9 MB: 4.4 us, a wave
@@ -62,10 +65,10 @@ __global__ __launch_bounds__(256) void k_join_few(JoinArgs a, unsigned all, Head
         if (i < a.splits) {
             const float f = __builtin_amdgcn_exp2f((st[i].x - z) * a.by);
             n += f * st[i].y;
-            o.x += f * p[i].x;
-            o.y += f * p[i].y;
-            o.z += f * p[i].z;
-            o.w += f * p[i].w;
+            o.x += share_of(f, p[i].x);
+            o.y += share_of(f, p[i].y);
+            o.z += share_of(f, p[i].z);
+            o.w += share_of(f, p[i].w);
         }
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 y = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
@@ -103,8 +106,8 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a, Heads<T> out)
             if (s0 + 4 * i >= a.splits) break;
             const float f = __builtin_amdgcn_exp2f((st[i].x - z) * a.by);
             n += f * st[i].y;
-            o.x += f * p[i].x;
-            o.y += f * p[i].y;
+            o.x += share_of(f, p[i].x);
+            o.y += share_of(f, p[i].y);
         }
     }
     acc_s[wave][l] = o;

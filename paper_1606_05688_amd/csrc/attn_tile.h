@@ -83,30 +83,24 @@ struct Mfma<bf16> {
     typedef bf16 V __attribute__((ext_vector_type(8)));
     typedef bf16 V4 __attribute__((ext_vector_type(4)));
     __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-    __device__ static unsigned cleared(unsigned x)
-    {
-        return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
-    }
 };
 template <>
 struct Mfma<f16> {
     typedef f16 V __attribute__((ext_vector_type(8)));
     typedef f16 V4 __attribute__((ext_vector_type(4)));
     __device__ static f32x16 mul(V a, V b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u; }
-    __device__ static unsigned cleared(unsigned x)
-    {
-        return ((x & 0x7c00u) == 0x7c00u ? 0u : x & 0xffffu) | ((x & 0x7c000000u) == 0x7c000000u ? 0u : x & 0xffff0000u);
-    }
 };
 template <>
 struct Mfma<float> {
     typedef float V __attribute__((ext_vector_type(4)));
     __device__ static f32x16 mul(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-    __device__ static bool odd(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u; }
-    __device__ static unsigned cleared(unsigned x) { return odd(x) ? 0u : x; }
 };
+
+// What kind of number x is, so that a sum of up to 64 says which kinds were there: 1 for infinity, 128 for minus infinity, both for NaN, 0 else.
+__device__ inline float kind_of(float x)
+{
+    return fabsf(x) <= 3.402823466e38f ? 0.f : x == INFINITY ? 1.f : x == -INFINITY ? 128.f : 129.f;
+}
 
 // What rows at positions p0 .. p1 (none if p1 < p0) see of nk keys: the first row's keys go from lo0 to hi0, the last one's from lo1
 // to hi1, besides sinks.

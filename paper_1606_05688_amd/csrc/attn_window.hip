@@ -162,12 +162,47 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 
     f32x16 acc[NA];
     float top, sum, off;            // sums stand for weights of 2^(by (s - top) + off)
-    // Values that are not finite leave their mark on rows that do not see them (their weight is zero, and zero times those is NaN).
-    // So the walk over the keys takes place without a thought for them, and where a result is not finite once more, carefully: such values
-    // are taken out of the tiles that only some rows see, and given to those at the end.
+    // one bit for each of 32 keys: whether the lane's row sees them
+    auto sight = [&](int j) { return lowest(hi + 1 - j) & (~lowest(lo - j) | lowest(a.w.sinks - j)); };
+    // adds 32 elements of the head (from 32 x on) of values of 32 keys (32 n on), times weights of this lane's row: 16 of those keys
+    auto add_values = [&](f32x16& to, const char* from, int x, int n, auto weight) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                to = M::mul(*(const T*)(from + (v_at ^ x * 128) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T)), weight(i), to);
+        } else {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                typename M::V w;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = (T)weight(8 * m + e);
+                const char* p = from + (v_at ^ x * 64) + 16 * (2 * n + m) * RS * (int)sizeof(T);
+                const typename M::V4 y0 = transposed<typename M::V4>(p), y1 = transposed<typename M::V4>(p + 8 * RS * (int)sizeof(T));
+                to = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, to);
+            }
+        }
+    };
+
+    // values of a tile, each thread its own chunks
+    auto change = [&](T* tile, auto to) {
+        typedef T Chunk __attribute__((ext_vector_type(EC)));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            Chunk* const at = (Chunk*)(tile + (i * ATTN_THREADS + t) * EC);
+            Chunk y = *at;
+#pragma unroll
+            for (int e = 0; e < EC; ++e) y[e] = to(y[e]);
+            *at = y;
+        }
+    };
+
+    // Values that are not finite leave their mark on rows that do not see them (their weight is zero, and zero times those is NaN), and
+    // infinities under weights that round to zero become NaN.  So the walk over the keys takes place without a thought for them, and where a result
+    // is not finite twice more: products of the values' kinds with zeros and ones say which kinds a row sees; then such values are taken out of
+    // the tiles, and the row gets what it sees at the end, whatever the weight.  The maximum is followed at once there, so that sums of values next
+    // to the largest do not pass it before they are rescaled.
     auto walk = [&](auto carefully) {
         constexpr bool careful = decltype(carefully)::value;
-        bool odd = false;                        // (in here: known outside, it costs the loop 5 % of its time)
 #pragma unroll
         for (int x = 0; x < NA; ++x)
 #pragma unroll
@@ -184,22 +219,9 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             else if (STAGES > 2 && it + 1 < end) wait_but_and_meet<ONE>();
             else wait_but_and_meet<0>();
             if (it + STAGES - 1 < end) bring(it + STAGES - 1);
-            if constexpr (careful) if (!all_rows.all(j0, BN)) {
-                bool x = false;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const uint4 y = *(const uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
-                    x = x || M::odd(y.x) || M::odd(y.y) || M::odd(y.z) || M::odd(y.w);
-                }
-                if (any_of_all(x)) {
-                    odd = true;
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) {
-                        uint4* y = (uint4*)&vs[buf][(i * ATTN_THREADS + t) * EC];
-                        *y = make_uint4(M::cleared(y->x), M::cleared(y->y), M::cleared(y->z), M::cleared(y->w));
-                    }
-                    __syncthreads();
-                }
+            if constexpr (careful) {
+                change(vs[buf], [](T y) { return kind_of((float)y) == 0.f ? y : (T)0.f; });
+                __syncthreads();
             }
             const int wj0 = j0 + key_part;                   // of the wave
             if (!wave_rows.any(wj0, 32 * KT)) continue;
@@ -256,9 +278,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             if (!wave_rows.all(wj0, 32 * KT)) {
 #pragma unroll
                 for (int n = 0; n < KT; ++n) {
-                    // one bit for each of 32 keys: two instructions a score
-                    const int j = wj0 + n * 32;
-                    const unsigned see = lowest(hi + 1 - j) & (~lowest(lo - j) | lowest(a.w.sinks - j)), mine = see >> 4 * h;
+                    const unsigned mine = sight(wj0 + n * 32) >> 4 * h;       // two instructions a score
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int m = (int)(mine << (31 - 8 * (i / 4) - i % 4)) >> 31;
@@ -279,7 +299,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             // shift, is in all weights of a row until `top` moves, and is made good there and where sums are joined.  It may be so large that
             // weights would leave the range of the type: then the difference comes first, which leaves nothing.
             float offset = shift;
-            if (wild || __any(most > top + ahead)) {
+            if (wild || __any(most > top + (careful ? 0.f : ahead))) {
                 most = fmaxf(fmaxf(most, __shfl_xor(most, 32)), top);
                 const float zero = most == -INFINITY ? 0.f : most, now = -zero * by;
                 const bool far = __any(!(fabsf(now) < 0x1p26f));
@@ -335,23 +355,6 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             sum += part[0] + part[1];
         }
         off = wild || top == -INFINITY ? 0.f : fmaf(top, by, shift);
-        if (odd)
-            for (int it = begin; it < end; ++it) {
-                const int j0 = tiles.base(it);
-                if (all_rows.all(j0, BN)) continue;
-                for (int j = j0 + key_part; j < min(j0 + key_part + 32 * KT, nk); ++j) {
-                    const bool see = j <= hi && (j >= lo || j < a.w.sinks);
-                    const T* vr = vp + (long long)j * v.token;
-#pragma unroll
-                    for (int x = 0; x < NA; ++x)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int d = d_part + 32 * x + 8 * (i / 4) + 4 * h + i % 4;
-                            const float y = d < a.D ? (float)vr[d] : 0.f;
-                            if (see && !(fabsf(y) <= 3.402823466e38f)) acc[x][i] += y;
-                        }
-                }
-            }
     };
     walk(std::false_type());
     bool fine = true;
@@ -359,7 +362,38 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     for (int x = 0; x < NA; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[x][i]) <= 3.402823466e38f;
-    if (__builtin_expect(any_of_all(!fine && d_part < a.D), 0)) walk(std::true_type());
+    const int odd_sums = any_of_all(!fine && d_part < a.D);
+    if (__builtin_expect(odd_sums, 0)) {
+        unsigned met[NA] = {};                   // for each element of a result whether infinity (16 bits), minus infinity (16 more) are seen
+        bring_first();
+        for (int it = begin; it < end; ++it) {
+            const int buf = (it - begin) % STAGES, j0 = tiles.base(it) + key_part;
+            wait_but_and_meet<0>();
+            if (it + STAGES - 1 < end) bring(it + STAGES - 1);
+            change(vs[buf], [](T y) { return (T)kind_of((float)y); });
+            wait_and_meet();
+            if (!wave_rows.any(j0, 32 * KT) || d_part >= a.D) continue;
+#pragma unroll
+            for (int x = 0; x < NA; ++x) {
+                f32x16 seen;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) seen[i] = 0.f;
+#pragma unroll
+                for (int n = 0; n < KT; ++n) {
+                    const unsigned mine = sight(j0 + n * 32) >> 4 * h;
+                    add_values(seen, (const char*)vs[buf], x, n, [&](int i) { return (float)(mine >> (8 * (i / 4) + i % 4) & 1); });
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) met[x] |= ((int)seen[i] & 127 ? 1u << i : 0u) | ((int)seen[i] >= 128 ? 0x10000u << i : 0u);
+            }
+        }
+        __syncthreads();
+        walk(std::true_type());
+#pragma unroll
+        for (int x = 0; x < NA; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[x][i] += (met[x] >> i & 1 ? INFINITY : 0.f) - (met[x] >> (16 + i) & 1 ? INFINITY : 0.f);
+    }
     sum += __shfl_xor(sum, 32);
     if constexpr (SHARE == 2) {
         // the second wave's sums by way of the tiles' memory
@@ -377,22 +411,24 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
         if (part) return;
         const float3 theirs = stat[l];
         const float most = fmaxf(top, theirs.x), zero = most == -INFINITY ? 0.f : most;
-        // (not zero, which would make NaN of a sum that is infinite)
-        const float f0 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((top - zero) * by - off), 0x1p-126f);
-        const float f1 = __builtin_elementwise_maximum(__builtin_amdgcn_exp2f((theirs.x - zero) * by - theirs.z), 0x1p-126f);
+        const float f0 = __builtin_amdgcn_exp2f((top - zero) * by - off), f1 = __builtin_amdgcn_exp2f((theirs.x - zero) * by - theirs.z);
         top = most;
         off = 0.f;
         sum = f0 * sum + f1 * theirs.y;
+        auto join = [&](auto share) {
 #pragma unroll
-        for (int x = 0; x < NA; ++x)
+            for (int x = 0; x < NA; ++x)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 y = sums[(x * 4 + i / 4) * 64 + l];
-                acc[x][i] = f0 * acc[x][i] + f1 * y.x;
-                acc[x][i + 1] = f0 * acc[x][i + 1] + f1 * y.y;
-                acc[x][i + 2] = f0 * acc[x][i + 2] + f1 * y.z;
-                acc[x][i + 3] = f0 * acc[x][i + 3] + f1 * y.w;
-            }
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 y = sums[(x * 4 + i / 4) * 64 + l];
+                    acc[x][i] = share(f0, acc[x][i]) + share(f1, y.x);
+                    acc[x][i + 1] = share(f0, acc[x][i + 1]) + share(f1, y.y);
+                    acc[x][i + 2] = share(f0, acc[x][i + 2]) + share(f1, y.z);
+                    acc[x][i + 3] = share(f0, acc[x][i + 3]) + share(f1, y.w);
+                }
+        };
+        if (__builtin_expect(odd_sums, 0)) join(share_of);
+        else join([](float f, float x) { return f * x; });
     }
     if (wrow0 + c32 >= rows) return;
     if (a.splits == 1) {
