@@ -73,7 +73,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     const int part = wave % SHARE, wrow = wave / SHARE * 32, key_part = BY_D ? 0 : part * KT * 32;
     const long long wrow0 = row0 + wrow;
     const Sight all_rows(base + row0 / shared, base + last / shared, nk, a.w);
-    const Sight wave_rows(base + wrow0 / shared, wrow0 < rows ? base + min(wrow0 + 31, last) / shared : LLONG_MIN, nk, a.w);
+    const Sight wave_rows(base + wrow0 / shared, base + (wrow0 < rows ? min(wrow0 + 31, last) / shared : wrow0 / shared - 1), nk, a.w);
     const long long row = min(wrow0 + c32, rows - 1);
     const long long pos = base + row / shared;                                         // of the lane
     int lo, hi;
