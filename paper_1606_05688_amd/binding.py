@@ -385,8 +385,9 @@ def _result(like, given, shape, kind):
     return out, _descriptor(out.data_ptr(), shape[1] * shape[2], shape[2])
 
 
-def _ints(x, *shape):
-    assert x.is_cuda and x.dtype == torch.int32 and x.shape == shape and x.is_contiguous(), f"need contiguous int32 {shape}"
+def _ints(x, kind, *shape):
+    assert x.is_cuda and x.get_device() == kind[2] and x.dtype == torch.int32 and x.shape == shape and x.is_contiguous(), \
+        f"need contiguous int32 {shape} on GPU {kind[2]}"
     return x.data_ptr()
 
 
@@ -419,7 +420,7 @@ def _scratch(need, workspace, x):
             return None, 0, None
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
         return workspace.data_ptr(), need, workspace
-    assert workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    assert workspace.is_cuda and workspace.get_device() == x.get_device() and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
@@ -440,8 +441,8 @@ def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_
         assert kshape == (T, Hk, D)
         dk = _heads(k, kshape, kind)
         out_k, do_k = _result(k, out_k, kshape, kind)
-    assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
-    _check(lib().znni_rope_axes(kind[0], T, Hq, Hk, D, _heads(q, shape, kind), dk, _ints(pos, T, axes), freq.data_ptr(), axes,
+    assert freq.is_cuda and freq.get_device() == kind[2] and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
+    _check(lib().znni_rope_axes(kind[0], T, Hq, Hk, D, _heads(q, shape, kind), dk, _ints(pos, kind, T, axes), freq.data_ptr(), axes,
                                 struct.pack("%di" % axes, *sections), do_q, do_k, _PAIRINGS[pairing], _current(q)))
     return out_q, out_k
 
@@ -473,7 +474,7 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     out, do = _result(q, out, q.shape, kind)
     w, n, held = _scratch(_attn_window_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
     _check(lib().znni_attn_window(kind[0], B, Hq, Hk, D, _heads(q, q.shape, kind), _heads(k, k.shape, kind), _heads(v, k.shape, kind),
-                                  _ints(cu_q, B + 1), _ints(cu_k, B + 1), max_q, max_k, left, right, sinks,
+                                  _ints(cu_q, kind, B + 1), _ints(cu_k, kind, B + 1), max_q, max_k, left, right, sinks,
                                   D ** -0.5 if scale is None else scale, do, w, n, _current(q)))
     return out
 
@@ -486,11 +487,12 @@ def kv8_alloc(pages, Hk, D, device="cuda"):
             torch.empty((pages, Hk, 2), dtype=torch.float32, device=device))
 
 
-def _cache(kcodes, vcodes, scales, Hk, D):
+def _cache(kcodes, vcodes, scales, Hk, D, kind):
     """Addresses of a cache's three tensors, and its pages."""
     pages = kcodes.shape[0]
     assert kcodes.dtype == vcodes.dtype == torch.uint8 and scales.dtype == torch.float32
     assert kcodes.is_cuda and kcodes.is_contiguous() and vcodes.is_cuda and vcodes.is_contiguous() and scales.is_cuda and scales.is_contiguous()
+    assert kcodes.get_device() == vcodes.get_device() == scales.get_device() == kind[2], f"need a cache on GPU {kind[2]}"
     assert kcodes.shape == (pages, Hk, KV8_PAGE, D) and vcodes.shape == (pages, Hk, D, KV8_PAGE) and scales.shape == (pages, Hk, 2)
     return kcodes.data_ptr(), vcodes.data_ptr(), scales.data_ptr(), pages
 
@@ -503,9 +505,9 @@ def znni_kv8_append(kcodes, vcodes, scales, k, v, table, cu, start, max_new, str
     T, Hk, D = k.shape
     B, width = table.shape
     kind = _kind(k)
-    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
-    _check(lib().znni_kv8_append(kind[0], B, Hk, D, _heads(k, k.shape, kind), _heads(v, k.shape, kind), _ints(cu, B + 1), _ints(start, B),
-                                 int(max_new) if T else 0, kc, vc, sc, pages, _ints(table, B, width), width, _current(k)))
+    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D, kind)
+    _check(lib().znni_kv8_append(kind[0], B, Hk, D, _heads(k, k.shape, kind), _heads(v, k.shape, kind), _ints(cu, kind, B + 1), _ints(start, kind, B),
+                                 int(max_new) if T else 0, kc, vc, sc, pages, _ints(table, kind, B, width), width, _current(k)))
 
 
 def _kv8_attn_need(type, B, Lq, Hq, Hk, D, max_len, left, sinks):
@@ -526,9 +528,9 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
         return _on(stream, q, znni_kv8_attn, q, kcodes, vcodes, scales, table, lens, max_len, left, sinks, scale, out, workspace)
     B, Lq, Hq, D = q.shape
     Hk, width = kcodes.shape[1], table.shape[1]
-    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D)
-    left, sinks, max_len = _window(left), int(sinks), int(max_len)
     kind = _kind(q)
+    kc, vc, sc, pages = _cache(kcodes, vcodes, scales, Hk, D, kind)
+    left, sinks, max_len = _window(left), int(sinks), int(max_len)
     shape, rows = (B * Lq, Hq, D), q
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -541,7 +543,7 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
         token = q.stride(0)
     dq = _descriptor(rows.data_ptr(), token if shape[0] > 1 else 0, head if Hq > 1 else 0)
     w, n, held = _scratch(_kv8_attn_need(kind[0], B, Lq, Hq, Hk, D, max_len, left, sinks), workspace, q)
-    _check(lib().znni_kv8_attn(kind[0], B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, B, width), width, _ints(lens, B), max_len, left,
+    _check(lib().znni_kv8_attn(kind[0], B, Lq, Hq, Hk, D, dq, kc, vc, sc, pages, _ints(table, kind, B, width), width, _ints(lens, kind, B), max_len, left,
                                sinks, D ** -0.5 if scale is None else scale, _descriptor(out.data_ptr(), Hq * D, D), w, n,
                                _current(q)))
     return out
