@@ -336,7 +336,8 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *
  * Conventions, besides those at the top of this file:
  *   - `type` is a znni_type, the type of all tensors of heads of a call; scores, softmax statistics and sums are fp32.
- *     znni_attn_window rounds weights to a 16-bit type before they meet the values; znni_kv8_attn keeps 16 bits of them and more.
+ *     znni_attn_window rounds weights to a 16-bit type before they meet the values, or, where max_q * Hq / Hk is at most 64, to two
+ *     values of it, which keep 16 bits and more; znni_kv8_attn always keeps 16 bits and more.
  *   - A tensor of heads is a znni_heads: element (token t, head h, d) lies at data[t * token + h * head + d], strides in
  *     elements.  Data 16-byte aligned, strides multiples of 16 bytes (zero and negative ones included for what is read),
  *     D a multiple of 8.  ZNNI_ERR_ALIGN, ZNNI_ERR_UNSUPPORTED_SIZE.

@@ -7,7 +7,8 @@
 //   exchange; the weights as they stand are the right operand of  out^T [D][32 rows] += V^T W^T.
 // V^T's operand: 16-bit types by transposing LDS reads, fp32 (products of fp32) by plain ones, keys permuted to match.
 // Rows in LDS are permuted by 16-byte chunks so that neither kind of read meets a bank twice.
-// Rounded: 16-bit weights to their type before the second product (at most 2^8 times a row's largest then), sums stay fp32.
+// Rounded: 16-bit weights to their type before the second product (at most 2^8 times a row's largest then; two values of the type where a
+// sequence has few rows), sums stay fp32.
 //
 // bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 520 to 600 us, 800 to 926 TFLOP/s, against 1090 of a large bf16 product.  Bound by
 // the LDS reads of a wave (32 KB a tile, each used for 32 rows), the weights' instructions between the products, and the clock, which falls to
@@ -32,7 +33,8 @@ __device__ inline unsigned lowest(int x) { return x <= 0 ? 0u : ~0u >> (32 - min
 // SHARE waves share 32 rows, 128 / SHARE rows a workgroup.  Two: each has half of a tile's keys, their sums are joined at the end.  Four (fp32, whose
 // tile has no more keys than a product): each has a quarter of the head's elements, in the scores, whose parts are added through LDS, and
 // in the results; softmax statistics are the same in all four.
-template <typename T, int NC, int SHARE>
+// TWICE (16-bit types): weights as two values of the type, for few rows.
+template <typename T, int NC, int SHARE, bool TWICE>
 __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> out)
 {
     using G = AttnTile<T, NC, ATTN_THREADS>;
@@ -337,18 +339,21 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
             } else {
 #pragma unroll
                 for (int n = 0; n < 2 * KT; ++n) {
-                    typename M::V w;
+                    typename M::V w, rest;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[n / 2][8 * (n & 1) + e], by, offset));
                         part[e & 1] += p;
                         w[e] = (T)p;
+                        if constexpr (TWICE) rest[e] = (T)(p - (float)w[e]);
                     }
 #pragma unroll
                     for (int x = 0; x < NA; ++x) {
                         const char* from = vb + (v_at ^ x * 64) + 16 * n * RS * (int)sizeof(T);
                         const typename M::V4 y0 = transposed<typename M::V4>(from), y1 = transposed<typename M::V4>(from + 8 * RS * (int)sizeof(T));
-                        acc[x] = M::mul(__builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[x]);
+                        const typename M::V y = __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
+                        acc[x] = M::mul(y, w, acc[x]);
+                        if constexpr (TWICE) acc[x] = M::mul(y, rest, acc[x]);
                     }
                 }
             }
@@ -464,6 +469,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
 
 struct AttnPlan {
     int share, tiles, splits, tile_rows;
+    bool twice;                        // weights as two values of a 16-bit type
     long long groups;                  // workgroups without splitting
     size_t rows;                       // rows of parts
 };
@@ -475,6 +481,7 @@ static AttnPlan attn_plan(int share, int type, int B, int Hq, int Hk, int max_q,
     AttnPlan p;
     const int bm = BM / share;
     p.share = share;
+    p.twice = false;
     const long long rows = (long long)max_q * (Hq / Hk);
     const long long tiles = (rows + bm - 1) / bm;
     p.tiles = (int)(tiles < INT_MAX ? tiles : INT_MAX);
@@ -496,14 +503,22 @@ static AttnPlan attn_plan(int share, int type, int B, int Hq, int Hk, int max_q,
 // instructions: two share the rows.  fp16, heads 8 x 64, 300 queries, window of 100, with 128 and with 64 rows a workgroup: 24 workgroups
 // 10.8 and 9.4 us, 288: 13.8 and 11.9, 384: 14.1 and 13.3, 480: 14.6 and 17.7, 768: 18.2 and 23.0; bf16, heads 16 of 4 x 128, 2048
 // queries, 256 workgroups: 61.6 and 54.7 us.
+// A sequence whose rows fit one such tile (single tokens) is bound by its keys and values, so weights keep the bits that a second value of
+// the type holds: error 0.0017 of the result in bf16 as with an fp32 softmax rounded once, 0.0023 with one value.  bf16, heads 16 of 4 x 128, one
+// query: 8 sequences of 8192 keys 29.0 us with one value, 29.7 with two, 32 of 500 13.3 and 13.9, one of 16384 18.6 and 19.3.  More rows are bound by
+// products: 2048 queries 45.5 and 55.2, 16384 with a window of 4096 495 and 681, fp16, heads 8 x 64, 300 ragged queries 10.7 and 11.6.
 // fp32: where one wave's rows are all, the other three would wait for its products (heads 16 of 4 x 128, one query, 8 sequences of 8192
 // keys: 89 us with one wave at work, 60 with four; of 500: 27 and 16); and where workgroups are very few (heads 5 x 40, 200 queries: 20.9
 // and 16.8, 400: 19.5 and 16.2, 700, 30 workgroups: 21.1 and 24.0; 16 of 4 x 128, 100 queries: 24.6 and 13.0, 256 of 4000 keys: 89 and 105).
 static AttnPlan attn_plan(int type, int B, int Hq, int Hk, int max_q, int max_k, int left, int right, int sinks)
 {
-    const AttnPlan p = attn_plan(1, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
-    const int share = type != ZNNI_F32 ? (p.groups <= 384 ? 2 : 1) : p.groups <= 20 || (long long)max_q * (Hq / Hk) <= 32 ? 4 : 1;
-    return share == 1 ? p : attn_plan(share, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    AttnPlan p = attn_plan(1, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    const long long rows = (long long)max_q * (Hq / Hk);
+    const bool twice = type != ZNNI_F32 && rows <= BM / 2;
+    const int share = type != ZNNI_F32 ? (twice || p.groups <= 384 ? 2 : 1) : p.groups <= 20 || rows <= 32 ? 4 : 1;
+    if (share != 1) p = attn_plan(share, type, B, Hq, Hk, max_q, max_k, left, right, sinks);
+    p.twice = twice;
+    return p;
 }
 
 template <typename T>
@@ -513,21 +528,23 @@ static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const AttnPl
     const dim3 grid = launch_of(a.groups), block(ATTN_THREADS);
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v);
     const Heads<T> o = heads_of<T>(out);
-    auto launch = [&](auto share) {
+    auto launch = [&](auto share, auto twice) {
         constexpr int SHARE = decltype(share)::value;
+        constexpr bool TWICE = decltype(twice)::value;
         switch ((a.D + 31) / 32) {
-            case 1: k_attn<T, 1, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-            case 2: k_attn<T, 2, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-            case 3: k_attn<T, 3, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
-            default: k_attn<T, 4, SHARE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            case 1: k_attn<T, 1, SHARE, TWICE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            case 2: k_attn<T, 2, SHARE, TWICE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            case 3: k_attn<T, 3, SHARE, TWICE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
+            default: k_attn<T, 4, SHARE, TWICE><<<grid, block, 0, st>>>(a, qi, ki, vi, o); break;
         }
     };
     if constexpr (sizeof(T) == 2) {
-        if (p.share == 2) launch(std::integral_constant<int, 2>());
-        else launch(std::integral_constant<int, 1>());
+        if (p.twice) launch(std::integral_constant<int, 2>(), std::true_type());
+        else if (p.share == 2) launch(std::integral_constant<int, 2>(), std::false_type());
+        else launch(std::integral_constant<int, 1>(), std::false_type());
     } else {
-        if (p.share == 4) launch(std::integral_constant<int, 4>());
-        else launch(std::integral_constant<int, 1>());
+        if (p.share == 4) launch(std::integral_constant<int, 4>(), std::false_type());
+        else launch(std::integral_constant<int, 1>(), std::false_type());
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;
