@@ -386,7 +386,7 @@ def _result(like, given, shape, kind):
 
 
 def _ints(x, kind, *shape):
-    assert x.is_cuda and x.get_device() == kind[2] and x.dtype == torch.int32 and x.shape == shape and x.is_contiguous(), \
+    assert x.get_device() == kind[2] and x.dtype == torch.int32 and x.shape == shape and x.is_contiguous(), \
         f"need contiguous int32 {shape} on GPU {kind[2]}"
     return x.data_ptr()
 
@@ -420,7 +420,7 @@ def _scratch(need, workspace, x):
             return None, 0, None
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
         return workspace.data_ptr(), need, workspace
-    assert workspace.is_cuda and workspace.get_device() == x.get_device() and workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    assert workspace.get_device() == x.get_device() and workspace.dtype == torch.uint8 and workspace.is_contiguous()
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
@@ -441,7 +441,7 @@ def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_
         assert kshape == (T, Hk, D)
         dk = _heads(k, kshape, kind)
         out_k, do_k = _result(k, out_k, kshape, kind)
-    assert freq.is_cuda and freq.get_device() == kind[2] and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
+    assert freq.get_device() == kind[2] and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),)
     _check(lib().znni_rope_axes(kind[0], T, Hq, Hk, D, _heads(q, shape, kind), dk, _ints(pos, kind, T, axes), freq.data_ptr(), axes,
                                 struct.pack("%di" % axes, *sections), do_q, do_k, _PAIRINGS[pairing], _current(q)))
     return out_q, out_k
@@ -491,7 +491,7 @@ def _cache(kcodes, vcodes, scales, Hk, D, kind):
     """Addresses of a cache's three tensors, and its pages."""
     pages = kcodes.shape[0]
     assert kcodes.dtype == vcodes.dtype == torch.uint8 and scales.dtype == torch.float32
-    assert kcodes.is_cuda and kcodes.is_contiguous() and vcodes.is_cuda and vcodes.is_contiguous() and scales.is_cuda and scales.is_contiguous()
+    assert kcodes.is_contiguous() and vcodes.is_contiguous() and scales.is_contiguous()
     assert kcodes.get_device() == vcodes.get_device() == scales.get_device() == kind[2], f"need a cache on GPU {kind[2]}"
     assert kcodes.shape == (pages, Hk, KV8_PAGE, D) and vcodes.shape == (pages, Hk, D, KV8_PAGE) and scales.shape == (pages, Hk, 2)
     return kcodes.data_ptr(), vcodes.data_ptr(), scales.data_ptr(), pages
