@@ -46,6 +46,9 @@ __device__ inline const void* uniform(const void* p)
     return (const void*)((unsigned long long)hi << 32 | lo);
 }
 
+// (The compiler keeps m0 for itself and warns of its name in the lists below, which is what tells it not to count on m0 across them.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 // 16 bytes a lane from memory to LDS, 1024 bytes of a wave from `lds` on.  As assembly, since the compiler, which sees one
 // array in LDS, waits for such a load before any read of it: wait_but_and_meet() is what waits for these.
 __device__ inline void to_lds(const void* base, unsigned offset, unsigned lds)
@@ -57,6 +60,8 @@ __device__ inline void to_lds(const void* from, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(from) : "m0", "memory");
 }
+#pragma clang diagnostic pop
+
 __device__ inline unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
 // Four elements of one column of four rows: lanes 4r .. 4r + 3 of sixteen bring row r, lane c of them gets column c.
