@@ -33,7 +33,7 @@ def _check(dtype, q, k, v, copies, left, sinks):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("D", [64, 40, 128])
+@pytest.mark.parametrize("D", [64, 40, 128, 96, 24])
 @pytest.mark.parametrize("copies,nq,nk", CALLS)
 def test_infinities_under_weights_that_vanish(dtype, D, copies, nq, nk):
     """A row that sees an infinity has it, however small its weight (e^-190 and less here) and however the keys are shared out."""
