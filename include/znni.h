@@ -348,6 +348,8 @@ znni_status znni_maxpool(int S, int f, const int n[3], const int p[3], const flo
  *     that element infinite, however small its weight (infinities of both signs: NaN).  A row that sees nothing, or whose weights are all
  *     zero, is zero.
  *   - Lengths of zero are fine; a call without tokens launches nothing.
+ *   - Hq, Hk and B up to 65535; row tiles times key heads (times sequences) fit a launch: for znni_kv8_attn
+ *     ceil(Lq * Hq / Hk / 16) * Hk up to 65535.  ZNNI_ERR_SHAPE.
  *   - Results are deterministic; a row's depends on how many sequences, rows and keys its call says there may be (B, max_q,
  *     max_k, max_len), by rounding only.
  */
@@ -421,7 +423,7 @@ znni_status znni_kv8_append(int type, int B, int Hk, int D, const znni_heads* k,
  * position p = lens[b] - Lq + i (rows before the first token are zero), visibility with right = 0.  lens [B] device, counted
  * as at most width * ZNNI_KV8_PAGE; max_len: no sequence is longer (host; the launch is made for it).  Keys and
  * values are taken as they stand in the cache.
- * Other arguments as for znni_attn_window and znni_kv8_append.
+ * Other arguments as for znni_attn_window and znni_kv8_append; without pages every row is zero, and table may be NULL.
  */
 znni_status znni_kv8_attn_workspace(int type, int B, int Lq, int Hq, int Hk, int D, int max_len, int left, int sinks, size_t* bytes);
 

@@ -357,6 +357,8 @@ def znni_copy_probe(dst, src, stream=None):
     return dst
 
 
+# The attention operators.  Each call is asynchronous on `stream` (a torch.cuda.Stream of the tensors' GPU; default: torch's current
+# stream).  Inputs have to be there in that stream's order; results made by the call belong to it.
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _byref = ctypes.byref
 _descriptor = struct.Struct("Pqq").pack          # a znni_heads (data, token stride, head stride) as bytes

@@ -10,10 +10,10 @@
 // Rounded: 16-bit weights to their type before the second product (at most 2^8 times a row's largest then; two values of the type where a
 // sequence has few rows), sums stay fp32.
 //
-// bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 520 to 600 us, 800 to 926 TFLOP/s, against 1090 of a large bf16 product.  Bound by
-// the LDS reads of a wave (32 KB a tile, each used for 32 rows), the weights' instructions between the products, and the clock, which falls to
+// bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 484 to 503 us by card, 960 to 997 TFLOP/s, against 1090 of a large bf16 product.  Bound
+// by the LDS reads of a wave (32 KB a tile, each used for 32 rows), the weights' instructions between the products, and the clock, which falls to
 // 2.2 GHz.  fp32, 2744 tokens, heads 5 x 40: 40 us and 4 for the join, matrix units busy for a third.  16-bit calls of few rows: one
-// wave's chain of a tile, 1.1 us.
+// wave's chain of a tile, 1.1 us.  Values that are not finite cost two more walks: that volume with one infinity 636 us, all NaN 2030.
 #include <type_traits>
 
 #include "attn_join.h"
