@@ -26,13 +26,17 @@ EXPORTS = ("znni_version", "znni_status_string", "znni_fft_size", "znni_conv3d_f
            "znni_conv3d_fft", "znni_conv3d_fft_profile", "znni_conv3d_fft_workspace_v", "znni_conv3d_fft_v",
            "znni_conv3d_fft_profile_v", "znni_conv3d_fft_static_v", "znni_conv3d_fft_stage_work_v", "znni_conv3d_fft_call_work_v", "znni_conv3d_fft_sublayers_v", "znni_conv3d_fft_budget_v", "znni_conv3d_direct_workspace_v", "znni_conv3d_direct_v", "znni_conv3d_choose_v", "znni_conv3d_workspace_v", "znni_conv3d_v", "znni_mpf", "znni_maxpool",
            "znni_copy_probe", "znni_rope_axes", "znni_attn_window_workspace", "znni_attn_window", "znni_kv8_append",
-           "znni_kv8_attn_workspace", "znni_kv8_attn")
+           "znni_kv8_attn_workspace", "znni_kv8_attn", "znni_linear_workspace", "znni_linear", "znni_linear_backward_workspace",
+           "znni_linear_backward", "znni_block_norm", "znni_block_norm_backward_workspace", "znni_block_norm_backward")
 
 F32, BF16, F16 = 0, 1, 2
 ALL = 2147483647
 KV8_PAGE = 64
 ROPE_NEIGHBOURS = 1
 _PAIRINGS = {"halves": 0, "neighbours": ROPE_NEIGHBOURS}
+_ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}
+LINEAR_DX, LINEAR_DW, LINEAR_DBIAS = 1, 2, 4
+NORM_POST, NORM_PRE, NORM_CENTRED, NORM_GATE_SHARED = 1, 2, 4, 8
 
 _lib = None
 
@@ -106,6 +110,21 @@ def lib():
         L.znni_kv8_attn_workspace.argtypes = [i] * 9 + [ctypes.POINTER(sz)]
         L.znni_kv8_attn.restype = i
         L.znni_kv8_attn.argtypes = [i, i, i, i, i, i, hp, vp, vp, vp, i, vp, i, vp, i, i, i, ctypes.c_float, hp, vp, sz, vp]
+        rp, szp, fl = vp, ctypes.POINTER(sz), ctypes.c_float               # znni_rows *: bytes that hold one
+        L.znni_linear_workspace.restype = i
+        L.znni_linear_workspace.argtypes = [i, i, i, i, szp]
+        L.znni_linear.restype = i
+        L.znni_linear.argtypes = [i, i, i, i, rp, rp, vp, i, rp, rp, rp, vp, sz, vp]
+        L.znni_linear_backward_workspace.restype = i
+        L.znni_linear_backward_workspace.argtypes = [i, i, i, i, i, u, szp]
+        L.znni_linear_backward.restype = i
+        L.znni_linear_backward.argtypes = [i, i, i, i, rp, rp, rp, rp, i, rp, rp, vp, vp, sz, vp]
+        L.znni_block_norm.restype = i
+        L.znni_block_norm.argtypes = [i, i, i, rp, rp, rp, vp, vp, fl, fl, u, rp, rp, vp]
+        L.znni_block_norm_backward_workspace.restype = i
+        L.znni_block_norm_backward_workspace.argtypes = [i, i, i, u, szp]
+        L.znni_block_norm_backward.restype = i
+        L.znni_block_norm_backward.argtypes = [i, i, i, rp, rp, rp, rp, rp, vp, vp, fl, fl, u, rp, rp, rp, vp, vp, vp, sz, vp]
         L.znni_copy_probe.restype = i
         L.znni_copy_probe.argtypes = [vp, vp, sz, vp]
         _lib = L
@@ -549,3 +568,137 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
                                sinks, D ** -0.5 if scale is None else scale, _descriptor(out.data_ptr(), Hq * D, D), w, n,
                                _current(q)))
     return out
+
+
+# Products with weights and norms between blocks: what is said of streams at the attention operators holds.
+_rows_descriptor = struct.Struct("Pq").pack      # a znni_rows (data, row stride) as bytes
+
+
+def _rows(x, rows, cols, kind):
+    """The znni_rows of a [rows, cols] tensor of this kind whose last index is contiguous; None for None."""
+    if x is None:
+        return None
+    assert x.shape == (rows, cols) and x.dtype == kind[1] and x.get_device() == kind[2], f"need {kind[1]} rows ({rows}, {cols}) on GPU {kind[2]}"
+    row, unit = x.stride()
+    assert unit == 1 or cols < 2, "matrices are [rows, columns], columns contiguous"
+    return _rows_descriptor(x.data_ptr(), row if rows > 1 else cols)
+
+
+def _vector(x, n, kind):
+    """The address of a contiguous vector; None for None."""
+    if x is None:
+        return None
+    assert x.shape == (n,) and x.dtype == kind[1] and x.get_device() == kind[2] and x.is_contiguous(), f"need a contiguous {kind[1]} vector of {n} on GPU {kind[2]}"
+    return x.data_ptr()
+
+
+def _new(x, *shape):
+    return torch.empty(shape, dtype=x.dtype, device=x.device)
+
+
+def _need(call, *args):
+    b = ctypes.c_size_t(0)
+    _check(call(*args, _byref(b)))
+    return b.value
+
+
+def znni_linear_workspace(dtype, M, N, K):
+    return _need(lib().znni_linear_workspace, _TYPES[dtype], int(M), int(N), int(K))
+
+
+def znni_linear(x, w, bias=None, act=None, residual=None, keep=False, out=None, workspace=None, stream=None):
+    """residual + act(x w^T + bias): x [M, K], w [N, K], bias [N], residual [M, N] (may be `out`); act: None, "relu", "gelu" (by erf) or
+    "silu".  keep: returns (out, z) with z = x w^T + bias, which the gradients need (or the tensor to put it in)."""
+    if stream is not None:
+        return _on(stream, x, znni_linear, x, w, bias, act, residual, keep, out, workspace)
+    kind = _kind(x)
+    M, K = x.shape
+    N = w.shape[0]
+    out = _new(x, M, N) if out is None else out
+    z = None if keep is False else _new(x, M, N) if keep is True else keep
+    p, n, held = _scratch(_need(lib().znni_linear_workspace, kind[0], M, N, K), workspace, x)
+    _check(lib().znni_linear(kind[0], M, N, K, _rows(x, M, K, kind), _rows(w, N, K, kind), _vector(bias, N, kind), _ACTIVATIONS[act],
+                             _rows(residual, M, N, kind), _rows(z, M, N, kind), _rows(out, M, N, kind), p, n, _current(x)))
+    return out if z is None else (out, z)
+
+
+def znni_linear_backward_workspace(dtype, M, N, K, act=None, wanted=LINEAR_DX | LINEAR_DW | LINEAR_DBIAS):
+    return _need(lib().znni_linear_backward_workspace, _TYPES[dtype], int(M), int(N), int(K), _ACTIVATIONS[act], int(wanted))
+
+
+def znni_linear_backward(dout, x, w, z=None, act=None, bias=True, inputs=True, weights=True, dx=None, dw=None, dbias=None, workspace=None,
+                         stream=None):
+    """Gradients (dx, dw, dbias) of znni_linear from its result's, dout [M, N]; None for those that `inputs`, `weights` and `bias` do not ask
+    for.  z: what the forward call kept (with an activation).  The residual's gradient is dout."""
+    if stream is not None:
+        return _on(stream, dout, znni_linear_backward, dout, x, w, z, act, bias, inputs, weights, dx, dw, dbias, workspace)
+    kind = _kind(dout)
+    M, N = dout.shape
+    K = w.shape[1]
+    dx = (_new(dout, M, K) if dx is None else dx) if inputs else None
+    dw = (_new(dout, N, K) if dw is None else dw) if weights else None
+    dbias = (_new(dout, N) if dbias is None else dbias) if bias else None
+    wanted = (LINEAR_DX if inputs else 0) | (LINEAR_DW if weights else 0) | (LINEAR_DBIAS if bias else 0)
+    a = _ACTIVATIONS[act]
+    p, n, held = _scratch(_need(lib().znni_linear_backward_workspace, kind[0], M, N, K, a, wanted), workspace, dout)
+    _check(lib().znni_linear_backward(kind[0], M, N, K, _rows(dout, M, N, kind), _rows(x, M, K, kind), _rows(w, N, K, kind),
+                                      _rows(z, M, N, kind), a, _rows(dx, M, K, kind), _rows(dw, N, K, kind), _vector(dbias, N, kind), p, n,
+                                      _current(dout)))
+    return dx, dw, dbias
+
+
+def _gate(gate, T, C, kind):
+    """(whether one gate is for all tokens, its znni_rows)."""
+    if gate is None:
+        return 0, None
+    if gate.dim() == 1:
+        return NORM_GATE_SHARED, _rows_descriptor(_vector(gate, C, kind), C)
+    return 0, _rows(gate, T, C, kind)
+
+
+def znni_block_norm(x, y=None, gate=None, post=None, pre=None, scale=1.0, eps=1e-5, centred=False, norm_post=True, norm_pre=True, h=None,
+                    z=None, stream=None):
+    """(h, z): h = x + scale * gate * post * n(y), z = pre * n(h), for x, y [T, C], gate [T, C] or [C], post and pre [C] (None: ones).
+    n divides a row by its root mean square, or, `centred`, takes its mean off and divides it by its deviation.  Without norm_post y is taken as
+    it is, without norm_pre there is no z (None).  y None: there is no block, and h is x."""
+    if stream is not None:
+        return _on(stream, x, znni_block_norm, x, y, gate, post, pre, scale, eps, centred, norm_post, norm_pre, h, z)
+    kind = _kind(x)
+    T, C = x.shape
+    shared, dg = _gate(gate, T, C, kind)
+    norm_post = norm_post and y is not None
+    flags = (NORM_POST if norm_post else 0) | (NORM_PRE if norm_pre else 0) | (NORM_CENTRED if centred else 0) | shared
+    h = x if y is None else _new(x, T, C) if h is None else h
+    z = (_new(x, T, C) if z is None else z) if norm_pre else None
+    _check(lib().znni_block_norm(kind[0], T, C, _rows(x, T, C, kind), _rows(y, T, C, kind), dg, _vector(post, C, kind), _vector(pre, C, kind), scale, eps,
+                                 flags, _rows(h, T, C, kind) if y is not None else None, _rows(z, T, C, kind), _current(x)))
+    return h, z
+
+
+def znni_block_norm_backward_workspace(dtype, T, C):
+    return _need(lib().znni_block_norm_backward_workspace, _TYPES[dtype], int(T), int(C), 0)
+
+
+def znni_block_norm_backward(dh, dz, h, y=None, gate=None, post=None, pre=None, scale=1.0, eps=1e-5, centred=False, norm_post=True,
+                             norm_pre=True, dx=None, dy=None, dgate=None, dpost=None, dpre=None, workspace=None, stream=None):
+    """Gradients (dx, dy, dgate, dpost, dpre) of znni_block_norm from those of its results, dh (None: zero) and dz, and from h and y as it had
+    them; None for what the call does not have."""
+    if stream is not None:
+        return _on(stream, h, znni_block_norm_backward, dh, dz, h, y, gate, post, pre, scale, eps, centred, norm_post, norm_pre, dx, dy, dgate, dpost, dpre, workspace)
+    kind = _kind(h)
+    T, C = h.shape
+    shared, dg = _gate(gate, T, C, kind)
+    norm_post = norm_post and y is not None
+    flags = (NORM_POST if norm_post else 0) | (NORM_PRE if norm_pre else 0) | (NORM_CENTRED if centred else 0) | shared
+    dx = _new(h, T, C) if dx is None else dx
+    dy = (_new(h, T, C) if dy is None else dy) if y is not None else None
+    dgate = (_new(h, *gate.shape) if dgate is None else dgate) if gate is not None else None
+    dpost = (_new(h, C) if dpost is None else dpost) if post is not None else None
+    dpre = (_new(h, C) if dpre is None else dpre) if pre is not None else None
+    summed = shared or dpost is not None or dpre is not None
+    p, n, held = _scratch(_need(lib().znni_block_norm_backward_workspace, kind[0], T, C, flags) if summed else 0, workspace, h)
+    _check(lib().znni_block_norm_backward(kind[0], T, C, _rows(dh, T, C, kind), _rows(dz, T, C, kind), _rows(h, T, C, kind), _rows(y, T, C, kind), dg,
+                                          _vector(post, C, kind), _vector(pre, C, kind), scale, eps, flags, _rows(dx, T, C, kind),
+                                          _rows(dy, T, C, kind), _gate(dgate, T, C, kind)[1], _vector(dpost, C, kind), _vector(dpre, C, kind), p, n,
+                                          _current(h)))
+    return dx, dy, dgate, dpost, dpre

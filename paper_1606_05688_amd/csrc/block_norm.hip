@@ -1,0 +1,468 @@
+// block_norm.hip -- norms where a block ends and the next one begins, with the block's gate and scale, and their gradients.
+//
+//   h = x + scale * gate * post * n(y),   z = pre * n(h),   n(a) = a r,  r = 1 / sqrt(mean a^2 + eps)   (centred: of a - mean a)
+//   gradients: dx = dh + n'(h)[pre dz],   n'(a)[g] = r (g - n(a) mean(g n(a)))   (centred: less its mean);
+//   dgate = scale dx post n(y),   dy = n'(y)[scale dx gate post],   dpost = sum over tokens of scale dx gate n(y),   dpre = of dz n(h)
+//
+// Bound by memory: every tensor is read or written once.  Rows stay in registers, 8 or 32 elements a lane, one to eight waves a row.
+#include <initializer_list>
+#include <type_traits>
+
+#include "rows_common.h"
+
+namespace znni {
+
+struct NormArgs {
+    int T, C, per;                       // per: rows of a workgroup
+    float scale, eps;
+    bool post, pre, centred;             // whether y and h are normed, whether means are taken off
+    bool shared;                         // one gate for all tokens
+};
+
+template <typename T>
+struct Rows {
+    T* p;
+    long long row;
+};
+
+template <typename T>
+static Rows<T> rows_of(const znni_rows* r)
+{
+    return r ? Rows<T>{(T*)r->data, r->row} : Rows<T>{nullptr, 0};
+}
+
+// A row over the lanes of W waves: E elements a lane in vectors of VEC.
+template <typename T, int VEC, int E, int W>
+struct Row {
+    static constexpr int LANES = 64 * W, NV = E / VEC;
+    typedef T V __attribute__((ext_vector_type(VEC)));
+    __device__ static int column(int lane, int v) { return (v * LANES + lane) * VEC; }
+    __device__ static void load(V (&y)[NV], const T* p, int lane, int C)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = column(lane, v);
+            if (c < C) y[v] = *(const V*)(p + c);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) y[v][e] = (T)0.f;
+        }
+    }
+    __device__ static float sum(float x, float* shared)
+    {
+#pragma unroll
+        for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+        if constexpr (W > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+            __syncthreads();
+            x = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) x += shared[i];
+        }
+        return x;
+    }
+};
+
+// Mean (or 0) and factor of a row; lanes past its end hold zeros.
+template <typename R, int E, typename F>
+__device__ inline void moments(F at, const NormArgs& a, int lane, int vec, float* shared, float* mean, float* r)
+{
+    float s = 0.f, m = 0.f;
+    if (a.centred) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) s += at(i);
+        m = R::sum(s, shared) / a.C;
+        s = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const float d = R::column(lane, i / vec) < a.C ? at(i) - m : 0.f;
+        s += d * d;
+    }
+    *mean = m;
+    *r = 1.f / sqrtf(R::sum(s, shared) / a.C + a.eps);
+}
+
+template <typename T, int VEC, int E, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows<const T> x, Rows<const T> y, Rows<const T> gate, const T* post, const T* pre,
+                                                               Rows<T> h, Rows<T> z)
+{
+    using R = Row<T, VEC, E, W>;
+    typedef typename R::V V;
+    constexpr int NV = R::NV;
+    __shared__ float shared[W];
+    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const long long t = W == 1 ? group_id() * 4 + (threadIdx.x >> 6) : group_id();
+    if (t >= a.T) return;
+    V xv[NV];
+    R::load(xv, x.p + t * x.row, lane, a.C);
+    float s[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[i] = (float)xv[i / VEC][i % VEC];
+    float mean, r;
+    if (y.p) {
+        V yv[NV], w[NV], g[NV];
+        R::load(yv, y.p + t * y.row, lane, a.C);
+        if (gate.p) R::load(g, gate.p + t * gate.row, lane, a.C);
+        if (post) R::load(w, post, lane, a.C);
+        mean = 0.f;
+        r = 1.f;
+        if (a.post) moments<R, E>([&](int i) { return (float)yv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            float u = ((float)yv[i / VEC][i % VEC] - mean) * r;
+            if (post) u *= (float)w[i / VEC][i % VEC];
+            if (gate.p) u *= (float)g[i / VEC][i % VEC];
+            s[i] += a.scale * u;
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            V o;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o[e] = (T)s[v * VEC + e];
+            if (R::column(lane, v) < a.C) *(V*)(h.p + t * h.row + R::column(lane, v)) = o;
+            // (lanes past the row's end: whatever a mean taken off has left)
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[v * VEC + e] = 0.f;
+        }
+    }
+    if (!a.pre) return;
+    V w[NV];
+    if (pre) R::load(w, pre, lane, a.C);
+    moments<R, E>([&](int i) { return s[i]; }, a, lane, VEC, shared, &mean, &r);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        if (R::column(lane, v) >= a.C) continue;
+        V o;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            float n = (s[v * VEC + e] - mean) * r;
+            if (pre) n *= (float)w[v][e];
+            o[e] = (T)n;
+        }
+        *(V*)(z.p + t * z.row + R::column(lane, v)) = o;
+    }
+}
+
+// Where sums over tokens go: [workgroup][C] each, or NULL.
+struct NormSums {
+    float *gate, *post, *pre;
+};
+
+template <typename T, int VEC, int E, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a, Rows<const T> dh, Rows<const T> dz, Rows<const T> h, Rows<const T> y,
+                                                                    Rows<const T> gate, const T* post, const T* pre, Rows<T> dx, Rows<T> dy,
+                                                                    Rows<T> dgate, NormSums sums)
+{
+    using R = Row<T, VEC, E, W>;
+    typedef typename R::V V;
+    constexpr int NV = R::NV, AT_ONCE = W == 1 ? 4 : 1;
+    __shared__ float shared[W];
+    __shared__ float joined[W == 1 ? 4 * 64 * E : 1];
+    const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, mine = W == 1 ? threadIdx.x >> 6 : 0;
+    const long long t0 = group_id() * a.per, t1 = min((long long)a.T, t0 + a.per);
+    float sg[E], sp[E], sq[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) sg[i] = sp[i] = sq[i] = 0.f;
+    for (long long t = t0 + mine; t < t1; t += AT_ONCE) {
+        float d[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] = 0.f;
+        if (a.pre) {
+            V hv[NV], gv[NV], w[NV];
+            R::load(hv, h.p + t * h.row, lane, a.C);
+            R::load(gv, dz.p + t * dz.row, lane, a.C);
+            if (pre) R::load(w, pre, lane, a.C);
+            float mean, r, both = 0.f, only = 0.f;
+            moments<R, E>([&](int i) { return (float)hv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float n = ((float)hv[i / VEC][i % VEC] - mean) * r;
+                float g = (float)gv[i / VEC][i % VEC];
+                sq[i] += g * n;
+                if (pre) g *= (float)w[i / VEC][i % VEC];
+                d[i] = g;
+                both += g * n;
+                only += g;
+            }
+            both = R::sum(both, shared) / a.C;
+            only = a.centred ? R::sum(only, shared) / a.C : 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] = r * (d[i] - ((float)hv[i / VEC][i % VEC] - mean) * r * both - only);
+        }
+        if (dh.p) {
+            V gv[NV];
+            R::load(gv, dh.p + t * dh.row, lane, a.C);
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] += (float)gv[i / VEC][i % VEC];
+        }
+        auto put = [&](const Rows<T>& to, auto at) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (R::column(lane, v) >= a.C) continue;
+                V o;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) o[e] = (T)at(v * VEC + e);
+                *(V*)(to.p + t * to.row + R::column(lane, v)) = o;
+            }
+        };
+        if (dx.p) put(dx, [&](int i) { return d[i]; });
+        if (!y.p && !dy.p) continue;
+        V yv[NV], w[NV], gv[NV];
+        if (y.p) R::load(yv, y.p + t * y.row, lane, a.C);
+        if (post) R::load(w, post, lane, a.C);
+        if (gate.p) R::load(gv, gate.p + t * gate.row, lane, a.C);
+        float mean = 0.f, r = 1.f, both = 0.f, only = 0.f;
+        if (a.post) moments<R, E>([&](int i) { return (float)yv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
+        auto normed = [&](int i) { return ((float)yv[i / VEC][i % VEC] - mean) * r; };
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] *= a.scale;
+        if (gate.p) {
+            auto of_gate = [&](int i) { return d[i] * normed(i) * (post ? (float)w[i / VEC][i % VEC] : 1.f); };
+            if (dgate.p) put(dgate, of_gate);
+            if (sums.gate)
+#pragma unroll
+                for (int i = 0; i < E; ++i) sg[i] += of_gate(i);
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] *= (float)gv[i / VEC][i % VEC];
+        }
+        if (a.post) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float n = normed(i);
+                sp[i] += d[i] * n;
+                if (post) d[i] *= (float)w[i / VEC][i % VEC];
+                if (R::column(lane, i / VEC) >= a.C) d[i] = 0.f;
+                both += d[i] * n;
+                only += d[i];
+            }
+            both = R::sum(both, shared) / a.C;
+            only = a.centred ? R::sum(only, shared) / a.C : 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] = r * (d[i] - normed(i) * both - only);
+        }
+        if (dy.p) put(dy, [&](int i) { return d[i]; });
+    }
+    auto write = [&](float* to, const float (&s)[E]) {
+        if (!to) return;
+        to += group_id() * a.C;
+        if constexpr (W == 1) {
+            // the four waves' sums, in their order
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < E; ++i) joined[(mine * E + i) * 64 + lane] = s[i];
+            __syncthreads();
+            for (int i = mine; i < E; i += 4) {
+                const int c = R::column(lane, i / VEC) + i % VEC;
+                if (c < a.C) to[c] = (joined[i * 64 + lane] + joined[(E + i) * 64 + lane]) + (joined[(2 * E + i) * 64 + lane] + joined[(3 * E + i) * 64 + lane]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int c = R::column(lane, i / VEC) + i % VEC;
+                if (c < a.C) to[c] = s[i];
+            }
+        }
+    };
+    write(sums.gate, sg);
+    write(sums.post, sp);
+    write(sums.pre, sq);
+}
+
+constexpr int NORM_MOST = 16384;          // channels
+constexpr int NORM_GROUPS = 512;          // workgroups that share the rows, where sums over tokens are wanted
+
+// Elements a lane and waves a row: 8 and 1, 8 and 4, 32 and 1, 2, 4 or 8.
+struct NormShape {
+    int E, W;
+};
+static NormShape norm_shape(int T, int C)
+{
+    if (C <= 512) return {8, 1};
+    if (C <= 2048) return T <= 1024 ? NormShape{8, 4} : NormShape{32, 1};
+    return {32, C <= 4096 ? 2 : C <= 8192 ? 4 : 8};
+}
+
+static int norm_rows(int T, int C, bool sums)
+{
+    const int once = norm_shape(T, C).W == 1 ? 4 : 1;
+    if (!sums) return once;
+    const long long n = ((long long)T + NORM_GROUPS - 1) / NORM_GROUPS;
+    return (int)((n + once - 1) / once * once);
+}
+
+template <typename T, typename F>
+static znni_status with_row(int n, int C, bool wide, F f)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const NormShape s = norm_shape(n, C);
+    auto go = [&](auto vec) {
+        constexpr int V = decltype(vec)::value;
+        if (s.E == 8) return s.W == 1 ? f(Row<T, V, 8, 1>()) : f(Row<T, V, 8, 4>());
+        return s.W == 1 ? f(Row<T, V, 32, 1>()) : s.W == 2 ? f(Row<T, V, 32, 2>()) : s.W == 4 ? f(Row<T, V, 32, 4>()) : f(Row<T, V, 32, 8>());
+    };
+    if (wide) go(std::integral_constant<int, VEC>());
+    else go(std::integral_constant<int, 1>());
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+}
+
+template <typename T>
+static bool all_wide(int C, std::initializer_list<const znni_rows*> rows, std::initializer_list<const void*> vectors)
+{
+    if (C % (16 / (int)sizeof(T))) return false;
+    for (const znni_rows* r : rows)
+        if (r && !rows_wide(r->data, r->row, sizeof(T), 16)) return false;
+    for (const void* p : vectors)
+        if ((uintptr_t)p & 15u) return false;
+    return true;
+}
+
+template <typename T, int VEC, int E, int W, typename... A>
+static void launch_norm(Row<T, VEC, E, W>, dim3 grid, hipStream_t st, A... args)
+{
+    k_norm<T, VEC, E, W><<<grid, dim3(W == 1 ? 256 : 64 * W), 0, st>>>(args...);
+}
+
+template <typename T, int VEC, int E, int W, typename... A>
+static void launch_norm_back(Row<T, VEC, E, W>, dim3 grid, hipStream_t st, A... args)
+{
+    k_norm_back<T, VEC, E, W><<<grid, dim3(W == 1 ? 256 : 64 * W), 0, st>>>(args...);
+}
+
+template <typename T>
+static znni_status norm_forward(NormArgs a, const znni_rows* x, const znni_rows* y, const znni_rows* gate, const void* post, const void* pre,
+                                const znni_rows* h, const znni_rows* z, hipStream_t st)
+{
+    const dim3 grid = launch_of(((long long)a.T + a.per - 1) / a.per);
+    Rows<const T> g = rows_of<const T>(gate);
+    if (a.shared) g.row = 0;
+    const znni_rows one = {(void*)g.p, g.row};
+    return with_row<T>(a.T, a.C, all_wide<T>(a.C, {x, y, gate ? &one : nullptr, h, z}, {post, pre}), [&](auto row) {
+        launch_norm(row, grid, st, a, rows_of<const T>(x), rows_of<const T>(y), g, (const T*)post, (const T*)pre, rows_of<T>(h), rows_of<T>(z));
+        return 0;
+    });
+}
+
+template <typename T>
+static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_rows* dz, const znni_rows* h, const znni_rows* y, const znni_rows* gate,
+                                 const void* post, const void* pre, const znni_rows* dx, const znni_rows* dy, const znni_rows* dgate, void* dpost,
+                                 void* dpre, float* workspace, hipStream_t st)
+{
+    Rows<const T> g = rows_of<const T>(gate);
+    if (a.shared) g.row = 0;
+    const znni_rows one = {(void*)g.p, g.row};
+    const bool summed = a.shared && dgate;
+    const int groups = a.T ? (int)(((long long)a.T + a.per - 1) / a.per) : 0;
+    const size_t step = up((size_t)NORM_GROUPS * a.C * sizeof(float)) / sizeof(float);
+    NormSums sums = {};
+    SumOut<T> o = {};
+    int n = 0;
+    auto wants = [&](bool wanted, void* to) -> float* {
+        if (!wanted) return nullptr;
+        float* from = workspace + n * step;
+        o.to[n] = (T*)to;
+        o.from[n++] = from;
+        return from;
+    };
+    sums.gate = wants(summed, summed ? dgate->data : nullptr);
+    sums.post = wants(dpost, dpost);
+    sums.pre = wants(dpre, dpre);
+    if (a.T > 0) {
+        const Rows<T> dg = summed ? Rows<T>{nullptr, 0} : rows_of<T>(dgate);
+        const bool wide = all_wide<T>(a.C, {dh, dz, h, y, gate ? &one : nullptr, dx, dy, summed ? nullptr : dgate}, {post, pre});
+        const znni_status rc = with_row<T>(a.T, a.C, wide, [&](auto row) {
+            launch_norm_back(row, launch_of(((long long)a.T + a.per - 1) / a.per), st, a, rows_of<const T>(dh), rows_of<const T>(dz), rows_of<const T>(h), rows_of<const T>(y), g,
+                             (const T*)post, (const T*)pre, rows_of<T>(dx), rows_of<T>(dy), dg, sums);
+            return 0;
+        });
+        if (rc) return rc;
+    }
+    return n ? launch_sum_parts<T>(a.C, groups, o, n, st) : ZNNI_OK;
+}
+
+static znni_status norm_shape_fine(int type, int T, int C, unsigned flags)
+{
+    if (!type_ok(type)) return ZNNI_ERR_TYPE;
+    if (flags & ~(ZNNI_NORM_POST | ZNNI_NORM_PRE | ZNNI_NORM_CENTRED | ZNNI_NORM_GATE_SHARED)) return ZNNI_ERR_FLAGS;
+    if (T < 0 || C < 1 || T > ROWS_MOST) return ZNNI_ERR_SHAPE;
+    return C > NORM_MOST ? ZNNI_ERR_UNSUPPORTED_SIZE : ZNNI_OK;
+}
+
+}  // namespace znni
+
+using namespace znni;
+
+extern "C" {
+
+znni_status znni_block_norm(int type, int T, int C, const znni_rows* x, const znni_rows* y, const znni_rows* gate, const void* post, const void* pre,
+                            float scale, float eps, unsigned flags, const znni_rows* h, const znni_rows* z, void* stream)
+{
+    znni_status rc = norm_shape_fine(type, T, C, flags);
+    if (rc) return rc;
+    const bool has_pre = flags & ZNNI_NORM_PRE, has_post = flags & ZNNI_NORM_POST, shared = flags & ZNNI_NORM_GATE_SHARED;
+    if (!x || !y != !h || (has_pre && !z)) return ZNNI_ERR_NULL;
+    // what a call does not use has no place in it
+    if ((!y && (gate || has_post)) || (post && !has_post) || ((pre || z) && !has_pre) || (shared && !gate) || (!y && !has_pre)) return ZNNI_ERR_FLAGS;
+    if (T == 0) return ZNNI_OK;
+    if ((rc = rows_fine(x, type, T, C, false)) || (has_pre && (rc = rows_fine(z, type, T, C, true)))) return rc;
+    if (y && ((rc = rows_fine(y, type, T, C, false)) || (rc = rows_fine(h, type, T, C, true)))) return rc;
+    if (gate && (rc = rows_fine(gate, type, shared ? 1 : T, C, false))) return rc;
+    if (((uintptr_t)post | (uintptr_t)pre) % type_size(type)) return ZNNI_ERR_ALIGN;
+    const NormArgs a = {T, C, norm_rows(T, C, false), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
+    const hipStream_t st = (hipStream_t)stream;
+    switch (type) {
+        case ZNNI_F32: return norm_forward<float>(a, x, y, gate, post, pre, h, z, st);
+        case ZNNI_BF16: return norm_forward<bf16>(a, x, y, gate, post, pre, h, z, st);
+        default: return norm_forward<f16>(a, x, y, gate, post, pre, h, z, st);
+    }
+}
+
+znni_status znni_block_norm_backward_workspace(int type, int T, int C, unsigned flags, size_t* bytes)
+{
+    if (!bytes) return ZNNI_ERR_NULL;
+    const znni_status rc = norm_shape_fine(type, T, C, flags);
+    if (rc) return rc;
+    *bytes = 3 * up((size_t)NORM_GROUPS * C * sizeof(float));
+    return ZNNI_OK;
+}
+
+znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh, const znni_rows* dz, const znni_rows* h, const znni_rows* y,
+                                     const znni_rows* gate, const void* post, const void* pre, float scale, float eps, unsigned flags,
+                                     const znni_rows* dx, const znni_rows* dy, const znni_rows* dgate, void* dpost, void* dpre, void* workspace,
+                                     size_t workspace_bytes, void* stream)
+{
+    size_t need = 0;
+    znni_status rc = znni_block_norm_backward_workspace(type, T, C, flags, &need);
+    if (rc) return rc;
+    const bool has_pre = flags & ZNNI_NORM_PRE, has_post = flags & ZNNI_NORM_POST, shared = flags & ZNNI_NORM_GATE_SHARED;
+    if ((has_pre && (!h || !dz)) || (!has_pre && !dh)) return ZNNI_ERR_NULL;
+    if ((has_post || dgate || dpost) && !y) return ZNNI_ERR_NULL;
+    if (dgate && !gate) return ZNNI_ERR_NULL;
+    if ((post && !has_post) || (dpost && !has_post) || ((pre || dz || dpre) && !has_pre) || (shared && !gate)) return ZNNI_ERR_FLAGS;
+    const bool summed = (shared && dgate) || dpost || dpre;
+    if ((rc = dh ? rows_fine(dh, type, T, C, false) : ZNNI_OK)) return rc;
+    if (has_pre && ((rc = rows_fine(dz, type, T, C, false)) || (rc = rows_fine(h, type, T, C, false)))) return rc;
+    if (y && (rc = rows_fine(y, type, T, C, false))) return rc;
+    if (gate && (rc = rows_fine(gate, type, shared ? 1 : T, C, false))) return rc;
+    for (const znni_rows* o : {dx, dy})
+        if (o && (rc = rows_fine(o, type, T, C, true))) return rc;
+    if (dgate && (rc = rows_fine(dgate, type, shared ? 1 : T, C, true))) return rc;
+    if (((uintptr_t)post | (uintptr_t)pre | (uintptr_t)dpost | (uintptr_t)dpre) % type_size(type)) return ZNNI_ERR_ALIGN;
+    if (summed) {
+        if (!workspace) return ZNNI_ERR_NULL;
+        if ((uintptr_t)workspace & 255u) return ZNNI_ERR_ALIGN;
+        if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
+    }
+    const NormArgs a = {T, C, norm_rows(T, C, summed), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
+    float* const ws = (float*)workspace;
+    const hipStream_t st = (hipStream_t)stream;
+    switch (type) {
+        case ZNNI_F32: return norm_backward<float>(a, dh, dz, h, y, gate, post, pre, dx, dy, dgate, dpost, dpre, ws, st);
+        case ZNNI_BF16: return norm_backward<bf16>(a, dh, dz, h, y, gate, post, pre, dx, dy, dgate, dpost, dpre, ws, st);
+        default: return norm_backward<f16>(a, dh, dz, h, y, gate, post, pre, dx, dy, dgate, dpost, dpre, ws, st);
+    }
+}
+
+}  // extern "C"

@@ -1,0 +1,509 @@
+// linear.hip -- matrix products of tokens with weights: bias, activation and residual where the product ends, and the gradients.
+//
+//   out[m][n] = residual[m][n] + act(z[m][n]),   z[m][n] = sum_k x[m][k] w[n][k] + bias[n]
+//   dz = dout act'(z),   dx[m][k] = sum_n dz[m][n] w[n][k],   dw[n][k] = sum_m dz[m][n] x[m][k],   dbias[n] = sum_m dz[m][n]
+#include <type_traits>
+
+#include "product_tile.h"
+#include "rows_common.h"
+
+namespace znni {
+
+// ---- activations ----------------------------------------------------------------------------------------------------
+
+template <int ACT>
+__device__ inline float activated(float z)
+{
+    if constexpr (ACT == ZNNI_ACT_RELU) return z < 0.f ? 0.f : z;            // (NaN stays)
+    if constexpr (ACT == ZNNI_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752440f * z);
+    if constexpr (ACT == ZNNI_ACT_SILU) return z / (1.f + expf(-z));
+    return z;
+}
+
+template <int ACT>
+__device__ inline float slope(float z)
+{
+    if constexpr (ACT == ZNNI_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
+    if constexpr (ACT == ZNNI_ACT_GELU) return 0.5f * erfcf(-0.70710678118654752440f * z) + z * expf(-0.5f * z * z) * 0.39894228040143267794f;
+    if constexpr (ACT == ZNNI_ACT_SILU) {
+        const float p = 1.f / (1.f + expf(-z));
+        return p * (1.f + z * (1.f - p));
+    }
+    return 1.f;
+}
+
+template <typename F>
+static auto with_act(int act, F f)
+{
+    switch (act) {
+        case ZNNI_ACT_RELU: return f(std::integral_constant<int, ZNNI_ACT_RELU>());
+        case ZNNI_ACT_GELU: return f(std::integral_constant<int, ZNNI_ACT_GELU>());
+        case ZNNI_ACT_SILU: return f(std::integral_constant<int, ZNNI_ACT_SILU>());
+        default: return f(std::integral_constant<int, ZNNI_ACT_NONE>());
+    }
+}
+
+// ---- where a product ends -------------------------------------------------------------------------------------------
+
+template <typename T>
+struct End {
+    const T* bias;
+    const T* residual;
+    T* z;
+    T* out;
+    long long residual_row, z_row, out_row;
+    bool wide;                  // four elements of every row are aligned
+    float* parts;               // sums of a part of the steps, [split][M][Np], instead of all that
+    int Np;
+};
+
+// Four consecutive elements of a row, of which n are there.
+template <typename T, int ACT>
+__device__ inline void end_four(const End<T>& d, long long m, int n, int there, float4 v)
+{
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    float y[4] = {v.x, v.y, v.z, v.w};
+    const bool whole = d.wide && there >= 4;
+    T4 b = {}, r = {}, z, o;
+    if (whole) {
+        if (d.bias) b = *(const T4*)(d.bias + n);
+        if (d.residual) r = *(const T4*)(d.residual + m * d.residual_row + n);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e >= there) break;
+            if (d.bias) b[e] = d.bias[n + e];
+            if (d.residual) r[e] = d.residual[m * d.residual_row + n + e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (d.bias) y[e] += (float)b[e];
+        z[e] = (T)y[e];
+        y[e] = activated<ACT>(y[e]);
+        if (d.residual) y[e] += (float)r[e];
+        o[e] = (T)y[e];
+    }
+    if (whole) {
+        if (d.z) *(T4*)(d.z + m * d.z_row + n) = z;
+        *(T4*)(d.out + m * d.out_row + n) = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e >= there) break;
+            if (d.z) d.z[m * d.z_row + n + e] = z[e];
+            d.out[m * d.out_row + n + e] = o[e];
+        }
+    }
+}
+
+// ---- products over tiles --------------------------------------------------------------------------------------------
+
+struct ProductArgs {
+    int M, N, K;
+    int tiles_m, tiles_n, splits, per;      // steps of the sum that a split takes
+};
+
+// out^T [n][m] += W^T X: the columns of the result are the left operand, so that a lane holds four consecutive columns of a row.
+// WAVES_N x WAVES_M waves of NB x MB products of 32 x 32.
+template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES, int ACT>
+__global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductArgs a, Side<T> left, Side<T> right, End<T> d)
+{
+    constexpr int THREADS = 64 * WAVES_N * WAVES_M, TN = WAVES_N * NB * 32, TM = WAVES_M * MB * 32;
+    using L = Tile<T, LI, TN, THREADS>;
+    using R = Tile<T, RI, TM, THREADS>;
+    using M = Mfma<T>;
+    __shared__ __align__(1024) char tiles[STAGES][L::BYTES + R::BYTES];
+    const long long groups = (long long)a.tiles_m * a.tiles_n * a.splits;
+    const long long group = group_id();
+    if (group >= groups) return;
+    long long id = group;
+    const int split = (int)(id % a.splits); id /= a.splits;
+    const int tm = (int)(id % a.tiles_m), tn = (int)(id / a.tiles_m);
+    const int m0 = tm * TM, n0 = tn * TN;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wn = wave % WAVES_N * NB * 32, wm = wave / WAVES_N * MB * 32;
+    const int begin = split * a.per, end = min(a.K, begin + a.per);
+    const int n = end > begin ? (end - begin + L::BK - 1) / L::BK : 0;
+    L lt;
+    R rt;
+    lt.find(left, n0, t);
+    rt.find(right, m0, t);
+    auto bring = [&](int it) {
+        char* const to = tiles[it % STAGES];
+        lt.bring(left, n0, begin + it * L::BK, end, to, t);
+        rt.bring(right, m0, begin + it * L::BK, end, to + L::BYTES, t);
+    };
+    constexpr int ONE = STAGES > 2 ? L::PER + R::PER : 0, TWO = STAGES > 3 ? 2 * ONE : 0;      // loads of tiles behind the present one
+    f32x16 acc[NB][MB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < n) bring(i);
+    for (int it = 0; it < n; ++it) {
+        // tile `it` is there, those behind it may be on their way
+        const int behind = min(STAGES - 2, n - 1 - it);
+        if (STAGES > 3 && behind == 2) wait_but_and_meet<TWO>();
+        else if (STAGES > 2 && behind == 1) wait_but_and_meet<ONE>();
+        else wait_but_and_meet<0>();
+        if (it + STAGES - 1 < n) bring(it + STAGES - 1);
+        const char* const lb = tiles[it % STAGES];
+        const char* const rb = lb + L::BYTES;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            typename M::V x[NB], y[MB];
+#pragma unroll
+            for (int i = 0; i < NB; ++i) x[i] = L::operand(lb, wn + 32 * i, c, l);
+#pragma unroll
+            for (int j = 0; j < MB; ++j) y[j] = R::operand(rb, wm + 32 * j, c, l);
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) {
+                    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j] = M::mul(x[i][e], y[j][e], acc[i][j]);
+                    } else {
+                        acc[i][j] = M::mul(x[i], y[j], acc[i][j]);
+                    }
+                }
+        }
+    }
+    const int h = l >> 5, c32 = l & 31;
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+        const int m = m0 + wm + 32 * j + c32;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int col = n0 + wn + 32 * i + 8 * q + 4 * h;
+                if (col >= a.N) continue;
+                const float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                if (a.splits > 1) *(float4*)(d.parts + ((long long)split * a.M + m) * d.Np + col) = v;
+                else end_four<T, ACT>(d, m, col, a.N - col, v);
+            }
+    }
+}
+
+// Sums of the parts of the steps, then what an unsplit product does at its end.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void k_product_join(int M, int N, int splits, End<T> d)
+{
+    const long long i = (group_id() * 256 + threadIdx.x) * 4;
+    const int n = (int)(i % d.Np);
+    const long long m = i / d.Np;
+    if (m >= M) return;
+    float4 v = {0.f, 0.f, 0.f, 0.f};
+    const long long step = (long long)M * d.Np;
+    for (int s = 0; s < splits; ++s) {
+        const float4 p = *(const float4*)(d.parts + s * step + i);
+        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+    }
+    end_four<T, ACT>(d, m, n, N - n, v);
+}
+
+constexpr int SPLITS_MOST = 32;
+
+struct ProductPlan {
+    int kind;                    // 0: tiles of 64 x 64, 1: 128 x 128, 2: 256 x 256
+    int splits, per;
+    size_t parts;                // elements
+};
+
+static ProductPlan product_plan(int type, int M, int N, int K)
+{
+    ProductPlan p;
+    const int bk = type == ZNNI_F32 ? 32 : 64;
+    auto tiles = [&](long long e) { return ((M + e - 1) / e) * ((N + e - 1) / e); };
+    p.kind = type != ZNNI_F32 && tiles(256) >= 256 ? 2 : tiles(128) >= 256 ? 1 : 0;
+    const long long n = tiles(64 << p.kind), steps = ((long long)K + bk - 1) / bk;
+    long long s = p.kind == 0 && n < 256 ? 512 / (n ? n : 1) : 1;
+    if (s > steps / 2) s = steps / 2;
+    if (s > SPLITS_MOST) s = SPLITS_MOST;
+    if (s < 1) s = 1;
+    p.per = (int)((steps + s - 1) / s * bk);
+    p.splits = K ? (int)(((long long)K + p.per - 1) / p.per) : 1;
+    p.parts = p.splits > 1 ? (size_t)p.splits * M * ((N + 3) / 4 * 4) : 0;
+    return p;
+}
+
+template <typename T, bool LI, bool RI, int ACT>
+static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> right, End<T> d, hipStream_t st)
+{
+    const int type = sizeof(T) == 4 ? ZNNI_F32 : ZNNI_BF16;
+    const ProductPlan p = product_plan(type, M, N, K);
+    d.Np = (N + 3) / 4 * 4;
+    ProductArgs a = {M, N, K, 0, 0, p.splits, p.per};
+    const int edge = 64 << p.kind;
+    a.tiles_m = (M + edge - 1) / edge;
+    a.tiles_n = (N + edge - 1) / edge;
+    const dim3 grid = launch_of((long long)a.tiles_m * a.tiles_n * p.splits);
+    if (p.kind == 0) k_product<T, LI, RI, 2, 2, 1, 1, 4, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
+    else if (p.kind == 1) k_product<T, LI, RI, 2, 2, 2, 2, 2, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
+    else if constexpr (sizeof(T) == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(512), 0, st>>>(a, left, right, d);
+    if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    if (p.splits == 1) return ZNNI_OK;
+    k_product_join<T, ACT><<<launch_of(((long long)M * d.Np / 4 + 255) / 256), dim3(256), 0, st>>>(M, N, p.splits, d);
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+}
+
+// ---- gradient of what went into the activation, sums over tokens ----------------------------------------------------
+
+constexpr int SLOPE_ROWS = 8;             // rows of a workgroup at a time
+constexpr int SLOPE_PARTS = 256;          // parts of a sum over all tokens at most
+
+// dz = dout act'(z) (written if there is an activation), and its sum over `per` rows, 32 chunks of columns by 8 rows a workgroup.
+template <typename T, int ACT, int VEC>
+__global__ __launch_bounds__(256) void k_slope(int M, int N, int per, const T* __restrict__ dout, long long dout_row, const T* __restrict__ z,
+                                               long long z_row, T* __restrict__ dz, int dz_row, float* __restrict__ sums)
+{
+    typedef T V __attribute__((ext_vector_type(VEC)));
+    __shared__ float part[SLOPE_ROWS][32 * VEC];
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, n = ((int)blockIdx.x * 32 + c) * VEC;
+    const int m0 = (int)blockIdx.y * per, m1 = (int)min((long long)M, (long long)m0 + per);
+    float s[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+    if (n < N)
+        for (int m = m0 + r; m < m1; m += SLOPE_ROWS) {
+            V g = *(const V*)(dout + m * dout_row + n);
+            if constexpr (ACT != ZNNI_ACT_NONE) {
+                const V y = *(const V*)(z + m * z_row + n);
+                V o;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float f = (float)g[e] * slope<ACT>((float)y[e]);
+                    s[e] += f;
+                    o[e] = (T)f;
+                }
+                *(V*)(dz + (long long)m * dz_row + n) = o;
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[e] += (float)g[e];
+            }
+        }
+    if (!sums) return;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) part[r][c * VEC + e] = s[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * VEC; i += 256) {
+        const int col = (int)blockIdx.x * 32 * VEC + i;
+        if (col >= N) break;
+        float y = 0.f;
+#pragma unroll
+        for (int q = 0; q < SLOPE_ROWS; ++q) y += part[q][i];
+        sums[(long long)blockIdx.y * N + col] = y;
+    }
+}
+
+static int slope_parts(int M, int N)
+{
+    // about 1024 workgroups, of 32 rows at least
+    const long long across = ((long long)N + 255) / 256;
+    long long n = 1024 / (across > 0 ? across : 1);
+    if (n > ((long long)M + 31) / 32) n = ((long long)M + 31) / 32;
+    if (n > SLOPE_PARTS) n = SLOPE_PARTS;
+    return n < 1 ? 1 : (int)n;
+}
+
+// ---- what a call needs ----------------------------------------------------------------------------------------------
+
+struct BackwardPlan {
+    size_t dz, sums, parts;            // bytes
+    int dz_row;
+    size_t all() const { return dz + sums + parts; }
+};
+
+static BackwardPlan backward_plan(int type, int M, int N, int K, int act, bool dx, bool dw, bool dbias)
+{
+    BackwardPlan p = {};
+    const int per = 16 / type_size(type);
+    p.dz_row = (int)(((long long)N + per - 1) / per * per);
+    const bool products = dx || dw;
+    if (act != ZNNI_ACT_NONE && (products || dbias)) p.dz = up((size_t)M * p.dz_row * type_size(type));
+    if (dbias) p.sums = up((size_t)slope_parts(M, N) * N * sizeof(float));
+    size_t parts = 0;
+    if (dx) parts = product_plan(type, M, K, N).parts;
+    if (dw) {
+        const size_t q = product_plan(type, N, K, M).parts;
+        if (q > parts) parts = q;
+    }
+    p.parts = up(parts * sizeof(float));
+    return p;
+}
+
+template <typename T>
+static Side<T> side_of(const znni_rows* r, int rows)
+{
+    return {(const T*)r->data, r->row, rows, rows_wide(r->data, r->row, sizeof(T), 16)};
+}
+
+template <typename T>
+static End<T> end_of(const znni_rows* out)
+{
+    End<T> d = {};
+    d.out = (T*)out->data;
+    d.out_row = out->row;
+    d.wide = rows_wide(out->data, out->row, sizeof(T), 4 * sizeof(T));
+    return d;
+}
+
+template <typename T>
+static znni_status forward(int M, int N, int K, const znni_rows* x, const znni_rows* w, const void* bias, int act, const znni_rows* residual,
+                           const znni_rows* z, const znni_rows* out, void* workspace, hipStream_t st)
+{
+    End<T> d = end_of<T>(out);
+    const int four = 4 * sizeof(T);
+    d.bias = (const T*)bias;
+    d.wide = d.wide && !((uintptr_t)bias % four);
+    if (residual) {
+        d.residual = (const T*)residual->data;
+        d.residual_row = residual->row;
+        d.wide = d.wide && rows_wide(residual->data, residual->row, sizeof(T), four);
+    }
+    if (z) {
+        d.z = (T*)z->data;
+        d.z_row = z->row;
+        d.wide = d.wide && rows_wide(z->data, z->row, sizeof(T), four);
+    }
+    d.parts = (float*)workspace;
+    return with_act(act, [&](auto k) {
+        return launch_product<T, true, true, decltype(k)::value>(M, N, K, side_of<T>(w, N), side_of<T>(x, M), d, st);
+    });
+}
+
+template <typename T>
+static znni_status backward(int type, int M, int N, int K, const znni_rows* dout, const znni_rows* x, const znni_rows* w, const znni_rows* z, int act,
+                            const znni_rows* dx, const znni_rows* dw, void* dbias, void* workspace, hipStream_t st)
+{
+    const BackwardPlan p = backward_plan(type, M, N, K, act, dx, dw, dbias);
+    char* at = (char*)workspace;
+    T* const dz = (T*)at;
+    float* const sums = dbias ? (float*)(at + p.dz) : nullptr;
+    float* const parts = (float*)(at + p.dz + p.sums);
+    znni_rows g = *dout;
+    if (M > 0 && N > 0 && (act != ZNNI_ACT_NONE || dbias)) {
+        const int n = slope_parts(M, N), per = (int)(((long long)M + n - 1) / n);
+        const T* y = z ? (const T*)z->data : nullptr;
+        const long long yr = z ? z->row : 0;
+        constexpr int WIDE = 16 / sizeof(T);
+        const bool wide = N % WIDE == 0 && rows_wide(dout->data, dout->row, sizeof(T), 16) && (!z || rows_wide(y, yr, sizeof(T), 16));
+        with_act(act, [&](auto k) {
+            constexpr int ACT = decltype(k)::value;
+            const int across = wide ? 32 * WIDE : 32;
+            const dim3 grid((unsigned)((N + (long long)across - 1) / across), (unsigned)n);
+            if (wide) k_slope<T, ACT, WIDE><<<grid, dim3(256), 0, st>>>(M, N, per, (const T*)dout->data, dout->row, y, yr, dz, p.dz_row, sums);
+            else k_slope<T, ACT, 1><<<grid, dim3(256), 0, st>>>(M, N, per, (const T*)dout->data, dout->row, y, yr, dz, p.dz_row, sums);
+            return 0;
+        });
+        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+        if (act != ZNNI_ACT_NONE) g = {dz, p.dz_row};
+    }
+    if (dbias && N > 0) {
+        const znni_status rc = launch_sum_parts<T>(N, M > 0 ? slope_parts(M, N) : 0, SumOut<T>{{(T*)dbias}, {sums}}, 1, st);
+        if (rc) return rc;
+    }
+    if (dx && M > 0 && K > 0) {
+        End<T> d = end_of<T>(dx);
+        d.parts = parts;
+        const znni_status rc = launch_product<T, false, true, ZNNI_ACT_NONE>(M, K, N, side_of<T>(w, K), side_of<T>(&g, M), d, st);
+        if (rc) return rc;
+    }
+    if (dw && N > 0 && K > 0) {
+        End<T> d = end_of<T>(dw);
+        d.parts = parts;
+        const znni_status rc = launch_product<T, false, false, ZNNI_ACT_NONE>(N, K, M, side_of<T>(x, K), side_of<T>(&g, N), d, st);
+        if (rc) return rc;
+    }
+    return ZNNI_OK;
+}
+
+static znni_status linear_shape(int type, int M, int N, int K)
+{
+    if (!type_ok(type)) return ZNNI_ERR_TYPE;
+    if (M < 0 || N < 0 || K < 0 || M > ROWS_MOST || N > COLS_MOST || K > COLS_MOST) return ZNNI_ERR_SHAPE;
+    return ZNNI_OK;
+}
+
+}  // namespace znni
+
+using namespace znni;
+
+extern "C" {
+
+znni_status znni_linear_workspace(int type, int M, int N, int K, size_t* bytes)
+{
+    if (!bytes) return ZNNI_ERR_NULL;
+    const znni_status rc = linear_shape(type, M, N, K);
+    if (rc) return rc;
+    *bytes = M > 0 && N > 0 ? up(product_plan(type, M, N, K).parts * sizeof(float)) : 0;
+    return ZNNI_OK;
+}
+
+znni_status znni_linear(int type, int M, int N, int K, const znni_rows* x, const znni_rows* w, const void* bias, int act,
+                        const znni_rows* residual, const znni_rows* z, const znni_rows* out, void* workspace, size_t workspace_bytes,
+                        void* stream)
+{
+    if (!x || !w || !out) return ZNNI_ERR_NULL;
+    if (act < ZNNI_ACT_NONE || act > ZNNI_ACT_SILU) return ZNNI_ERR_FLAGS;
+    size_t need = 0;
+    znni_status rc = znni_linear_workspace(type, M, N, K, &need);
+    if (rc) return rc;
+    if (M == 0 || N == 0) return ZNNI_OK;
+    if ((rc = rows_fine(x, type, M, K, false)) || (rc = rows_fine(w, type, N, K, false)) || (rc = rows_fine(out, type, M, N, true))) return rc;
+    if (residual && (rc = rows_fine(residual, type, M, N, false))) return rc;
+    if (z && (rc = rows_fine(z, type, M, N, true))) return rc;
+    if (need && !workspace) return ZNNI_ERR_NULL;
+    if ((uintptr_t)bias % type_size(type) || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
+    if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
+    const hipStream_t st = (hipStream_t)stream;
+    switch (type) {
+        case ZNNI_F32: return forward<float>(M, N, K, x, w, bias, act, residual, z, out, workspace, st);
+        case ZNNI_BF16: return forward<bf16>(M, N, K, x, w, bias, act, residual, z, out, workspace, st);
+        default: return forward<f16>(M, N, K, x, w, bias, act, residual, z, out, workspace, st);
+    }
+}
+
+znni_status znni_linear_backward_workspace(int type, int M, int N, int K, int act, unsigned wanted, size_t* bytes)
+{
+    if (!bytes) return ZNNI_ERR_NULL;
+    if (act < ZNNI_ACT_NONE || act > ZNNI_ACT_SILU || wanted & ~(ZNNI_LINEAR_DX | ZNNI_LINEAR_DW | ZNNI_LINEAR_DBIAS)) return ZNNI_ERR_FLAGS;
+    const znni_status rc = linear_shape(type, M, N, K);
+    if (rc) return rc;
+    *bytes = backward_plan(type, M, N, K, act, wanted & ZNNI_LINEAR_DX, wanted & ZNNI_LINEAR_DW, wanted & ZNNI_LINEAR_DBIAS).all();
+    return ZNNI_OK;
+}
+
+znni_status znni_linear_backward(int type, int M, int N, int K, const znni_rows* dout, const znni_rows* x, const znni_rows* w,
+                                 const znni_rows* z, int act, const znni_rows* dx, const znni_rows* dw, void* dbias, void* workspace,
+                                 size_t workspace_bytes, void* stream)
+{
+    if (!dout || (dw && !x) || (dx && !w)) return ZNNI_ERR_NULL;
+    size_t need = 0;
+    znni_status rc = znni_linear_backward_workspace(type, M, N, K, act, (dx ? ZNNI_LINEAR_DX : 0) | (dw ? ZNNI_LINEAR_DW : 0) | (dbias ? ZNNI_LINEAR_DBIAS : 0), &need);
+    if (rc) return rc;
+    if (act != ZNNI_ACT_NONE && !z) return ZNNI_ERR_NULL;
+    if ((rc = rows_fine(dout, type, M, N, false))) return rc;
+    if (act != ZNNI_ACT_NONE && (rc = rows_fine(z, type, M, N, false))) return rc;
+    if (dw && ((rc = rows_fine(x, type, M, K, false)) || (rc = rows_fine(dw, type, N, K, true)))) return rc;
+    if (dx && ((rc = rows_fine(w, type, N, K, false)) || (rc = rows_fine(dx, type, M, K, true)))) return rc;
+    if (need && !workspace) return ZNNI_ERR_NULL;
+    if ((uintptr_t)dbias % type_size(type) || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
+    if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
+    if (act == ZNNI_ACT_NONE) z = nullptr;
+    const hipStream_t st = (hipStream_t)stream;
+    switch (type) {
+        case ZNNI_F32: return backward<float>(type, M, N, K, dout, x, w, z, act, dx, dw, dbias, workspace, st);
+        case ZNNI_BF16: return backward<bf16>(type, M, N, K, dout, x, w, z, act, dx, dw, dbias, workspace, st);
+        default: return backward<f16>(type, M, N, K, dout, x, w, z, act, dx, dw, dbias, workspace, st);
+    }
+}
+
+}  // extern "C"
