@@ -196,75 +196,6 @@ znni_status znni_conv3d_fft_profile(int S, int f, int fo, int n, int k,
                                     float* stage_ms);
 
 /*
- * What makes a block of the attention, and trains it: products of tokens with weights, norms between blocks, gradients of both and
- * of windowed attention.  Conventions as above (types, statuses, streams, fp32 sums, deterministic results), and:
- *   - A matrix of tokens or weights is a znni_rows: element (row r, column c) lies at data[r * row + c], `row` in elements.  What is read may
- *     have any row stride, what is written one of at least its columns (ZNNI_ERR_SHAPE); addresses are aligned to an element
- *     (ZNNI_ERR_ALIGN).  Rows that begin at multiples of 16 bytes are read fastest.  Vectors are contiguous, of the call's type.
- *   - Outputs overlap no input, unless said otherwise.  Infinities and NaN go where the formulas take them.
- *   - Up to 2^30 rows, 2^26 columns (ZNNI_ERR_SHAPE).
- */
-typedef struct {
-    void* data;
-    long long row;
-} znni_rows;
-
-enum { ZNNI_ACT_NONE = 0, ZNNI_ACT_RELU = 1, ZNNI_ACT_GELU = 2, ZNNI_ACT_SILU = 3 };
-
-/*
- * out[m][n] = residual[m][n] + act(z[m][n]),   z[m][n] = sum_k x[m][k] w[n][k] + bias[n]
- *   x [M][K], w [N][K], bias [N] or NULL, residual [M][N] or NULL (may be out), z [M][N] or NULL: where what goes into the activation
- *   is kept for the gradients, out [M][N].  gelu(z) = z (1 + erf(z / sqrt 2)) / 2, silu(z) = z / (1 + exp(-z)).
- * Sums are fp32; z and out are rounded once (out from the z that is not).  M, N, K of zero are fine (K = 0: z is the bias).
- * The workspace (may be zero bytes: then NULL will do; 256-byte aligned) holds parts of sums that are split over workgroups.
- */
-znni_status znni_linear_workspace(int type, int M, int N, int K, size_t* bytes);
-
-znni_status znni_linear(int type, int M, int N, int K, const znni_rows* x, const znni_rows* w, const void* bias, int act,
-                        const znni_rows* residual, const znni_rows* z, const znni_rows* out, void* workspace, size_t workspace_bytes,
-                        void* stream);
-
-/*
- * Its gradients:  dz = dout act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over tokens of dz  (the residual's is dout itself).
- * dx, dw and dbias that are not wanted are NULL, and so may be what only they need (x, w); z is what the forward call kept (NULL without
- * an activation).  relu'(0) = 0.  dz is rounded to the type before the products of 16-bit types, as their operands are; dbias sums it unrounded.
- * Workspace as above; `wanted` says which of the three the call will ask for.
- */
-enum { ZNNI_LINEAR_DX = 1u, ZNNI_LINEAR_DW = 2u, ZNNI_LINEAR_DBIAS = 4u };
-
-znni_status znni_linear_backward_workspace(int type, int M, int N, int K, int act, unsigned wanted, size_t* bytes);
-
-znni_status znni_linear_backward(int type, int M, int N, int K, const znni_rows* dout, const znni_rows* x, const znni_rows* w,
-                                 const znni_rows* z, int act, const znni_rows* dx, const znni_rows* dw, void* dbias, void* workspace,
-                                 size_t workspace_bytes, void* stream);
-
-/*
- * Norms where a block ends and the next one begins, for T tokens of C channels (C <= 16384):
- *     h = x + scale * gate * u,   u = post * n(y), or y as it is without ZNNI_NORM_POST;      z = pre * n(h)   (with ZNNI_NORM_PRE)
- *     n(a) = a / sqrt(mean(a^2) + eps),   with ZNNI_NORM_CENTRED (a - mean(a)) / sqrt(var(a) + eps)
- *   x [T][C]: the stream before the block, y [T][C]: the block's result (NULL: there is no block, h is x and not written, h = NULL),
- *   gate [T][C], [C] with ZNNI_NORM_GATE_SHARED, or NULL (ones), post, pre [C] or NULL (ones), h and z [T][C]; h may be x or y.
- * z is worked out from the h that is not yet rounded.  No workspace.  ZNNI_ERR_FLAGS for arguments that a call's flags do not use.
- */
-enum { ZNNI_NORM_POST = 1u, ZNNI_NORM_PRE = 2u, ZNNI_NORM_CENTRED = 4u, ZNNI_NORM_GATE_SHARED = 8u };
-
-znni_status znni_block_norm(int type, int T, int C, const znni_rows* x, const znni_rows* y, const znni_rows* gate, const void* post, const void* pre,
-                            float scale, float eps, unsigned flags, const znni_rows* h, const znni_rows* z, void* stream);
-
-/*
- * Its gradients, from dh and dz, those of h (what the stream brings from behind; NULL: zero) and z, and from h and y as the forward call had them:
- *     dx = dh + n'(h)[pre dz],   dgate = scale dx u (summed over tokens if the gate is shared),   dy = n'(y)[scale dx gate post],
- *     dpost = sum over tokens of scale dx gate n(y),   dpre = sum over tokens of dz n(h)
- * What is not wanted is NULL.  dx may be dh, dy may be y.  The workspace is needed for sums over tokens alone (dpost, dpre, a shared gate's).
- */
-znni_status znni_block_norm_backward_workspace(int type, int T, int C, unsigned flags, size_t* bytes);
-
-znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh, const znni_rows* dz, const znni_rows* h, const znni_rows* y,
-                                     const znni_rows* gate, const void* post, const void* pre, float scale, float eps, unsigned flags,
-                                     const znni_rows* dx, const znni_rows* dy, const znni_rows* dgate, void* dpost, void* dpre, void* workspace,
-                                     size_t workspace_bytes, void* stream);
-
-/*
  * Measurement aid (host only): the work the method itself has to do in each stage of a layer call with these
  * flags, by the route that the call would take through whole planes.  hbm_bytes[s] = bytes stage s must read plus write once (its input
  * and output tensors, unpadded); flops[s] = floating-point operations of the contraction in the
@@ -466,6 +397,14 @@ znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_
                              const znni_heads* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The same, and of each row what the gradients need, stats [cu_q[B]][Hq][2] (8-byte aligned; NULL: not kept): a reference r near the
+ * row's largest sign(scale) q.k, and the sum of exp(|scale| (sign(scale) q.k - r)) over the keys that it sees (0 where it sees none).
+ */
+znni_status znni_attn_window_stats(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                                   const int* cu_q, const int* cu_k, int max_q, int max_k, int left, int right, int sinks, float scale,
+                                   const znni_heads* out, float* stats, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The 8-bit cache of keys and values.  Tokens of a sequence lie in pages of ZNNI_KV8_PAGE; table [B][width] (device) names
  * the pages of each sequence in order.  A page holds e4m3 codes (4 exponent, 3 mantissa bits, largest 448), a value is
  * code * scale, one power of two as scale for the keys and one for the values of a page and head:
@@ -500,6 +439,93 @@ znni_status znni_kv8_attn(int type, int B, int Lq, int Hq, int Hk, int D, const 
                           const unsigned char* vcodes, const float* scales, int pages, const int* table, int width,
                           const int* lens, int max_len, int left, int sinks, float scale, const znni_heads* out, void* workspace,
                           size_t workspace_bytes, void* stream);
+
+/*
+ * What makes a block of the attention, and trains it: products of tokens with weights, norms between blocks, gradients of both and
+ * of windowed attention.  Conventions as above (types, statuses, streams, fp32 sums, deterministic results), and:
+ *   - A matrix of tokens or weights is a znni_rows: element (row r, column c) lies at data[r * row + c], `row` in elements.  What is read may
+ *     have any row stride, what is written one of at least its columns (ZNNI_ERR_SHAPE); addresses are aligned to an element
+ *     (ZNNI_ERR_ALIGN).  Rows that begin at multiples of 16 bytes are read fastest.  Vectors are contiguous, of the call's type.
+ *   - Outputs overlap no input, unless said otherwise.  Infinities and NaN go where the formulas take them.
+ *   - Up to 2^30 rows, 2^26 columns (ZNNI_ERR_SHAPE).
+ */
+typedef struct {
+    void* data;
+    long long row;
+} znni_rows;
+
+enum { ZNNI_ACT_NONE = 0, ZNNI_ACT_RELU = 1, ZNNI_ACT_GELU = 2, ZNNI_ACT_SILU = 3 };
+
+/*
+ * out[m][n] = residual[m][n] + act(z[m][n]),   z[m][n] = sum_k x[m][k] w[n][k] + bias[n]
+ *   x [M][K], w [N][K], bias [N] or NULL, residual [M][N] or NULL (may be out), z [M][N] or NULL: where what goes into the activation
+ *   is kept for the gradients, out [M][N].  gelu(z) = z (1 + erf(z / sqrt 2)) / 2, silu(z) = z / (1 + exp(-z)).
+ * Sums are fp32; z and out are rounded once (out from the z that is not).  M, N, K of zero are fine (K = 0: z is the bias).
+ * The workspace (may be zero bytes: then NULL will do; 256-byte aligned) holds parts of sums that are split over workgroups.
+ */
+znni_status znni_linear_workspace(int type, int M, int N, int K, size_t* bytes);
+
+znni_status znni_linear(int type, int M, int N, int K, const znni_rows* x, const znni_rows* w, const void* bias, int act,
+                        const znni_rows* residual, const znni_rows* z, const znni_rows* out, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
+ * Its gradients:  dz = dout act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over tokens of dz  (the residual's is dout itself).
+ * dx, dw and dbias that are not wanted are NULL, and so may be what only they need (x, w); z is what the forward call kept (NULL without
+ * an activation).  relu'(0) = 0.  dz is rounded to the type before the products of 16-bit types, as their operands are; dbias sums it unrounded.
+ * Workspace as above; `wanted` says which of the three the call will ask for.
+ */
+enum { ZNNI_LINEAR_DX = 1u, ZNNI_LINEAR_DW = 2u, ZNNI_LINEAR_DBIAS = 4u };
+
+znni_status znni_linear_backward_workspace(int type, int M, int N, int K, int act, unsigned wanted, size_t* bytes);
+
+znni_status znni_linear_backward(int type, int M, int N, int K, const znni_rows* dout, const znni_rows* x, const znni_rows* w,
+                                 const znni_rows* z, int act, const znni_rows* dx, const znni_rows* dw, void* dbias, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Norms where a block ends and the next one begins, for T tokens of C channels (C <= 16384):
+ *     h = x + scale * gate * u,   u = post * n(y), or y as it is without ZNNI_NORM_POST;      z = pre * n(h)   (with ZNNI_NORM_PRE)
+ *     n(a) = a / sqrt(mean(a^2) + eps),   with ZNNI_NORM_CENTRED (a - mean(a)) / sqrt(var(a) + eps)
+ *   x [T][C]: the stream before the block, y [T][C]: the block's result (NULL: there is no block, h is x and not written, h = NULL),
+ *   gate [T][C], [C] with ZNNI_NORM_GATE_SHARED, or NULL (ones), post, pre [C] or NULL (ones), h and z [T][C]; h may be x or y.
+ * z is worked out from the h that is not yet rounded.  No workspace.  ZNNI_ERR_FLAGS for arguments that a call's flags do not use.
+ */
+enum { ZNNI_NORM_POST = 1u, ZNNI_NORM_PRE = 2u, ZNNI_NORM_CENTRED = 4u, ZNNI_NORM_GATE_SHARED = 8u };
+
+znni_status znni_block_norm(int type, int T, int C, const znni_rows* x, const znni_rows* y, const znni_rows* gate, const void* post, const void* pre,
+                            float scale, float eps, unsigned flags, const znni_rows* h, const znni_rows* z, void* stream);
+
+/*
+ * Its gradients, from dh and dz, those of h (what the stream brings from behind; NULL: zero) and z, and from h and y as the forward call had them:
+ *     dx = dh + n'(h)[pre dz],   dgate = scale dx u (summed over tokens if the gate is shared),   dy = n'(y)[scale dx gate post],
+ *     dpost = sum over tokens of scale dx gate n(y),   dpre = sum over tokens of dz n(h)
+ * What is not wanted is NULL.  dx may be dh, dy may be y.  The workspace is needed for sums over tokens alone (dpost, dpre, a shared gate's).
+ */
+znni_status znni_block_norm_backward_workspace(int type, int T, int C, unsigned flags, size_t* bytes);
+
+znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh, const znni_rows* dz, const znni_rows* h, const znni_rows* y,
+                                     const znni_rows* gate, const void* post, const void* pre, float scale, float eps, unsigned flags,
+                                     const znni_rows* dx, const znni_rows* dy, const znni_rows* dgate, void* dpost, void* dpre, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of windowed attention from its result's, dout (strided as q): dq, dk, dv.  q, k, v, out and stats are the forward call's, and so
+ * are cu_q ... scale.  With P the row's weights, dP = dout.v and delta = dout.out:  dS = P (dP - delta),  dq = scale dS k,
+ * dk = scale dS^T q,  dv = P^T dout, the last two summed over the query heads that share a key head.  Rows that see nothing have
+ * gradients of zero, and so have keys that nothing sees.  What is not finite makes gradients that it enters not finite, and no others: a row's
+ * q and dout those of what it sees, a key's k and v those of the rows that see it.
+ * 16-bit types: P and dS are rounded to the type (fp16: scaled by powers of two, so that its range is none of theirs) before their
+ * last product; sums stay fp32.  Tokens past max_q and keys past max_k, and those behind the last sequence, are not written.
+ * max_q * Hq / Hk and max_k up to 2^31 - 257.  Workspace as for znni_attn_window, never of zero bytes.
+ */
+znni_status znni_attn_window_backward_workspace(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks,
+                                                size_t* bytes);
+
+znni_status znni_attn_window_backward(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                                      const znni_heads* out, const float* stats, const znni_heads* dout, const int* cu_q, const int* cu_k,
+                                      int max_q, int max_k, int left, int right, int sinks, float scale, const znni_heads* dq,
+                                      const znni_heads* dk, const znni_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid: a plain device-to-device copy of `bytes` bytes (a multiple of 16; both pointers 16-byte

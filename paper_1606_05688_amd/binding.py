@@ -26,7 +26,8 @@ EXPORTS = ("znni_version", "znni_status_string", "znni_fft_size", "znni_conv3d_f
            "znni_conv3d_fft", "znni_conv3d_fft_profile", "znni_conv3d_fft_workspace_v", "znni_conv3d_fft_v",
            "znni_conv3d_fft_profile_v", "znni_conv3d_fft_static_v", "znni_conv3d_fft_stage_work_v", "znni_conv3d_fft_call_work_v", "znni_conv3d_fft_sublayers_v", "znni_conv3d_fft_budget_v", "znni_conv3d_direct_workspace_v", "znni_conv3d_direct_v", "znni_conv3d_choose_v", "znni_conv3d_workspace_v", "znni_conv3d_v", "znni_mpf", "znni_maxpool",
            "znni_copy_probe", "znni_rope_axes", "znni_attn_window_workspace", "znni_attn_window", "znni_kv8_append",
-           "znni_kv8_attn_workspace", "znni_kv8_attn", "znni_linear_workspace", "znni_linear", "znni_linear_backward_workspace",
+           "znni_kv8_attn_workspace", "znni_kv8_attn", "znni_attn_window_stats", "znni_attn_window_backward_workspace",
+           "znni_attn_window_backward", "znni_linear_workspace", "znni_linear", "znni_linear_backward_workspace",
            "znni_linear_backward", "znni_block_norm", "znni_block_norm_backward_workspace", "znni_block_norm_backward")
 
 F32, BF16, F16 = 0, 1, 2
@@ -110,6 +111,12 @@ def lib():
         L.znni_kv8_attn_workspace.argtypes = [i] * 9 + [ctypes.POINTER(sz)]
         L.znni_kv8_attn.restype = i
         L.znni_kv8_attn.argtypes = [i, i, i, i, i, i, hp, vp, vp, vp, i, vp, i, vp, i, i, i, ctypes.c_float, hp, vp, sz, vp]
+        L.znni_attn_window_stats.restype = i
+        L.znni_attn_window_stats.argtypes = [i, i, i, i, i, hp, hp, hp, vp, vp, i, i, i, i, i, ctypes.c_float, hp, vp, vp, sz, vp]
+        L.znni_attn_window_backward_workspace.restype = i
+        L.znni_attn_window_backward_workspace.argtypes = [i] * 10 + [ctypes.POINTER(sz)]
+        L.znni_attn_window_backward.restype = i
+        L.znni_attn_window_backward.argtypes = [i, i, i, i, i, hp, hp, hp, hp, vp, hp, vp, vp, i, i, i, i, i, ctypes.c_float, hp, hp, hp, vp, sz, vp]
         rp, szp, fl = vp, ctypes.POINTER(sz), ctypes.c_float               # znni_rows *: bytes that hold one
         L.znni_linear_workspace.restype = i
         L.znni_linear_workspace.argtypes = [i, i, i, i, szp]
@@ -479,12 +486,13 @@ def znni_attn_window_workspace(dtype, B, Hq, Hk, D, max_q, max_k, left=None, rig
 
 
 def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sinks=0, scale=None, out=None, workspace=None,
-                     stream=None):
+                     stream=None, stats=None):
     """Attention over B sequences one behind the other: q [Tq, Hq, D], k and v [Tk, Hk, D], cu_q and cu_k int32 [B + 1] their
     starts.  The last query of a sequence stands at its last key; a row at position p sees keys p - left .. p + right (None:
-    without an end) and, up to p + right, the first `sinks` keys.  Rows that see nothing are zero.  scale: D ** -0.5."""
+    without an end) and, up to p + right, the first `sinks` keys.  Rows that see nothing are zero.  scale: D ** -0.5.
+    stats: True returns (out, stats), float32 [Tq, Hq, 2], which the gradients need (or the tensor to put them in)."""
     if stream is not None:
-        return _on(stream, q, znni_attn_window, q, k, v, cu_q, cu_k, max_q, max_k, left, right, sinks, scale, out, workspace)
+        return _on(stream, q, znni_attn_window, q, k, v, cu_q, cu_k, max_q, max_k, left, right, sinks, scale, out, workspace, None, stats)
     Tq, Hq, D = q.shape
     Tk, Hk, _ = k.shape
     B = cu_q.numel() - 1
@@ -494,10 +502,54 @@ def znni_attn_window(q, k, v, cu_q, cu_k, max_q, max_k, left=None, right=0, sink
     kind = _kind(q)
     out, do = _result(q, out, q.shape, kind)
     w, n, held = _scratch(_attn_window_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
-    _check(lib().znni_attn_window(kind[0], B, Hq, Hk, D, _heads(q, q.shape, kind), _heads(k, k.shape, kind), _heads(v, k.shape, kind),
-                                  _ints(cu_q, kind, B + 1), _ints(cu_k, kind, B + 1), max_q, max_k, left, right, sinks,
-                                  D ** -0.5 if scale is None else scale, do, w, n, _current(q)))
-    return out
+    args = (kind[0], B, Hq, Hk, D, _heads(q, q.shape, kind), _heads(k, k.shape, kind), _heads(v, k.shape, kind), _ints(cu_q, kind, B + 1),
+            _ints(cu_k, kind, B + 1), max_q, max_k, left, right, sinks, D ** -0.5 if scale is None else scale, do)
+    if stats is None:
+        _check(lib().znni_attn_window(*args, w, n, _current(q)))
+        return out
+    stats = torch.empty((Tq, Hq, 2), dtype=torch.float32, device=q.device) if stats is True else stats
+    _check(lib().znni_attn_window_stats(*args, _stats(stats, Tq, Hq, kind), w, n, _current(q)))
+    return out, stats
+
+
+def _stats(stats, Tq, Hq, kind):
+    assert stats.shape == (Tq, Hq, 2) and stats.dtype == torch.float32 and stats.get_device() == kind[2] and stats.is_contiguous(), \
+        f"need contiguous float32 statistics {(Tq, Hq, 2)} on GPU {kind[2]}"
+    return stats.data_ptr()
+
+
+def _attn_window_backward_need(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks):
+    b = ctypes.c_size_t(0)
+    _check(lib().znni_attn_window_backward_workspace(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks, _byref(b)))
+    return b.value
+
+
+def znni_attn_window_backward_workspace(dtype, B, Hq, Hk, D, max_q, max_k, left=None, right=0, sinks=0):
+    return _attn_window_backward_need(_TYPES[dtype], int(B), int(Hq), int(Hk), int(D), int(max_q), int(max_k), _window(left), _window(right), int(sinks))
+
+
+def znni_attn_window_backward(dout, q, k, v, out, stats, cu_q, cu_k, max_q, max_k, left=None, right=0, sinks=0, scale=None, dq=None, dk=None,
+                              dv=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dv) of znni_attn_window from its result's, dout; out and stats are what that call gave (stats=True), all else as it had it."""
+    if stream is not None:
+        return _on(stream, q, znni_attn_window_backward, dout, q, k, v, out, stats, cu_q, cu_k, max_q, max_k, left, right, sinks, scale, dq, dk, dv,
+                   workspace)
+    Tq, Hq, D = shape = q.shape
+    Tk, Hk, _ = kshape = k.shape
+    B = cu_q.numel() - 1
+    assert v.shape == kshape and kshape[2] == D
+    left, right, sinks = _window(left), _window(right), int(sinks)
+    max_q, max_k = int(max_q) if Tq else 0, int(max_k) if Tk else 0          # tensors of no tokens have no address
+    kind = _kind(q)
+    dq, do_q = _result(q, dq, shape, kind)
+    dk, do_k = _result(k, dk, kshape, kind)
+    dv, do_v = _result(v, dv, kshape, kind)
+    w, n, held = _scratch(_attn_window_backward_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
+    _check(lib().znni_attn_window_backward(kind[0], B, Hq, Hk, D, _heads(q, shape, kind), _heads(k, kshape, kind), _heads(v, kshape, kind),
+                                           _heads(out, shape, kind), _stats(stats, Tq, Hq, kind), _heads(dout, shape, kind), _ints(cu_q, kind, B + 1),
+                                           _ints(cu_k, kind, B + 1), max_q, max_k, left, right, sinks, D ** -0.5 if scale is None else scale,
+                                           do_q, do_k, do_v, w, n, _current(q)))
+    return dq, dk, dv
 
 
 def kv8_alloc(pages, Hk, D, device="cuda"):

@@ -1,0 +1,706 @@
+// attn_back.hip -- gradients of windowed attention: the weights are worked out again from the scores and each row's statistics.
+//
+//   P = exp(scale q.k - lse),  dP = dout.v,  delta = sum over d of dout out,  dS = P (dP - delta)
+//   dv = P^T dout,  dk = scale dS^T q  (sums over the rows, of all query heads that share the key head),  dq = scale dS k
+//
+// Two kernels of one pattern: a workgroup holds 128 keys (or rows) as operands in registers, 32 a wave, and walks the rows (or keys) that
+// see them (or that they see) in tiles through LDS, so that every sum has one owner and one order.  Per 32 x 32 pairs, `loop` the walked side:
+//   S [loop][lane] = A a,  dP [loop][lane] = B b     (A, B: q and dout, or k and v, from LDS; a, b: k and v, or q and dout)
+//   dA^T [D][lane] += A^T dS,  for keys also dB^T [D][lane] += B^T P     (P and dS as they stand are right operands; A^T, B^T by transposing reads)
+// Accumulators start from what is subtracted: S from -(the row's reference), dP from -delta.
+#include <type_traits>
+
+#include "attn_tile.h"
+
+namespace znni {
+
+constexpr int BACK_THREADS = 256, BACK_LANES = 128;      // keys (or rows) of a workgroup
+
+struct BackArgs {
+    int Hq, Hk, D;
+    const int* cu_q;
+    const int* cu_k;
+    Window w;
+    float scale;
+    int max_q, max_k;
+    int tiles, splits;                // tiles of keys (or rows) of a sequence, workgroups that share a tile's walk
+    int far_tiles, far;               // of keys: tiles that hold first tokens, workgroups that walk the rows past a tile's window
+    long long groups;
+    long long pitch;                  // rows of a sequence and key head in `rows`
+    const float* rows;                // [3][B * Hk][pitch]: minus the reference, minus delta, log2 of the sum
+    long long all_rows;               // B * Hk * pitch
+    const unsigned* peaks;            // fp16: largest magnitudes of dout and v (bits of an fp32 number)
+    float* parts;
+};
+
+// fp16 has no room for weights of long rows (2^-14 is its least normal number) nor for gradients of any size: P goes into its product times 2^15,
+// dS times a power of two for which |dout.v - delta| <= 2 D max|dout| max|v| stays below 2^15.  Other types have the range of fp32.
+constexpr int WEIGHT_POWER = 15;
+__device__ inline int slope_power(const BackArgs& a)
+{
+    const float most = __uint_as_float(a.peaks[0]) * __uint_as_float(a.peaks[1]) * (float)a.D;
+    return most > 0.f ? WEIGHT_POWER - 2 - ilogbf(most) : 0;
+}
+
+__global__ void k_back_clear(unsigned* peaks)
+{
+    if (threadIdx.x < 2) peaks[threadIdx.x] = 0;
+}
+
+// The largest finite magnitude of a workgroup's values into a peak (a maximum has no order).
+__device__ inline void raise_peak(unsigned* peak, float most)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(peak, __float_as_uint(most));
+}
+__device__ inline float finite_size(float x) { return fabsf(x) <= 65504.f ? fabsf(x) : 0.f; }
+
+__global__ __launch_bounds__(256) void k_back_peak(BackArgs a, int B, Heads<const f16> v, unsigned* peaks)
+{
+    typedef f16 V __attribute__((ext_vector_type(8)));
+    const int b = blockIdx.y, k0 = a.cu_k[b], nk = min(a.cu_k[b + 1] - k0, a.max_k), chunks = a.D / 8;
+    float most = 0.f;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)nk * a.Hk * chunks; i += (long long)gridDim.x * 256) {
+        const long long row = i / chunks;
+        const V x = *(const V*)(v.row(k0 + row / a.Hk, (int)(row % a.Hk)) + i % chunks * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size((float)x[e]));
+    }
+    raise_peak(peaks + 1, most);
+}
+
+// What a score is multiplied by to count powers of two; of a scale of 0 the least there is (as in the forward kernel).
+__host__ __device__ inline float back_powers(float scale) { return scale == 0.f ? 0x1p-149f : fabsf(scale) * 1.44269504088896340736f; }
+
+__device__ inline unsigned low_bits(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
+
+// ---- of every row: delta and its statistics --------------------------------------------------------------------------
+
+// Sixteen lanes a row, 16 bytes a lane at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, int B, Heads<const T> dout, Heads<const T> out, const float2* __restrict__ stats,
+                                                   float* __restrict__ rows)
+{
+    constexpr int EC = 16 / sizeof(T);
+    typedef T V __attribute__((ext_vector_type(EC)));
+    const int G = a.Hq / a.Hk, l = threadIdx.x & 15;
+    const long long id = group_id() * 16 + (threadIdx.x >> 4);
+    const long long r = id % a.pitch, bh = id / a.pitch;
+    const int b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
+    constexpr bool F16 = std::is_same<T, f16>::value;
+    const int q0 = b < B ? a.cu_q[b] : 0, nq = b < B ? min(a.cu_q[b + 1] - q0, a.max_q) : 0;
+    float s = 0.f, most = 0.f;
+    const long long token = q0 + r / G;
+    const int head = hk * G + (int)(r % G);
+    const bool there = r < (long long)nq * G;
+    if (there)
+        for (int d = l * EC; d < a.D; d += 16 * EC) {
+            const V x = *(const V*)(dout.row(token, head) + d), y = *(const V*)(out.row(token, head) + d);
+#pragma unroll
+            for (int e = 0; e < EC; ++e) {
+                s += (float)x[e] * (float)y[e];
+                if constexpr (F16) most = fmaxf(most, finite_size((float)x[e]));
+            }
+        }
+#pragma unroll
+    for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o);
+    if constexpr (F16) raise_peak((unsigned*)a.peaks, most);
+    if (l || !there) return;
+    const float2 st = stats[token * a.Hq + head];
+    // (a row without weights: none whatever the scores)
+    rows[id] = st.y == 0.f ? 0.f : -st.x;
+    rows[a.all_rows + id] = -s;
+    rows[2 * a.all_rows + id] = st.y == 0.f ? INFINITY : log2f(st.y) - (F16 ? WEIGHT_POWER : 0);
+}
+
+// ---- tiles of the walk ------------------------------------------------------------------------------------------------
+
+template <typename T, int NC>
+struct BackTile {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int RT = F32 ? 32 : 64;                       // rows (or keys)
+    static constexpr int EC = 16 / sizeof(T);
+    static constexpr int RS = NC == 3 ? 128 : 32 * NC;             // elements of a row in LDS
+    static constexpr int CR = RS / EC;
+    static constexpr int PER = RT * CR / BACK_THREADS;             // chunks a thread brings of a tensor
+    static constexpr int BYTES = RT * RS * sizeof(T);
+    // Chunk c of row j lies at c ^ swizzle(j).  Every tile is read both ways: one chunk of 32 rows (16 consecutive rows get different
+    // places), and transposed, 16-bit: four rows, 64 bytes each, fp32: two rows four apart, 128 bytes each.
+    __device__ static constexpr int swizzle(int j)
+    {
+        if (F32) return CR >= 16 ? (j >> 2 & 1) << 3 | (j >> 3 & 1) << 2 | (j & 3) : j >> 1 & 7;
+        return CR == 16 ? (j & 3) << 2 | (j >> 2 & 3) : CR == 8 ? (j >> 1 & 1) << 2 | (j >> 2 & 3) : j >> 2 & 3;
+    }
+};
+
+template <typename T>
+__device__ inline bool finite_of(T x)
+{
+    if constexpr (sizeof(T) == 4) return fabsf(x) <= 3.402823466e38f;
+    else {
+        const unsigned short all = std::is_same<T, bf16>::value ? 0x7f80 : 0x7c00;
+        return (__builtin_bit_cast(unsigned short, x) & all) != all;
+    }
+}
+
+// KEYS: lanes are keys, the walk is over rows; else lanes are rows, the walk is over keys.
+template <typename T, int NC, bool KEYS>
+__global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(BackArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+                                                                              Heads<const T> dout, Heads<T> da, Heads<T> db)
+{
+    using G = BackTile<T, NC>;
+    using M = Mfma<T>;
+    constexpr bool F32 = G::F32;
+    constexpr int RT = G::RT, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER, QS = F32 ? 4 * NC : 2 * NC;
+    __shared__ __align__(1024) char as[2][G::BYTES];
+    __shared__ __align__(1024) char bs[2][G::BYTES];
+    __shared__ __align__(1024) float rc[2][3 * RT];                 // of the rows walked: minus the reference, minus delta, log2 of the sum
+
+    const long long group = group_id();
+    if (group >= a.groups) return;
+    const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
+    const int shared = a.Hq / a.Hk, per_head = a.tiles * a.splits + a.far_tiles * a.far;
+    const long long bh = group / per_head;
+    const int slot = (int)(group % per_head), b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
+    const bool far = KEYS && slot >= a.tiles * a.splits;
+    const int tile = far ? (slot - a.tiles * a.splits) / a.far : KEYS ? slot / a.splits : a.tiles - 1 - slot / a.splits;
+    const int split = far ? (slot - a.tiles * a.splits) % a.far : slot % a.splits, splits = far ? a.far : a.splits;
+    const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q), all_q = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
+    const long long base = (long long)nk - all_q;                   // position of the first row's token
+    const int rows = nq * shared;                                    // (fits: checked by the host)
+    const int x0 = tile * BACK_LANES, count = KEYS ? min(nk, a.max_k) : rows;       // of keys (or rows)
+    if (x0 >= count) return;
+    const int wx0 = x0 + 32 * wave, mine = min(wx0 + c32, count - 1), last = min(x0 + BACK_LANES, count) - 1, wlast = min(wx0 + 32, count) - 1;
+
+    // rows that see key j: from, up to (the window's, or all if it is one of the first)
+    auto row_of = [&](long long p) {                                 // the first row at position p or behind it
+        const long long y = (p - base) * shared;
+        return y < 0 ? 0 : y > rows ? rows : (int)y;
+    };
+    auto from_row = [&](int j) { return row_of((long long)j - a.w.right); };
+    auto window_end = [&](int j) { return row_of((long long)j + a.w.left + 1); };
+    auto to_row = [&](int j) { return j < a.w.sinks ? rows : window_end(j); };
+    int lo = 0, hi = 0;                                              // of the lane: rows lo .. hi - 1, or keys lo .. hi
+    const long long pos = base + mine / shared;
+    if (KEYS) {
+        lo = from_row(mine);
+        hi = to_row(mine);
+    } else {
+        window_of(pos, nk, a.w, &lo, &hi);
+    }
+    const Sight all_rows(base + x0 / shared, base + last / shared, nk, a.w);
+    const Sight wave_rows(base + wx0 / shared, base + (wx0 < count ? wlast / shared : wx0 / shared - 1), nk, a.w);
+    // of the wave, where lanes are keys: some key is seen by rows any0 .. any1 - 1, all are by all0 .. all1 - 1
+    int any0 = 0, any1 = 0, all0 = 0, all1 = 0;
+    if (KEYS && wx0 < count) {
+        any0 = from_row(wx0);
+        any1 = wx0 < a.w.sinks ? rows : window_end(wlast);
+        all0 = from_row(wlast);
+        all1 = wlast < a.w.sinks ? rows : window_end(max(wx0, a.w.sinks));
+    }
+    auto any = [&](int i) { return KEYS ? i < any1 && i + 32 > any0 : wave_rows.any(i, 32); };
+    auto all = [&](int i) { return KEYS ? i >= all0 && i + 32 <= all1 : wave_rows.all(i, 32); };
+    // bits of the 32 walked from i on that the lane's pair sees
+    auto sight = [&](int i) {
+        return KEYS ? low_bits(hi - i) & ~low_bits(lo - i) : low_bits(hi + 1 - i) & (~low_bits(lo - i) | low_bits(a.w.sinks - i));
+    };
+
+    // tiles of the walk
+    const KeyTiles<RT> keys(all_rows);
+    int first = 0, n = keys.n;
+    if (KEYS) {
+        const int r1 = window_end(last), r0 = far ? r1 : from_row(x0), end = far ? rows : r1;
+        first = r0 / RT;
+        // (a far walk begins in the tile in which the window's has ended, and the rows that the window had are masked)
+        n = end > r0 ? (end + RT - 1) / RT - first : 0;
+        if (far) lo = max(lo, r1), any0 = max(any0, r1), all0 = max(all0, r1);
+        else hi = min(hi, r1), any1 = min(any1, r1), all1 = min(all1, r1);
+    }
+    const int per = (n + splits - 1) / splits, begin = split * per, stop = min(n, begin + per);
+    auto at = [&](int it) { return KEYS ? (first + it) * RT : keys.base(it); };
+    const int walked = KEYS ? rows : nk;
+
+    const Heads<const T> A = KEYS ? q : k, B = KEYS ? dout : v;
+    const T* const ap = KEYS ? A.row(q0, hk * shared) : A.row(k0, hk);
+    const T* const bp = KEYS ? B.row(q0, hk * shared) : B.row(k0, hk);
+    const long long arows = a.pitch * bh;
+    auto element = [&](const Heads<const T>& x, int r) { return KEYS ? r / shared * x.token + r % shared * x.head : r * x.token; };
+    // offsets of 32 bits from a tile's first row on
+    auto near = [&](const Heads<const T>& x) { return x.token >= 0 && x.token < 1 << 22 && (!KEYS || (x.head >= 0 && x.head < 1 << 22)); };
+    const bool plain = near(A) && near(B) && a.D == RS && (!KEYS || RT % shared == 0);
+    unsigned ao[PER], bo[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = i * BACK_THREADS + t, j = s / CR, c = (s % CR ^ G::swizzle(j)) * EC;
+        ao[i] = (unsigned)(element(A, j) + c) * (unsigned)sizeof(T);
+        bo[i] = (unsigned)(element(B, j) + c) * (unsigned)sizeof(T);
+    }
+    const unsigned a_lds = lds_address(as) + wave * 1024, b_lds = lds_address(bs) + wave * 1024;
+    auto bring = [&](int it) {
+        const int buf = (it - begin) & 1, i0 = at(it);
+        if (KEYS && t < 3 * RT / 4) {
+            const int c = t / (RT / 4);
+            to_lds(a.rows + c * a.all_rows + arows + i0 + (t - c * (RT / 4)) * 4, lds_address(rc[buf]));
+        }
+        if (plain && i0 + RT <= walked) {
+            const T* const a0 = ap + element(A, i0);
+            const T* const b0 = bp + element(B, i0);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                to_lds(a0, ao[i], a_lds + buf * G::BYTES + i * 4096);
+                to_lds(b0, bo[i], b_lds + buf * G::BYTES + i * 4096);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int s = i * BACK_THREADS + t, j = s / CR, c = (s % CR ^ G::swizzle(j)) * EC, r = min(i0 + j, walked - 1);
+            if (c < a.D) {
+                to_lds(ap + element(A, r) + c, a_lds + buf * G::BYTES + i * 4096);
+                to_lds(bp + element(B, r) + c, b_lds + buf * G::BYTES + i * 4096);
+            }
+        }
+    };
+    // chunks past a head's end are never brought: zero
+    if (a.D < RS)
+        for (int i = t; i < 2 * RT * CR; i += BACK_THREADS) {
+            const int s = i % (RT * CR), j = s / CR;
+            if ((s % CR ^ G::swizzle(j)) * EC >= a.D) {
+                *(uint4*)(as[i / (RT * CR)] + s * 16) = make_uint4(0, 0, 0, 0);
+                *(uint4*)(bs[i / (RT * CR)] + s * 16) = make_uint4(0, 0, 0, 0);
+            }
+        }
+    if (begin < stop) bring(begin);
+
+    // the lanes' own operands
+    typename M::V af[QS], bf[QS];
+    {
+        const T* const x = KEYS ? k.row(k0 + mine, hk) : q.row(q0 + mine / shared, hk * shared + mine % shared);
+        const T* const y = KEYS ? v.row(k0 + mine, hk) : dout.row(q0 + mine / shared, hk * shared + mine % shared);
+#pragma unroll
+        for (int c = 0; c < QS; ++c) {
+            const int d = (2 * c + h) * EC;
+            if (d < a.D) {
+                af[c] = *(const typename M::V*)(x + d);
+                bf[c] = *(const typename M::V*)(y + d);
+            } else {
+#pragma unroll
+                for (int e = 0; e < EC; ++e) af[c][e] = bf[c][e] = (T)0.f;
+            }
+            // a negative scale turns the scores, as in the forward kernel
+            if (a.scale < 0.f)
+#pragma unroll
+                for (int e = 0; e < EC; ++e) af[c][e] = -af[c][e];
+        }
+    }
+    float own0 = 0.f, own1 = 0.f, own2 = 0.f;
+    if (!KEYS) {
+        own0 = a.rows[arows + mine];
+        own1 = a.rows[a.all_rows + arows + mine];
+        own2 = a.rows[2 * a.all_rows + arows + mine];
+    }
+    const float by = back_powers(a.scale);
+    constexpr bool F16 = std::is_same<T, f16>::value;
+    const int power = F16 ? slope_power(a) : 0;
+    const float slope = F16 ? ldexpf(1.f, power - WEIGHT_POWER) : 1.f;
+
+    const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
+    const int k_at = (c32 * RS + (h ^ G::swizzle(c32)) * EC) * (int)sizeof(T);
+    const int v_at = F32 ? (4 * h * RS + ((c32 >> 2) ^ G::swizzle(4 * h)) * EC + (c32 & 3)) * (int)sizeof(T)
+                         : ((4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
+    // 32 elements of the head (from 32 x on) of the walked rows 16 m .. 16 m + 15 (fp32: row 8 (i / 4) + 4 h + i % 4 of element i)
+    auto turned = [&](const char* from, int x, int m) {
+        const char* const p = from + (v_at ^ x * 64) + 16 * m * RS * (int)sizeof(T);
+        const char* const p8 = from + (v_at ^ x * 64 ^ 32) + (16 * m + 8) * RS * (int)sizeof(T);
+        if constexpr (!F32) {
+            const typename M::V4 y0 = transposed<typename M::V4>(p), y1 = transposed<typename M::V4>(p8);
+            return __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            return (typename M::V){};
+        }
+    };
+    auto single = [&](const char* from, int x, int i) {
+        return *(const T*)(from + (v_at ^ x * 128 ^ G::swizzle(8 * (i / 4) + i % 4) * 16) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T));
+    };
+
+    f32x16 acc_a[NC], acc_b[KEYS ? NC : 1];
+#pragma unroll
+    for (int x = 0; x < NC; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            acc_a[x][i] = 0.f;
+            if (KEYS) acc_b[KEYS ? x : 0][i] = 0.f;
+        }
+    unsigned met_a[NC] = {}, met_b[NC] = {};          // elements of results that something that is not finite enters (16 bits each)
+
+    for (int it = begin; it < stop; ++it) {
+        const int buf = (it - begin) & 1, i0 = at(it);
+        wait_but_and_meet<0>();
+        if (it + 1 < stop) bring(it + 1);
+#pragma unroll
+        for (int u = 0; u < RT / 32; ++u) {
+            const int i = i0 + 32 * u;
+            if (!any(i)) continue;
+            const char* const ab = as[buf] + 32 * u * RS * sizeof(T);
+            const char* const bb = bs[buf] + 32 * u * RS * sizeof(T);
+            f32x16 s, dp;
+            float l2[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float4 x0 = make_float4(own0, own0, own0, own0), x1 = make_float4(own1, own1, own1, own1), x2 = make_float4(own2, own2, own2, own2);
+                if (KEYS) {
+                    const float* const p = rc[buf] + 32 * u + 2 * e + 4 * h;
+                    x0 = *(const float4*)p;
+                    x1 = *(const float4*)(p + RT);
+                    x2 = *(const float4*)(p + 2 * RT);
+                }
+                s[e] = x0.x; s[e + 1] = x0.y; s[e + 2] = x0.z; s[e + 3] = x0.w;
+                dp[e] = x1.x; dp[e + 1] = x1.y; dp[e + 2] = x1.z; dp[e + 3] = x1.w;
+                l2[e] = x2.x; l2[e + 1] = x2.y; l2[e + 2] = x2.z; l2[e + 3] = x2.w;
+            }
+#pragma unroll
+            for (int c = 0; c < QS; ++c) {
+                const typename M::V x = *(const typename M::V*)(ab + (k_at ^ c * 32));
+                const typename M::V y = *(const typename M::V*)(bb + (k_at ^ c * 32));
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s = M::mul(x[e], af[c][e], s);
+                        dp = M::mul(y[e], bf[c][e], dp);
+                    }
+                } else {
+                    s = M::mul(x, af[c], s);
+                    dp = M::mul(y, bf[c], dp);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], by, -l2[e]));
+                dp[e] *= F16 ? s[e] * slope : s[e];
+            }
+            const bool whole = all(i);
+            unsigned seen = ~0u;
+            if (!whole) {
+                seen = sight(i) >> 4 * h;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int m = (int)(seen << (31 - 8 * (e / 4) - e % 4)) >> 31;
+                    s[e] = __int_as_float(__float_as_int(s[e]) & m);
+                    dp[e] = __int_as_float(__float_as_int(dp[e]) & m);
+                }
+            }
+            // Pairs that do not see each other have weights of zero here, and zero times what is not finite is NaN: where there are such pairs, what
+            // is not finite counts as zero, and marks the results of those that do see it.
+            auto add = [&](f32x16* acc, const char* from, const f32x16& weight, unsigned* met) {
+                bool odd = false;
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+#pragma unroll
+                        for (int x = 0; x < NC; ++x) {
+                            T y = single(from, x, e);
+                            if (!whole && !finite_of(y)) y = 0.f, odd = true;
+                            acc[x] = M::mul(y, weight[e], acc[x]);
+                        }
+                } else {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        typename M::V w;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = (T)weight[8 * m + e];
+#pragma unroll
+                        for (int x = 0; x < NC; ++x) {
+                            typename M::V y = turned(from, x, m);
+                            if (!whole)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    if (!finite_of((T)y[e])) y[e] = (T)0.f, odd = true;
+                            acc[x] = M::mul(y, w, acc[x]);
+                        }
+                    }
+                }
+                if (whole || !__any(odd)) return;
+#pragma unroll
+                for (int x = 0; x < NC; ++x) {
+                    f32x16 kinds;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) kinds[e] = 0.f;
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            kinds = M::mul(finite_of(single(from, x, e)) ? 0.f : 1.f, (float)(seen >> (8 * (e / 4) + e % 4) & 1), kinds);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            typename M::V y = turned(from, x, m), w;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int i8 = 8 * m + e;
+                                y[e] = finite_of((T)y[e]) ? (T)0.f : (T)1.f;
+                                w[e] = (T)(float)(seen >> (8 * (i8 / 4) + i8 % 4) & 1);
+                            }
+                            kinds = M::mul(y, w, kinds);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) met[x] |= kinds[e] != 0.f ? 1u << e : 0u;
+                }
+            };
+            if constexpr (KEYS) add(acc_b, bb, s, met_b);
+            add(acc_a, ab, dp, met_a);
+            // The compiler has been seen to read a sum right behind its product, on the other side of a branch, without the 18 wait states of fp32
+            // products (one element of 16 was wrong): they are here.
+            if constexpr (F32) {
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_nop 15\n\ts_nop 1");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    if (wx0 + c32 >= count) return;
+    auto put = [&](const Heads<T>& to, f32x16* acc, const unsigned* met, float scale, int which) {
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (met[x] >> e & 1) acc[x][e] = NAN;
+                else acc[x][e] *= scale;
+            }
+        const bool parts = a.splits > 1 || (KEYS && tile < a.far_tiles);
+        T* const y = KEYS ? to.row(k0 + mine, hk) : to.row(q0 + mine / shared, hk * shared + mine % shared);
+        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones
+        const int owns = a.splits > 1 ? a.tiles * a.splits : a.far_tiles;
+        const long long part = bh * (owns + a.far_tiles * a.far) + (far ? owns + tile * a.far + split : tile * a.splits + split);
+        float* const z = a.parts + ((part * (KEYS ? 2 : 1) + which) * BACK_LANES + (mine - x0)) * a.D;
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int d = 32 * x + 2 * e + 4 * h;
+                if (d >= a.D) continue;
+                if (parts) {
+                    *(float4*)(z + d) = make_float4(acc[x][e], acc[x][e + 1], acc[x][e + 2], acc[x][e + 3]);
+                } else {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    T4 o;
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) o[f] = (T)acc[x][e + f];
+                    *(T4*)(y + d) = o;
+                }
+            }
+    };
+    put(da, acc_a, met_a, F16 ? ldexpf(a.scale, -power) : a.scale, 0);
+    if constexpr (KEYS) put(db, acc_b, met_b, F16 ? 1.f / (1 << WEIGHT_POWER) : 1.f, 1);
+}
+
+// Sums of the parts of a tile: 32 lanes a key (or row), four elements a lane.
+template <typename T, bool KEYS>
+__global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles, Heads<T> da, Heads<T> db)
+{
+    const long long id = group_id() * 8 + (threadIdx.x >> 5);
+    const int d = (threadIdx.x & 31) * 4, shared = a.Hq / a.Hk;
+    const long long across = (long long)tiles * BACK_LANES;
+    const int x = (int)(id % across), tile = x / BACK_LANES;
+    const long long bh = id / across;
+    const int b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
+    if (b >= B || d >= a.D) return;
+    const int x0 = KEYS ? a.cu_k[b] : a.cu_q[b];
+    const int count = KEYS ? min(a.cu_k[b + 1] - x0, a.max_k) : min(a.cu_q[b + 1] - x0, a.max_q) * shared;
+    if (x >= count) return;
+    const int owns = a.splits > 1 ? a.tiles * a.splits : a.far_tiles, N = KEYS ? 2 : 1;
+    const long long head = bh * (owns + a.far_tiles * a.far);
+    const int more = tile < a.far_tiles ? a.far : 0;
+#pragma unroll
+    for (int which = 0; which < N; ++which) {
+        float4 s = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < a.splits + more; ++i) {
+            const long long part = head + (i < a.splits ? tile * a.splits + i : owns + tile * a.far + i - a.splits);
+            const float4 p = *(const float4*)(a.parts + ((part * N + which) * BACK_LANES + x % BACK_LANES) * a.D + d);
+            s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
+        }
+        const Heads<T>& to = which ? db : da;
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        T* const y = KEYS ? to.row(x0 + x, hk) : to.row(x0 + x / shared, hk * shared + x % shared);
+        *(T4*)(y + d) = T4{(T)s.x, (T)s.y, (T)s.z, (T)s.w};
+    }
+}
+
+struct BackPlan {
+    int tiles, splits, far_tiles, far;
+    long long groups;
+    size_t parts;                          // elements
+};
+
+// Few tiles: workgroups share the walk until there are two for every compute unit, each with four tiles at least.
+static int back_splits(long long groups, long long walk, int rt)
+{
+    long long n = groups > 0 && groups < 512 ? 512 / groups : 1;
+    const long long most = (walk + rt - 1) / rt / 4;
+    if (n > most) n = most;
+    return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
+static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
+{
+    BackPlan p = {};
+    const int G = Hq / Hk, rt = type == ZNNI_F32 ? 32 : 64;
+    const long long count = keys ? max_k : (long long)max_q * G;
+    p.tiles = (int)((count + BACK_LANES - 1) / BACK_LANES);
+    const long long groups = (long long)p.tiles * Hk * B;
+    // what a tile walks at most, first tokens (seen by all rows that follow) apart
+    const long long wide = (long long)left + right + (keys ? BACK_LANES : BACK_LANES / G + 2);
+    long long walk;
+    if (keys) {
+        walk = (wide < max_q ? wide : max_q) * G;
+        const int lanes = sinks < max_k ? sinks : max_k;
+        // rows past the window of first tokens: as many workgroups as keep each at the length of the others
+        if (lanes > 0 && (long long)left + 1 < max_k) {
+            p.far_tiles = (lanes + BACK_LANES - 1) / BACK_LANES;
+            const long long n = ((long long)max_q + wide - 1) / wide;
+            p.far = n < 1 ? 1 : n > 64 ? 64 : (int)n;
+        }
+    } else {
+        walk = wide + sinks < max_k ? wide + sinks : max_k;
+    }
+    p.splits = back_splits(groups, walk, rt);
+    const long long per_head = (long long)p.tiles * p.splits + (long long)p.far_tiles * p.far;
+    p.groups = per_head * Hk * B;
+    const long long owns = p.splits > 1 ? (long long)p.tiles * p.splits : p.far_tiles;
+    p.parts = (size_t)(owns + (long long)p.far_tiles * p.far) * Hk * B * (keys ? 2 : 1) * BACK_LANES * D;
+    return p;
+}
+
+struct BackSizes {
+    size_t rows, parts;                    // bytes
+    long long pitch;
+};
+
+static BackSizes back_sizes(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
+{
+    BackSizes s = {};
+    s.pitch = ((long long)max_q * (Hq / Hk) + 63) / 64 * 64;
+    s.rows = 256 + ((size_t)3 * B * Hk * s.pitch * sizeof(float) + 255) & ~(size_t)255;
+    const size_t p0 = back_plan(true, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
+    const size_t p1 = back_plan(false, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
+    s.parts = (p0 > p1 ? p0 : p1) * sizeof(float);
+    return s;
+}
+
+template <typename T, bool KEYS>
+static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> dout,
+                                Heads<T> da, Heads<T> db, hipStream_t st)
+{
+    a.tiles = p.tiles;
+    a.splits = p.splits;
+    a.far_tiles = p.far_tiles;
+    a.far = p.far;
+    a.groups = p.groups;
+    if (p.groups == 0) return ZNNI_OK;
+    const dim3 grid = launch_of(p.groups), block(BACK_THREADS);
+    switch ((a.D + 31) / 32) {
+        case 1: k_back<T, 1, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+        case 2: k_back<T, 2, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+        case 3: k_back<T, 3, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+        default: k_back<T, 4, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+    }
+    if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    const int tiles = p.splits > 1 ? p.tiles : p.far_tiles;
+    if (!tiles) return ZNNI_OK;
+    k_back_join<T, KEYS><<<launch_of((long long)tiles * (BACK_LANES / 8) * a.Hk * B), dim3(256), 0, st>>>(a, B, tiles, da, db);
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+}
+
+template <typename T>
+static znni_status launch_back(BackArgs a, int type, int B, const znni_heads* q, const znni_heads* k, const znni_heads* v, const znni_heads* dout,
+                               const znni_heads* out, const float* stats, const znni_heads* dq, const znni_heads* dk, const znni_heads* dv,
+                               hipStream_t st)
+{
+    const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v), gi = heads_of<const T>(dout);
+    if (std::is_same<T, f16>::value) {
+        k_back_clear<<<dim3(1), dim3(64), 0, st>>>((unsigned*)a.peaks);
+        if (a.max_k > 0) {
+            const long long n = ((long long)a.max_k * a.Hk * (a.D / 8) + 2047) / 2048;
+            k_back_peak<<<dim3((unsigned)(n < 512 ? n : 512), (unsigned)B), dim3(256), 0, st>>>(a, B, heads_of<const f16>(v), (unsigned*)a.peaks);
+        }
+        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    }
+    if (a.max_q > 0) {
+        k_back_rows<T><<<launch_of((a.all_rows + 15) / 16), dim3(256), 0, st>>>(a, B, gi, heads_of<const T>(out), (const float2*)stats, (float*)a.rows);
+        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    }
+    const BackPlan pk = back_plan(true, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
+    const BackPlan pq = back_plan(false, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
+    const znni_status rc = launch_walks<T, true>(a, pk, B, qi, ki, vi, gi, heads_of<T>(dk), heads_of<T>(dv), st);
+    if (rc) return rc;
+    return launch_walks<T, false>(a, pq, B, qi, ki, vi, gi, heads_of<T>(dq), heads_of<T>(dq), st);
+}
+
+static znni_status back_shape(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
+{
+    if (!type_ok(type)) return ZNNI_ERR_TYPE;
+    if (B < 0 || B > 65535 || max_q < 0 || max_k < 0 || left < 0 || right < 0 || sinks < 0) return ZNNI_ERR_SHAPE;
+    const znni_status rc = heads_shape(Hq, Hk, D);
+    if (rc) return rc;
+    // (tiles' ends, a tile past the last, are 32 bits)
+    const long long rows = (long long)max_q * (Hq / Hk), most = INT_MAX - 2 * BACK_LANES;
+    if (rows > most || max_k > most) return ZNNI_ERR_SHAPE;
+    const long long tiles = ((rows > max_k ? rows : max_k) + BACK_LANES - 1) / BACK_LANES;
+    return tiles * Hk > INT_MAX / (B ? B : 1) ? ZNNI_ERR_SHAPE : ZNNI_OK;
+}
+
+}  // namespace znni
+
+using namespace znni;
+
+extern "C" {
+
+znni_status znni_attn_window_backward_workspace(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks,
+                                                size_t* bytes)
+{
+    if (!bytes) return ZNNI_ERR_NULL;
+    const znni_status rc = back_shape(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks);
+    if (rc) return rc;
+    const BackSizes s = back_sizes(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks);
+    *bytes = s.rows + s.parts;
+    return ZNNI_OK;
+}
+
+znni_status znni_attn_window_backward(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                                      const znni_heads* out, const float* stats, const znni_heads* dout, const int* cu_q, const int* cu_k,
+                                      int max_q, int max_k, int left, int right, int sinks, float scale, const znni_heads* dq,
+                                      const znni_heads* dk, const znni_heads* dv, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!q || !k || !v || !out || !dout || !dq || !dk || !dv) return ZNNI_ERR_NULL;
+    size_t need = 0;
+    const znni_status rc = znni_attn_window_backward_workspace(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks, &need);
+    if (rc) return rc;
+    if (B == 0 || (max_q == 0 && max_k == 0)) return ZNNI_OK;
+    if (max_q > 0 && (!q->data || !out->data || !dout->data || !dq->data || !stats)) return ZNNI_ERR_NULL;
+    if (max_k > 0 && (!k->data || !v->data || !dk->data || !dv->data)) return ZNNI_ERR_NULL;
+    if (!cu_q || !cu_k || (need && !workspace)) return ZNNI_ERR_NULL;
+    if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
+    if (((uintptr_t)cu_q | (uintptr_t)cu_k) & 3u || (uintptr_t)stats & 7u || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
+    for (const znni_heads* x : {q, k, v, out, dout, dq, dk, dv})
+        if (!heads_aligned(x, type)) return ZNNI_ERR_ALIGN;
+    const BackSizes s = back_sizes(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks);
+    BackArgs a = {};
+    a.Hq = Hq; a.Hk = Hk; a.D = D;
+    a.cu_q = cu_q; a.cu_k = cu_k;
+    a.w = {left, right, sinks};
+    a.scale = scale;
+    a.max_q = max_q; a.max_k = max_k;
+    a.pitch = s.pitch;
+    a.all_rows = (long long)B * Hk * s.pitch;
+    a.peaks = (const unsigned*)workspace;
+    a.rows = (const float*)workspace + 64;
+    a.parts = (float*)((char*)workspace + s.rows);
+    const hipStream_t st = (hipStream_t)stream;
+    switch (type) {
+        case ZNNI_F32: return launch_back<float>(a, type, B, q, k, v, dout, out, stats, dq, dk, dv, st);
+        case ZNNI_BF16: return launch_back<bf16>(a, type, B, q, k, v, dout, out, stats, dq, dk, dv, st);
+        default: return launch_back<f16>(a, type, B, q, k, v, dout, out, stats, dq, dk, dv, st);
+    }
+}
+
+}  // extern "C"

@@ -13,6 +13,7 @@ struct JoinArgs {
     float by;
     const float* parts;
     const float2* stats;
+    float2* keep;               // the caller's statistics of each row [token][Hq], or NULL
 };
 
 // The row, its token and head, and where its first part is; false past the sequence's end.
@@ -70,6 +71,7 @@ __global__ __launch_bounds__(256) void k_join_few(JoinArgs a, unsigned all, Head
             o.z += share_of(f, p[i].z);
             o.w += share_of(f, p[i].w);
         }
+    if (a.keep && d == 0) a.keep[r.token * a.Hq + r.head] = make_float2(z, n);
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 y = {(T)0.f, (T)0.f, (T)0.f, (T)0.f};
     if (n != 0.f) y = T4{(T)(o.x / n), (T)(o.y / n), (T)(o.z / n), (T)(o.w / n)};
@@ -115,6 +117,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a, Heads<T> out)
     __syncthreads();
     if (wave || 2 * l >= a.D) return;
     n = (sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]);
+    if (a.keep && l == 0) a.keep[r.token * a.Hq + r.head] = make_float2(z, n);
     o.x = (acc_s[0][l].x + acc_s[1][l].x) + (acc_s[2][l].x + acc_s[3][l].x);
     o.y = (acc_s[0][l].y + acc_s[1][l].y) + (acc_s[2][l].y + acc_s[3][l].y);
     typedef T T2 __attribute__((ext_vector_type(2)));

@@ -17,6 +17,7 @@ struct AttnArgs {
     int tiles, splits, tile_rows;     // row tiles of a sequence, workgroups that share a tile's keys, rows of a tile in `parts`
     float* parts;
     float2* stats;
+    float2* keep;                     // the caller's statistics of each row, or NULL
 };
 
 template <typename T, int NC, int THREADS>

@@ -439,6 +439,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
     if (a.splits == 1) {
         T* y = out.row(q0 + row / shared, qh);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.keep && h == 0 && d_part == 0) a.keep[(q0 + row / shared) * a.Hq + qh] = make_float2(top == -INFINITY ? 0.f : top, __builtin_amdgcn_exp2f(-off) * sum);
 #pragma unroll
         for (int x = 0; x < NA; ++x)
 #pragma unroll
@@ -548,7 +549,7 @@ static znni_status launch_attn(const AttnArgs& a, int B, int max_q, const AttnPl
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;
-    const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, powers_of(a.scale), a.parts, a.stats};
+    const JoinArgs j = {a.Hq, a.Hk, a.D, p.splits, p.tiles, p.tile_rows, max_q * (a.Hq / a.Hk), a.cu_q, 0, powers_of(a.scale), a.parts, a.stats, a.keep};
     return launch_join<T>(j, B, o, st);
 }
 
@@ -580,9 +581,9 @@ znni_status znni_attn_window_workspace(int type, int B, int Hq, int Hk, int D, i
     return ZNNI_OK;
 }
 
-znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
-                             const int* cu_q, const int* cu_k, int max_q, int max_k, int left, int right, int sinks, float scale,
-                             const znni_heads* out, void* workspace, size_t workspace_bytes, void* stream)
+znni_status znni_attn_window_stats(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                                   const int* cu_q, const int* cu_k, int max_q, int max_k, int left, int right, int sinks, float scale,
+                                   const znni_heads* out, float* stats, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!q || !k || !v || !out) return ZNNI_ERR_NULL;
     size_t need = 0;
@@ -591,19 +592,27 @@ znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_
     if (B == 0 || max_q == 0) return ZNNI_OK;
     if (!q->data || !out->data || (max_k > 0 && (!k->data || !v->data)) || !cu_q || !cu_k || (need && !workspace)) return ZNNI_ERR_NULL;
     if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
-    if (((uintptr_t)cu_q | (uintptr_t)cu_k) & 3u || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
+    if (((uintptr_t)cu_q | (uintptr_t)cu_k) & 3u || (uintptr_t)stats & 7u || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
     for (const znni_heads* h : {q, k, v, out})
         if (!heads_aligned(h, type)) return ZNNI_ERR_ALIGN;
     const AttnPlan p = attn_plan(type, B, Hq, Hk, max_q, max_k, left, right, sinks);
     float* parts = (float*)workspace;
     const AttnArgs a = {Hq, Hk, D, cu_q, cu_k, {left, right, sinks}, scale, (int)(p.groups * p.splits), max_q, p.tiles, p.splits, p.tile_rows, parts,
-                        (float2*)(parts + p.rows * D)};
+                        (float2*)(parts + p.rows * D), (float2*)stats};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
         case ZNNI_F32: return launch_attn<float>(a, B, max_q, p, q, k, v, out, st);
         case ZNNI_BF16: return launch_attn<bf16>(a, B, max_q, p, q, k, v, out, st);
         default: return launch_attn<f16>(a, B, max_q, p, q, k, v, out, st);
     }
+}
+
+znni_status znni_attn_window(int type, int B, int Hq, int Hk, int D, const znni_heads* q, const znni_heads* k, const znni_heads* v,
+                             const int* cu_q, const int* cu_k, int max_q, int max_k, int left, int right, int sinks, float scale,
+                             const znni_heads* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return znni_attn_window_stats(type, B, Hq, Hk, D, q, k, v, cu_q, cu_k, max_q, max_k, left, right, sinks, scale, out, nullptr, workspace,
+                                  workspace_bytes, stream);
 }
 
 }  // extern "C"
