@@ -24,7 +24,8 @@ struct BackArgs {
     float scale;
     int max_q, max_k;
     int tiles, splits;                // tiles of keys (or rows) of a sequence, workgroups that share a tile's walk
-    int far_tiles, far;               // of keys: tiles that hold first tokens, workgroups that walk the rows past a tile's window
+    int first_tiles;                  // of keys: tiles that hold first tokens, which rows past their window see too:
+    int far_tiles, far;               // 32 keys at a time, so many workgroups that walk those rows
     long long groups;
     long long pitch;                  // rows of a sequence and key head in `rows`
     const float* rows;                // [3][B * Hk][pitch]: minus the reference, minus delta, log2 of the sum
@@ -50,9 +51,14 @@ __global__ void k_back_clear(unsigned* peaks)
 // The largest finite magnitude of a workgroup's values into a peak (a maximum has no order).
 __device__ inline void raise_peak(unsigned* peak, float most)
 {
+    __shared__ float waves[4];
 #pragma unroll
     for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    if ((threadIdx.x & 63) == 0 && most > 0.f) atomicMax(peak, __float_as_uint(most));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x) return;
+    const unsigned y = __float_as_uint(fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3])));
+    if (y > __hip_atomic_load(peak, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(peak, y);
 }
 __device__ inline float finite_size(float x) { return fabsf(x) <= 65504.f ? fabsf(x) : 0.f; }
 
@@ -144,11 +150,15 @@ __device__ inline bool finite_of(T x)
     }
 }
 
-// KEYS: lanes are keys, the walk is over rows; else lanes are rows, the walk is over keys.
-template <typename T, int NC, bool KEYS>
+// What a kernel makes.  Rows: dq.  Keys: dk and dv at once, or one of them.
+enum { BACK_DQ = 0, BACK_DK = 1, BACK_DV = 2 };
+
+// WHAT & (BACK_DK | BACK_DV): lanes are keys, the walk is over rows; else lanes are rows, the walk is over keys.
+template <typename T, int NC, int WHAT>
 __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(BackArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                                               Heads<const T> dout, Heads<T> da, Heads<T> db)
 {
+    constexpr bool KEYS = WHAT != BACK_DQ, SUM_A = WHAT != BACK_DV, SUM_B = WHAT & BACK_DV;
     using G = BackTile<T, NC>;
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
@@ -169,9 +179,11 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
     const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q), all_q = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
     const long long base = (long long)nk - all_q;                   // position of the first row's token
     const int rows = nq * shared;                                    // (fits: checked by the host)
-    const int x0 = tile * BACK_LANES, count = KEYS ? min(nk, a.max_k) : rows;       // of keys (or rows)
+    // of keys (or rows).  Far workgroups: all four waves have the same 32 keys, and take turns in the rows
+    const int x0 = far ? tile * 32 : tile * BACK_LANES, count = KEYS ? min(nk, a.max_k) : rows;
     if (x0 >= count) return;
-    const int wx0 = x0 + 32 * wave, mine = min(wx0 + c32, count - 1), last = min(x0 + BACK_LANES, count) - 1, wlast = min(wx0 + 32, count) - 1;
+    const int wx0 = far ? x0 : x0 + 32 * wave, mine = min(wx0 + c32, count - 1), wlast = min(wx0 + 32, count) - 1;
+    const int last = min(x0 / BACK_LANES * BACK_LANES + BACK_LANES, count) - 1;
 
     // rows that see key j: from, up to (the window's, or all if it is one of the first)
     auto row_of = [&](long long p) {                                 // the first row at position p or behind it
@@ -228,13 +240,17 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
     auto element = [&](const Heads<const T>& x, int r) { return KEYS ? r / shared * x.token + r % shared * x.head : r * x.token; };
     // offsets of 32 bits from a tile's first row on
     auto near = [&](const Heads<const T>& x) { return x.token >= 0 && x.token < 1 << 22 && (!KEYS || (x.head >= 0 && x.head < 1 << 22)); };
-    const bool plain = near(A) && near(B) && a.D == RS && (!KEYS || RT % shared == 0);
-    unsigned ao[PER], bo[PER];
+    // chunks that a thread brings lie STEP rows apart; the swizzle has a period of 16 rows, so they have KINDS places in a row
+    constexpr int STEP = BACK_THREADS / CR, KINDS = STEP % 16 ? 2 : 1;
+    const bool plain = near(A) && near(B) && a.D == RS && (!KEYS || STEP % shared == 0);
+    const int slot0 = t / CR;
+    int chunk[KINDS];
+    unsigned ao[KINDS], bo[KINDS];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int s = i * BACK_THREADS + t, j = s / CR, c = (s % CR ^ G::swizzle(j)) * EC;
-        ao[i] = (unsigned)(element(A, j) + c) * (unsigned)sizeof(T);
-        bo[i] = (unsigned)(element(B, j) + c) * (unsigned)sizeof(T);
+    for (int i = 0; i < KINDS; ++i) {
+        chunk[i] = (t % CR ^ G::swizzle(slot0 + i * STEP)) * EC;
+        ao[i] = (unsigned)(element(A, slot0) + chunk[i]) * (unsigned)sizeof(T);
+        bo[i] = (unsigned)(element(B, slot0) + chunk[i]) * (unsigned)sizeof(T);
     }
     const unsigned a_lds = lds_address(as) + wave * 1024, b_lds = lds_address(bs) + wave * 1024;
     auto bring = [&](int it) {
@@ -244,21 +260,20 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
             to_lds(a.rows + c * a.all_rows + arows + i0 + (t - c * (RT / 4)) * 4, lds_address(rc[buf]));
         }
         if (plain && i0 + RT <= walked) {
-            const T* const a0 = ap + element(A, i0);
-            const T* const b0 = bp + element(B, i0);
+            // (rows i0 + i STEP begin with a new token, or all heads share a key head of their own)
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                to_lds(a0, ao[i], a_lds + buf * G::BYTES + i * 4096);
-                to_lds(b0, bo[i], b_lds + buf * G::BYTES + i * 4096);
+                to_lds(ap + element(A, i0 + i * STEP), ao[i % KINDS], a_lds + buf * G::BYTES + i * 4096);
+                to_lds(bp + element(B, i0 + i * STEP), bo[i % KINDS], b_lds + buf * G::BYTES + i * 4096);
             }
             return;
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int s = i * BACK_THREADS + t, j = s / CR, c = (s % CR ^ G::swizzle(j)) * EC, r = min(i0 + j, walked - 1);
-            if (c < a.D) {
-                to_lds(ap + element(A, r) + c, a_lds + buf * G::BYTES + i * 4096);
-                to_lds(bp + element(B, r) + c, b_lds + buf * G::BYTES + i * 4096);
+            const int r = min(i0 + i * STEP + slot0, walked - 1);
+            if (chunk[i % KINDS] < a.D) {
+                to_lds(ap + element(A, r) + chunk[i % KINDS], a_lds + buf * G::BYTES + i * 4096);
+                to_lds(bp + element(B, r) + chunk[i % KINDS], b_lds + buf * G::BYTES + i * 4096);
             }
         }
     };
@@ -306,8 +321,8 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
     const float slope = F16 ? ldexpf(1.f, power - WEIGHT_POWER) : 1.f;
 
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
-    const int k_at = (c32 * RS + (h ^ G::swizzle(c32)) * EC) * (int)sizeof(T);
-    const int v_at = F32 ? (4 * h * RS + ((c32 >> 2) ^ G::swizzle(4 * h)) * EC + (c32 & 3)) * (int)sizeof(T)
+    int k_at = (c32 * RS + (h ^ G::swizzle(c32)) * EC) * (int)sizeof(T);
+    int v_at = F32 ? (4 * h * RS + ((c32 >> 2) ^ G::swizzle(4 * h)) * EC + (c32 & 3)) * (int)sizeof(T)
                          : ((4 * h + r4) * RS + ((2 * g16 + (c4 >> 1)) ^ G::swizzle(4 * h + r4)) * EC + (c4 & 1) * 4) * (int)sizeof(T);
     // 32 elements of the head (from 32 x on) of the walked rows 16 m .. 16 m + 15 (fp32: row 8 (i / 4) + 4 h + i % 4 of element i)
     auto turned = [&](const char* from, int x, int m) {
@@ -324,15 +339,12 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         return *(const T*)(from + (v_at ^ x * 128 ^ G::swizzle(8 * (i / 4) + i % 4) * 16) + (8 * (i / 4) + i % 4) * RS * (int)sizeof(T));
     };
 
-    f32x16 acc_a[NC], acc_b[KEYS ? NC : 1];
+    f32x16 acc_a[NC], acc_b[NC];
 #pragma unroll
     for (int x = 0; x < NC; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            acc_a[x][i] = 0.f;
-            if (KEYS) acc_b[KEYS ? x : 0][i] = 0.f;
-        }
-    unsigned met_a[NC] = {}, met_b[NC] = {};          // elements of results that something that is not finite enters (16 bits each)
+        for (int i = 0; i < 16; ++i) acc_a[x][i] = acc_b[x][i] = 0.f;
+    unsigned met[NC] = {};                             // elements of results that something that is not finite enters (dA 16 bits, dB 16 more)
 
     for (int it = begin; it < stop; ++it) {
         const int buf = (it - begin) & 1, i0 = at(it);
@@ -341,44 +353,59 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
 #pragma unroll
         for (int u = 0; u < RT / 32; ++u) {
             const int i = i0 + 32 * u;
-            if (!any(i)) continue;
+            if (!any(i) || (far && ((it - begin) * (RT / 32) + u) % 4 != wave)) continue;
+            // (worked out again for every tile: kept, the addresses of all steps would take the registers)
+            asm volatile("" : "+v"(k_at), "+v"(v_at));
             const char* const ab = as[buf] + 32 * u * RS * sizeof(T);
             const char* const bb = bs[buf] + 32 * u * RS * sizeof(T);
             f32x16 s, dp;
-            float l2[16];
+            const float* const rows_at = rc[buf] + 32 * u + 4 * h;
+            auto of_rows = [&](int which, int e, float own) {
+                return KEYS ? *(const float4*)(rows_at + which * RT + 2 * e) : make_float4(own, own, own, own);
+            };
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                float4 x0 = make_float4(own0, own0, own0, own0), x1 = make_float4(own1, own1, own1, own1), x2 = make_float4(own2, own2, own2, own2);
-                if (KEYS) {
-                    const float* const p = rc[buf] + 32 * u + 2 * e + 4 * h;
-                    x0 = *(const float4*)p;
-                    x1 = *(const float4*)(p + RT);
-                    x2 = *(const float4*)(p + 2 * RT);
-                }
-                s[e] = x0.x; s[e + 1] = x0.y; s[e + 2] = x0.z; s[e + 3] = x0.w;
-                dp[e] = x1.x; dp[e + 1] = x1.y; dp[e + 2] = x1.z; dp[e + 3] = x1.w;
-                l2[e] = x2.x; l2[e + 1] = x2.y; l2[e + 2] = x2.z; l2[e + 3] = x2.w;
+                const float4 y = of_rows(0, e, own0);
+                s[e] = y.x; s[e + 1] = y.y; s[e + 2] = y.z; s[e + 3] = y.w;
             }
 #pragma unroll
             for (int c = 0; c < QS; ++c) {
                 const typename M::V x = *(const typename M::V*)(ab + (k_at ^ c * 32));
-                const typename M::V y = *(const typename M::V*)(bb + (k_at ^ c * 32));
                 if constexpr (F32) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s = M::mul(x[e], af[c][e], s);
-                        dp = M::mul(y[e], bf[c][e], dp);
-                    }
+                    for (int e = 0; e < 4; ++e) s = M::mul(x[e], af[c][e], s);
                 } else {
                     s = M::mul(x, af[c], s);
-                    dp = M::mul(y, bf[c], dp);
+                }
+            }
+            if constexpr (SUM_A) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 y = of_rows(1, e, own1);
+                    dp[e] = y.x; dp[e + 1] = y.y; dp[e + 2] = y.z; dp[e + 3] = y.w;
+                }
+#pragma unroll
+                for (int c = 0; c < QS; ++c) {
+                    const typename M::V y = *(const typename M::V*)(bb + (k_at ^ c * 32));
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dp = M::mul(y[e], bf[c][e], dp);
+                    } else {
+                        dp = M::mul(y, bf[c], dp);
+                    }
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], by, -l2[e]));
-                dp[e] *= F16 ? s[e] * slope : s[e];
+            for (int e = 0; e < 16; e += 4) {
+                const float4 y = of_rows(2, e, own2);
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], by, -y.x));
+                s[e + 1] = __builtin_amdgcn_exp2f(fmaf(s[e + 1], by, -y.y));
+                s[e + 2] = __builtin_amdgcn_exp2f(fmaf(s[e + 2], by, -y.z));
+                s[e + 3] = __builtin_amdgcn_exp2f(fmaf(s[e + 3], by, -y.w));
             }
+            if constexpr (SUM_A)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] *= F16 ? s[e] * slope : s[e];
             const bool whole = all(i);
             unsigned seen = ~0u;
             if (!whole) {
@@ -386,13 +413,13 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int m = (int)(seen << (31 - 8 * (e / 4) - e % 4)) >> 31;
-                    s[e] = __int_as_float(__float_as_int(s[e]) & m);
-                    dp[e] = __int_as_float(__float_as_int(dp[e]) & m);
+                    if constexpr (SUM_B) s[e] = __int_as_float(__float_as_int(s[e]) & m);
+                    if constexpr (SUM_A) dp[e] = __int_as_float(__float_as_int(dp[e]) & m);
                 }
             }
             // Pairs that do not see each other have weights of zero here, and zero times what is not finite is NaN: where there are such pairs, what
             // is not finite counts as zero, and marks the results of those that do see it.
-            auto add = [&](f32x16* acc, const char* from, const f32x16& weight, unsigned* met) {
+            auto add = [&](f32x16* acc, const char* from, const f32x16& weight, int bit) {
                 bool odd = false;
                 if constexpr (F32) {
 #pragma unroll
@@ -444,11 +471,11 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) met[x] |= kinds[e] != 0.f ? 1u << e : 0u;
+                    for (int e = 0; e < 16; ++e) met[x] |= kinds[e] != 0.f ? 1u << (bit + e) : 0u;
                 }
             };
-            if constexpr (KEYS) add(acc_b, bb, s, met_b);
-            add(acc_a, ab, dp, met_a);
+            if constexpr (SUM_B) add(acc_b, bb, s, 16);
+            if constexpr (SUM_A) add(acc_a, ab, dp, 0);
             // The compiler has been seen to read a sum right behind its product, on the other side of a branch, without the 18 wait states of fp32
             // products (one element of 16 was wrong): they are here.
             if constexpr (F32) {
@@ -459,20 +486,20 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         }
     }
     if (wx0 + c32 >= count) return;
-    auto put = [&](const Heads<T>& to, f32x16* acc, const unsigned* met, float scale, int which) {
+    auto put = [&](const Heads<T>& to, f32x16* acc, float scale, int which) {
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                if (met[x] >> e & 1) acc[x][e] = NAN;
+                if (met[x] >> (16 * which + e) & 1) acc[x][e] = NAN;
                 else acc[x][e] *= scale;
             }
-        const bool parts = a.splits > 1 || (KEYS && tile < a.far_tiles);
+        const bool parts = far || a.splits > 1 || (KEYS && tile < a.first_tiles);
         T* const y = KEYS ? to.row(k0 + mine, hk) : to.row(q0 + mine / shared, hk * shared + mine % shared);
-        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones
-        const int owns = a.splits > 1 ? a.tiles * a.splits : a.far_tiles;
+        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones, a wave's 32 keys each
+        const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles;
         const long long part = bh * (owns + a.far_tiles * a.far) + (far ? owns + tile * a.far + split : tile * a.splits + split);
-        float* const z = a.parts + ((part * (KEYS ? 2 : 1) + which) * BACK_LANES + (mine - x0)) * a.D;
+        float* const z = a.parts + ((part * (KEYS ? 2 : 1) + which) * BACK_LANES + (far ? 32 * wave : 0) + (mine - x0)) * a.D;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
@@ -490,8 +517,8 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 }
             }
     };
-    put(da, acc_a, met_a, F16 ? ldexpf(a.scale, -power) : a.scale, 0);
-    if constexpr (KEYS) put(db, acc_b, met_b, F16 ? 1.f / (1 << WEIGHT_POWER) : 1.f, 1);
+    if constexpr (SUM_A) put(da, acc_a, F16 ? ldexpf(a.scale, -power) : a.scale, 0);
+    if constexpr (SUM_B) put(db, acc_b, F16 ? 1.f / (1 << WEIGHT_POWER) : 1.f, 1);
 }
 
 // Sums of the parts of a tile: 32 lanes a key (or row), four elements a lane.
@@ -508,15 +535,16 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles,
     const int x0 = KEYS ? a.cu_k[b] : a.cu_q[b];
     const int count = KEYS ? min(a.cu_k[b + 1] - x0, a.max_k) : min(a.cu_q[b + 1] - x0, a.max_q) * shared;
     if (x >= count) return;
-    const int owns = a.splits > 1 ? a.tiles * a.splits : a.far_tiles, N = KEYS ? 2 : 1;
+    const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles, N = KEYS ? 2 : 1;
     const long long head = bh * (owns + a.far_tiles * a.far);
-    const int more = tile < a.far_tiles ? a.far : 0;
+    const int more = KEYS && x / 32 < a.far_tiles ? 4 * a.far : 0;
 #pragma unroll
     for (int which = 0; which < N; ++which) {
         float4 s = {0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < a.splits + more; ++i) {
-            const long long part = head + (i < a.splits ? tile * a.splits + i : owns + tile * a.far + i - a.splits);
-            const float4 p = *(const float4*)(a.parts + ((part * N + which) * BACK_LANES + x % BACK_LANES) * a.D + d);
+            const int f = i - a.splits;
+            const long long part = head + (f < 0 ? tile * a.splits + i : owns + x / 32 * a.far + f / 4);
+            const float4 p = *(const float4*)(a.parts + ((part * N + which) * BACK_LANES + (f < 0 ? x % BACK_LANES : f % 4 * 32 + x % 32)) * a.D + d);
             s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
         }
         const Heads<T>& to = which ? db : da;
@@ -527,7 +555,7 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles,
 }
 
 struct BackPlan {
-    int tiles, splits, far_tiles, far;
+    int tiles, splits, first_tiles, far_tiles, far;
     long long groups;
     size_t parts;                          // elements
 };
@@ -556,7 +584,8 @@ static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int
         const int lanes = sinks < max_k ? sinks : max_k;
         // rows past the window of first tokens: as many workgroups as keep each at the length of the others
         if (lanes > 0 && (long long)left + 1 < max_k) {
-            p.far_tiles = (lanes + BACK_LANES - 1) / BACK_LANES;
+            p.first_tiles = (lanes + BACK_LANES - 1) / BACK_LANES;
+            p.far_tiles = (lanes + 31) / 32;
             const long long n = ((long long)max_q + wide - 1) / wide;
             p.far = n < 1 ? 1 : n > 64 ? 64 : (int)n;
         }
@@ -566,7 +595,7 @@ static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int
     p.splits = back_splits(groups, walk, rt);
     const long long per_head = (long long)p.tiles * p.splits + (long long)p.far_tiles * p.far;
     p.groups = per_head * Hk * B;
-    const long long owns = p.splits > 1 ? (long long)p.tiles * p.splits : p.far_tiles;
+    const long long owns = p.splits > 1 ? (long long)p.tiles * p.splits : p.first_tiles;
     p.parts = (size_t)(owns + (long long)p.far_tiles * p.far) * Hk * B * (keys ? 2 : 1) * BACK_LANES * D;
     return p;
 }
@@ -593,19 +622,37 @@ static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<cons
 {
     a.tiles = p.tiles;
     a.splits = p.splits;
+    a.first_tiles = p.first_tiles;
     a.far_tiles = p.far_tiles;
     a.far = p.far;
     a.groups = p.groups;
     if (p.groups == 0) return ZNNI_OK;
     const dim3 grid = launch_of(p.groups), block(BACK_THREADS);
-    switch ((a.D + 31) / 32) {
-        case 1: k_back<T, 1, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-        case 2: k_back<T, 2, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-        case 3: k_back<T, 3, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-        default: k_back<T, 4, KEYS><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+    auto launch = [&](auto what) {
+        constexpr int WHAT = decltype(what)::value;
+        constexpr bool NARROW = WHAT == BACK_DQ || WHAT == (BACK_DK | BACK_DV), WIDE = sizeof(T) == 4 || WHAT != (BACK_DK | BACK_DV);   // that calls reach
+        switch ((a.D + 31) / 32) {
+            case 1: if constexpr (NARROW) k_back<T, 1, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+            case 2: if constexpr (NARROW) k_back<T, 2, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+            case 3: if constexpr (NARROW) k_back<T, 3, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+            default: if constexpr (WIDE) k_back<T, 4, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+        }
+    };
+    // 16-bit types, wide heads: sums of both gradients leave a SIMD one wave; one at a time, at the cost of the scores again, two (bf16, 16384
+    // tokens, window of 4096, heads 16 of 4 x 128: 2700 us at once, XXX one after the other).
+    if constexpr (!KEYS) {
+        launch(std::integral_constant<int, BACK_DQ>());
+    } else {
+        if constexpr (sizeof(T) == 2) {
+            if (a.D > 96) {
+                launch(std::integral_constant<int, BACK_DK>());
+                launch(std::integral_constant<int, BACK_DV>());
+            }
+        }
+        if (sizeof(T) == 4 || a.D <= 96) launch(std::integral_constant<int, BACK_DK | BACK_DV>());
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    const int tiles = p.splits > 1 ? p.tiles : p.far_tiles;
+    const int tiles = p.splits > 1 ? p.tiles : p.first_tiles;
     if (!tiles) return ZNNI_OK;
     k_back_join<T, KEYS><<<launch_of((long long)tiles * (BACK_LANES / 8) * a.Hk * B), dim3(256), 0, st>>>(a, B, tiles, da, db);
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
