@@ -8,6 +8,7 @@
 //   S [loop][lane] = A a,  dP [loop][lane] = B b     (A, B: q and dout, or k and v, from LDS; a, b: k and v, or q and dout)
 //   dA^T [D][lane] += A^T dS,  for keys also dB^T [D][lane] += B^T P     (P and dS as they stand are right operands; A^T, B^T by transposing reads)
 // Accumulators start from what is subtracted: S from -(the row's reference), dP from -delta.
+#include <initializer_list>
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -23,101 +24,132 @@ struct BackArgs {
     Window w;
     float scale;
     int max_q, max_k;
+    int cycle;                        // tiles that a workgroup walks, or 0: they start with their first
+    int heads;                        // B * Hk
     int tiles, splits;                // tiles of keys (or rows) of a sequence, workgroups that share a tile's walk
     int first_tiles;                  // of keys: tiles that hold first tokens, which rows past their window see too:
     int far_tiles, far;               // 32 keys at a time, so many workgroups that walk those rows
-    long long groups;
+    long long groups;                 // of the launch
     long long pitch;                  // rows of a sequence and key head in `rows`
-    const float* rows;                // [3][B * Hk][pitch]: minus the reference, minus delta, log2 of the sum
+    const char* rows;                 // [2][B * Hk][pitch]: what is taken from a row's scores and its dP, as fp32 or in pieces
     long long all_rows;               // B * Hk * pitch
-    const unsigned* peaks;            // fp16: largest magnitudes of dout and v (bits of an fp32 number)
+    float2* peaks;                    // fp16: largest finite magnitudes of dout and of v, of each workgroup that looked
+    int peak_count;
     float* parts;
 };
 
 // fp16 has no room for weights of long rows (2^-14 is its least normal number) nor for gradients of any size: P goes into its product times 2^15,
 // dS times a power of two for which |dout.v - delta| <= 2 D max|dout| max|v| stays below 2^15.  Other types have the range of fp32.
 constexpr int WEIGHT_POWER = 15;
+constexpr int PEAKS = 512;            // workgroups of the rows' kernel, which leave two maxima each
 __device__ inline int slope_power(const BackArgs& a)
 {
-    const float most = __uint_as_float(a.peaks[0]) * __uint_as_float(a.peaks[1]) * (float)a.D;
-    return most > 0.f ? WEIGHT_POWER - 2 - ilogbf(most) : 0;
-}
-
-__global__ void k_back_clear(unsigned* peaks)
-{
-    if (threadIdx.x < 2) peaks[threadIdx.x] = 0;
-}
-
-// The largest finite magnitude of a workgroup's values into a peak (a maximum has no order).
-__device__ inline void raise_peak(unsigned* peak, float most)
-{
-    __shared__ float waves[4];
+    float2 most = {0.f, 0.f};
+    for (int i = threadIdx.x & 63; i < a.peak_count; i += 64) {
+        const float2 y = a.peaks[i];
+        most = make_float2(fmaxf(most.x, y.x), fmaxf(most.y, y.y));
+    }
 #pragma unroll
-    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
-    __syncthreads();
-    if (threadIdx.x) return;
-    const unsigned y = __float_as_uint(fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3])));
-    if (y > __hip_atomic_load(peak, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(peak, y);
+    for (int o = 32; o; o >>= 1) most = make_float2(fmaxf(most.x, __shfl_xor(most.x, o)), fmaxf(most.y, __shfl_xor(most.y, o)));
+    const float both = most.x * most.y * (float)a.D;
+    return both > 0.f ? WEIGHT_POWER - 2 - ilogbf(both) : 0;
 }
 __device__ inline float finite_size(float x) { return fabsf(x) <= 65504.f ? fabsf(x) : 0.f; }
 
-__global__ __launch_bounds__(256) void k_back_peak(BackArgs a, int B, Heads<const f16> v, unsigned* peaks)
-{
-    typedef f16 V __attribute__((ext_vector_type(8)));
-    const int b = blockIdx.y, k0 = a.cu_k[b], nk = min(a.cu_k[b + 1] - k0, a.max_k), chunks = a.D / 8;
-    float most = 0.f;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)nk * a.Hk * chunks; i += (long long)gridDim.x * 256) {
-        const long long row = i / chunks;
-        const V x = *(const V*)(v.row(k0 + row / a.Hk, (int)(row % a.Hk)) + i % chunks * 8);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size((float)x[e]));
-    }
-    raise_peak(peaks + 1, most);
-}
-
-// What a score is multiplied by to count powers of two; of a scale of 0 the least there is (as in the forward kernel).
-__host__ __device__ inline float back_powers(float scale) { return scale == 0.f ? 0x1p-149f : fabsf(scale) * 1.44269504088896340736f; }
+// What a score is multiplied by to count powers of two.
+// (At least 2^-120, so that the logarithm of a sum counts as a score: scales below that are 2^-120 for scores below 2^100.)
+__host__ __device__ inline float back_powers(float scale) { return fmaxf(fabsf(scale) * 1.44269504088896340736f, 0x1p-120f); }
 
 __device__ inline unsigned low_bits(int x) { return x <= 0 ? 0u : ~0u >> (32 - min(x, 32)); }
 
 // ---- of every row: delta and its statistics --------------------------------------------------------------------------
 
+// What is taken from a row's scores (its reference and, counted as a score, the logarithm of its sum) and from its dP (delta) is there
+// before the first product.  Where lanes are keys each of a lane's 16 sums has a row of its own: three times four reads from LDS would be as
+// much as the operands'.  So 16-bit types take it as a product: three bf16 numbers that add up to it, times -1, a row's 16 bytes.
+typedef bf16 Pieces __attribute__((ext_vector_type(8)));
+__device__ inline Pieces pieces_of(float x)
+{
+    Pieces y = {(bf16)x};
+    if (fabsf(x) < 0x1p127f) {
+        const float r = x - (float)y[0];
+        y[1] = (bf16)r;
+        y[2] = (bf16)(r - (float)y[1]);
+    }
+    return y;
+}
+template <typename T>
+struct RowNumber {
+    typedef std::conditional_t<sizeof(T) == 4, float, Pieces> type;
+    __device__ static type of(float x)
+    {
+        if constexpr (sizeof(T) == 4) return x;
+        else return pieces_of(x);
+    }
+    __device__ static float value(const type& x)
+    {
+        if constexpr (sizeof(T) == 4) return x;
+        else return ((float)x[0] + (float)x[1]) + (float)x[2];
+    }
+};
+
 // Sixteen lanes a row, 16 bytes a lane at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, int B, Heads<const T> dout, Heads<const T> out, const float2* __restrict__ stats,
-                                                   float* __restrict__ rows)
+__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, int B, Heads<const T> dout, Heads<const T> out, Heads<const T> v,
+                                                   const float2* __restrict__ stats, typename RowNumber<T>::type* __restrict__ rows)
 {
+    constexpr bool F16 = std::is_same<T, f16>::value;
     constexpr int EC = 16 / sizeof(T);
     typedef T V __attribute__((ext_vector_type(EC)));
     const int G = a.Hq / a.Hk, l = threadIdx.x & 15;
-    const long long id = group_id() * 16 + (threadIdx.x >> 4);
-    const long long r = id % a.pitch, bh = id / a.pitch;
-    const int b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
-    constexpr bool F16 = std::is_same<T, f16>::value;
-    const int q0 = b < B ? a.cu_q[b] : 0, nq = b < B ? min(a.cu_q[b + 1] - q0, a.max_q) : 0;
-    float s = 0.f, most = 0.f;
-    const long long token = q0 + r / G;
-    const int head = hk * G + (int)(r % G);
-    const bool there = r < (long long)nq * G;
-    if (there)
-        for (int d = l * EC; d < a.D; d += 16 * EC) {
-            const V x = *(const V*)(dout.row(token, head) + d), y = *(const V*)(out.row(token, head) + d);
+    const long long step = (long long)gridDim.x * gridDim.y * 16, begin = group_id() * 16 + (threadIdx.x >> 4);
+    float2 most = {0.f, 0.f};
+    for (long long id = begin; id < a.all_rows; id += step) {
+        const int bh = (int)(id / a.pitch), r = (int)(id - bh * a.pitch), b = bh / a.Hk, hk = bh - b * a.Hk;
+        const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q);
+        if (r < nq * G) {                                // (fits: checked by the host)
+            const int i = r / G, head = hk * G + r - i * G;
+            const long long token = q0 + i;
+            float s = 0.f;
+            for (int d = l * EC; d < a.D; d += 16 * EC) {
+                const V x = *(const V*)(dout.row(token, head) + d), y = *(const V*)(out.row(token, head) + d);
 #pragma unroll
-            for (int e = 0; e < EC; ++e) {
-                s += (float)x[e] * (float)y[e];
-                if constexpr (F16) most = fmaxf(most, finite_size((float)x[e]));
+                for (int e = 0; e < EC; ++e) {
+                    s += (float)x[e] * (float)y[e];
+                    if constexpr (F16) most.x = fmaxf(most.x, finite_size((float)x[e]));
+                }
+            }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o, 16);
+            if (l == 0) {
+                const float2 st = stats[token * a.Hq + head];
+                // (a row without weights: none whatever the scores)
+                rows[id] = RowNumber<T>::of(st.y == 0.f ? INFINITY : st.x + (log2f(st.y) - (F16 ? WEIGHT_POWER : 0)) / back_powers(a.scale));
+                rows[a.all_rows + id] = RowNumber<T>::of(s);
             }
         }
+    }
+    if constexpr (F16) {
+        const long long keys = (long long)B * a.Hk * a.max_k;
+        for (long long id = begin; id < keys; id += step) {
+            const int bh = (int)(id / a.max_k), j = (int)(id - (long long)bh * a.max_k), b = bh / a.Hk, k0 = a.cu_k[b];
+            if (j < a.cu_k[b + 1] - k0 && l * EC < a.D) {
+                const V x = *(const V*)(v.row(k0 + j, bh - b * a.Hk) + l * EC);
 #pragma unroll
-    for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o);
-    if constexpr (F16) raise_peak((unsigned*)a.peaks, most);
-    if (l || !there) return;
-    const float2 st = stats[token * a.Hq + head];
-    // (a row without weights: none whatever the scores)
-    rows[id] = st.y == 0.f ? 0.f : -st.x;
-    rows[a.all_rows + id] = -s;
-    rows[2 * a.all_rows + id] = st.y == 0.f ? INFINITY : log2f(st.y) - (F16 ? WEIGHT_POWER : 0);
+                for (int e = 0; e < EC; ++e) most.y = fmaxf(most.y, finite_size((float)x[e]));
+            }
+        }
+        __shared__ float2 waves[4];
+#pragma unroll
+        for (int o = 32; o; o >>= 1) most = make_float2(fmaxf(most.x, __shfl_xor(most.x, o)), fmaxf(most.y, __shfl_xor(most.y, o)));
+        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 1; i < 4; ++i) most = make_float2(fmaxf(most.x, waves[i].x), fmaxf(most.y, waves[i].y));
+            a.peaks[group_id()] = most;
+        }
+    }
 }
 
 // ---- tiles of the walk ------------------------------------------------------------------------------------------------
@@ -165,17 +197,21 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
     constexpr int RT = G::RT, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER, QS = F32 ? 4 * NC : 2 * NC;
     __shared__ __align__(1024) char as[2][G::BYTES];
     __shared__ __align__(1024) char bs[2][G::BYTES];
-    __shared__ __align__(1024) float rc[2][3 * RT];                 // of the rows walked: minus the reference, minus delta, log2 of the sum
+    using N = RowNumber<T>;
+    typedef typename N::type Number;
+    __shared__ __align__(16) int odds[4];
+    __shared__ __align__(1024) Number rc[2][KEYS ? 2 * RT + 4 : 1];  // of the rows walked; then zeros
 
-    const long long group = group_id();
-    if (group >= a.groups) return;
+    const long long all_groups = group_id();
+    if (all_groups >= a.groups) return;
+    const int group = (int)all_groups;                              // (fits: checked by the host)
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
-    const int shared = a.Hq / a.Hk, per_head = a.tiles * a.splits + a.far_tiles * a.far;
-    const long long bh = group / per_head;
-    const int slot = (int)(group % per_head), b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
-    const bool far = KEYS && slot >= a.tiles * a.splits;
-    const int tile = far ? (slot - a.tiles * a.splits) / a.far : KEYS ? slot / a.splits : a.tiles - 1 - slot / a.splits;
-    const int split = far ? (slot - a.tiles * a.splits) % a.far : slot % a.splits, splits = far ? a.far : a.splits;
+    // far workgroups of all heads first: others have the chip to the end
+    const int shared = a.Hq / a.Hk, fars = a.far_tiles * a.far, per_head = a.tiles * a.splits, heads = a.heads;
+    const bool far = KEYS && group < fars * heads;
+    const int slot = far ? group : in_runs(group - fars * heads, per_head * heads), bh = far ? slot / fars : slot / per_head, rest = far ? slot % fars : slot % per_head;
+    const int b = bh / a.Hk, hk = bh - b * a.Hk, splits = far ? a.far : a.splits;
+    const int tile = far ? rest / splits : KEYS ? rest / splits : a.tiles - 1 - rest / splits, split = rest % splits;
     const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q), all_q = a.cu_q[b + 1] - q0, k0 = a.cu_k[b], nk = a.cu_k[b + 1] - k0;
     const long long base = (long long)nk - all_q;                   // position of the first row's token
     const int rows = nq * shared;                                    // (fits: checked by the host)
@@ -211,6 +247,7 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         all0 = from_row(wlast);
         all1 = wlast < a.w.sinks ? rows : window_end(max(wx0, a.w.sinks));
     }
+    const int tile0 = KEYS ? from_row(last) : 0, tile1 = !KEYS ? 0 : last < a.w.sinks ? rows : window_end(max(x0, a.w.sinks));   // likewise of the workgroup
     auto any = [&](int i) { return KEYS ? i < any1 && i + 32 > any0 : wave_rows.any(i, 32); };
     auto all = [&](int i) { return KEYS ? i >= all0 && i + 32 <= all1 : wave_rows.all(i, 32); };
     // bits of the 32 walked from i on that the lane's pair sees
@@ -230,13 +267,23 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         else hi = min(hi, r1), any1 = min(any1, r1), all1 = min(all1, r1);
     }
     const int per = (n + splits - 1) / splits, begin = split * per, stop = min(n, begin + per);
-    auto at = [&](int it) { return KEYS ? (first + it) * RT : keys.base(it); };
+    // Workgroups of an XCD that walk nearly the same tiles should be at the same ones at the same time, when these are in its L2: each starts
+    // with the first of its tiles whose number is a multiple of what one walks, and takes those before it at the end.
+    int turn = 0;
+    if (a.cycle && !far) {
+        const int head = KEYS ? first : keys.first / RT, past = (a.cycle - head % a.cycle) % a.cycle + (KEYS ? 0 : keys.sink_tiles);
+        turn = past < n ? past : 0;
+    }
+    auto at = [&](int it) {
+        const int i = it + turn < n ? it + turn : it + turn - n;
+        return KEYS ? (first + i) * RT : keys.base(i);
+    };
     const int walked = KEYS ? rows : nk;
 
     const Heads<const T> A = KEYS ? q : k, B = KEYS ? dout : v;
     const T* const ap = KEYS ? A.row(q0, hk * shared) : A.row(k0, hk);
     const T* const bp = KEYS ? B.row(q0, hk * shared) : B.row(k0, hk);
-    const long long arows = a.pitch * bh;
+    const Number* const rows_at = (const Number*)a.rows + a.pitch * bh;
     auto element = [&](const Heads<const T>& x, int r) { return KEYS ? r / shared * x.token + r % shared * x.head : r * x.token; };
     // offsets of 32 bits from a tile's first row on
     auto near = [&](const Heads<const T>& x) { return x.token >= 0 && x.token < 1 << 22 && (!KEYS || (x.head >= 0 && x.head < 1 << 22)); };
@@ -252,19 +299,27 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         ao[i] = (unsigned)(element(A, slot0) + chunk[i]) * (unsigned)sizeof(T);
         bo[i] = (unsigned)(element(B, slot0) + chunk[i]) * (unsigned)sizeof(T);
     }
-    const unsigned a_lds = lds_address(as) + wave * 1024, b_lds = lds_address(bs) + wave * 1024;
+    const unsigned a_tile = (unsigned)element(A, RT) * (unsigned)sizeof(T), b_tile = (unsigned)element(B, RT) * (unsigned)sizeof(T);   // bytes, if plain
+    const unsigned a_lds = lds_address(as), b_lds = lds_address(bs);
     auto bring = [&](int it) {
         const int buf = (it - begin) & 1, i0 = at(it);
-        if (KEYS && t < 3 * RT / 4) {
-            const int c = t / (RT / 4);
-            to_lds(a.rows + c * a.all_rows + arows + i0 + (t - c * (RT / 4)) * 4, lds_address(rc[buf]));
+        if (KEYS) {
+            // both numbers of the tile's rows: a wave each, 16 bytes a lane
+            constexpr int LANES = RT * sizeof(Number) / 16;
+            if (wave < 2 && l < LANES)
+                to_lds((const char*)(rows_at + wave * a.all_rows + i0) + l * 16, lds_address(rc[buf]) + wave * LANES * 16);
         }
         if (plain && i0 + RT <= walked) {
             // (rows i0 + i STEP begin with a new token, or all heads share a key head of their own)
+            const char* a0 = (const char*)ap + (unsigned long long)((unsigned)i0 / RT) * a_tile;
+            const char* b0 = (const char*)bp + (unsigned long long)((unsigned)i0 / RT) * b_tile;
+            const unsigned lds = wave * 1024 + buf * G::BYTES;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                to_lds(ap + element(A, i0 + i * STEP), ao[i % KINDS], a_lds + buf * G::BYTES + i * 4096);
-                to_lds(bp + element(B, i0 + i * STEP), bo[i % KINDS], b_lds + buf * G::BYTES + i * 4096);
+                to_lds(a0, ao[i % KINDS], a_lds + lds + i * 4096);
+                to_lds(b0, bo[i % KINDS], b_lds + lds + i * 4096);
+                a0 += a_tile / PER;
+                b0 += b_tile / PER;
             }
             return;
         }
@@ -272,8 +327,8 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         for (int i = 0; i < PER; ++i) {
             const int r = min(i0 + i * STEP + slot0, walked - 1);
             if (chunk[i % KINDS] < a.D) {
-                to_lds(ap + element(A, r) + chunk[i % KINDS], a_lds + buf * G::BYTES + i * 4096);
-                to_lds(bp + element(B, r) + chunk[i % KINDS], b_lds + buf * G::BYTES + i * 4096);
+                to_lds(ap + element(A, r) + chunk[i % KINDS], a_lds + wave * 1024 + buf * G::BYTES + i * 4096);
+                to_lds(bp + element(B, r) + chunk[i % KINDS], b_lds + wave * 1024 + buf * G::BYTES + i * 4096);
             }
         }
     };
@@ -286,6 +341,7 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 *(uint4*)(bs[i / (RT * CR)] + s * 16) = make_uint4(0, 0, 0, 0);
             }
         }
+    if (KEYS && t < 8) ((uint4*)&rc[t / 4][2 * RT])[sizeof(T) == 4 ? 0 : t % 4] = make_uint4(0, 0, 0, 0);
     if (begin < stop) bring(begin);
 
     // the lanes' own operands
@@ -309,13 +365,12 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 for (int e = 0; e < EC; ++e) af[c][e] = -af[c][e];
         }
     }
-    float own0 = 0.f, own1 = 0.f, own2 = 0.f;
-    if (!KEYS) {
-        own0 = a.rows[arows + mine];
-        own1 = a.rows[a.all_rows + arows + mine];
-        own2 = a.rows[2 * a.all_rows + arows + mine];
-    }
     const float by = back_powers(a.scale);
+    float own0 = 0.f, own1 = 0.f;                    // minus what is taken, from scores in powers of two
+    if (!KEYS) {
+        own0 = -N::value(rows_at[mine]) * by;
+        own1 = -N::value(rows_at[a.all_rows + mine]);
+    }
     constexpr bool F16 = std::is_same<T, f16>::value;
     const int power = F16 ? slope_power(a) : 0;
     const float slope = F16 ? ldexpf(1.f, power - WEIGHT_POWER) : 1.f;
@@ -350,6 +405,23 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
         const int buf = (it - begin) & 1, i0 = at(it);
         wait_but_and_meet<0>();
         if (it + 1 < stop) bring(it + 1);
+        // Pairs that do not see each other have weights of zero, and zero times what is not finite is NaN: where there are such pairs and such
+        // values, these count as zero, and mark the results of those that do see them.
+        bool odd = false;
+        if (!(KEYS ? i0 >= tile0 && i0 + RT <= tile1 : all_rows.all(i0, RT))) {
+            typedef T Chunk __attribute__((ext_vector_type(EC)));
+#pragma unroll
+            for (int i = 0; i < 2 * PER; ++i) {
+                const Chunk y = *(const Chunk*)((i < PER ? as[buf] : bs[buf]) + (i % PER * BACK_THREADS + t) * 16);
+#pragma unroll
+                for (int e = 0; e < EC; ++e) odd = odd || !finite_of((T)y[e]);
+            }
+            if (l == 0) odds[wave] = 0;
+            if (__any(odd) && l == 0) odds[wave] = 1;
+            wait_and_meet();
+            const int4 y = *(const int4*)odds;
+            odd = __builtin_amdgcn_readfirstlane(y.x | y.y | y.z | y.w);
+        }
 #pragma unroll
         for (int u = 0; u < RT / 32; ++u) {
             const int i = i0 + 32 * u;
@@ -359,18 +431,30 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
             const char* const ab = as[buf] + 32 * u * RS * sizeof(T);
             const char* const bb = bs[buf] + 32 * u * RS * sizeof(T);
             f32x16 s, dp;
-            const float* const rows_at = rc[buf] + 32 * u + 4 * h;
-            auto of_rows = [&](int which, int e, float own) {
-                return KEYS ? *(const float4*)(rows_at + which * RT + 2 * e) : make_float4(own, own, own, own);
-            };
+            // minus what is taken from the rows' scores (0) or dP (1)
+            auto start = [&](f32x16& y, int which) {
+                if constexpr (!KEYS) {
+                    // (one number for all of a lane's sums: taken at the end, where it costs no registers)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const float4 y = of_rows(0, e, own0);
-                s[e] = y.x; s[e + 1] = y.y; s[e + 2] = y.z; s[e + 3] = y.w;
-            }
+                    for (int e = 0; e < 16; ++e) y[e] = 0.f;
+                } else if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 z = *(const float4*)(rc[buf] + which * RT + 32 * u + 2 * e + 4 * h);
+                        y[e] = -z.x; y[e + 1] = -z.y; y[e + 2] = -z.z; y[e + 3] = -z.w;
+                    }
+                } else {
+                    const Pieces minus = {(bf16)-1.f, (bf16)-1.f, (bf16)-1.f, (bf16)0.f, (bf16)0.f, (bf16)0.f, (bf16)0.f, (bf16)0.f};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = 0.f;
+                    y = Mfma<bf16>::mul(rc[buf][h ? 2 * RT : which * RT + 32 * u + c32], minus, y);
+                }
+            };
+            start(s, 0);
 #pragma unroll
             for (int c = 0; c < QS; ++c) {
                 const typename M::V x = *(const typename M::V*)(ab + (k_at ^ c * 32));
+                if (F32 && 8 * c >= a.D) continue;              // (256 cycles a step; in 16-bit types 32, which a branch would cost)
                 if constexpr (F32) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s = M::mul(x[e], af[c][e], s);
@@ -379,14 +463,11 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 }
             }
             if constexpr (SUM_A) {
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const float4 y = of_rows(1, e, own1);
-                    dp[e] = y.x; dp[e + 1] = y.y; dp[e + 2] = y.z; dp[e + 3] = y.w;
-                }
+                start(dp, 1);
 #pragma unroll
                 for (int c = 0; c < QS; ++c) {
                     const typename M::V y = *(const typename M::V*)(bb + (k_at ^ c * 32));
+                    if (F32 && 8 * c >= a.D) continue;
                     if constexpr (F32) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) dp = M::mul(y[e], bf[c][e], dp);
@@ -396,16 +477,10 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const float4 y = of_rows(2, e, own2);
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], by, -y.x));
-                s[e + 1] = __builtin_amdgcn_exp2f(fmaf(s[e + 1], by, -y.y));
-                s[e + 2] = __builtin_amdgcn_exp2f(fmaf(s[e + 2], by, -y.z));
-                s[e + 3] = __builtin_amdgcn_exp2f(fmaf(s[e + 3], by, -y.w));
-            }
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(KEYS ? s[e] * by : fmaf(s[e], by, own0));
             if constexpr (SUM_A)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] *= F16 ? s[e] * slope : s[e];
+                for (int e = 0; e < 16; ++e) dp[e] = (KEYS ? dp[e] : dp[e] + own1) * (F16 ? s[e] * slope : s[e]);
             const bool whole = all(i);
             unsigned seen = ~0u;
             if (!whole) {
@@ -417,17 +492,15 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                     if constexpr (SUM_A) dp[e] = __int_as_float(__float_as_int(dp[e]) & m);
                 }
             }
-            // Pairs that do not see each other have weights of zero here, and zero times what is not finite is NaN: where there are such pairs, what
-            // is not finite counts as zero, and marks the results of those that do see it.
-            auto add = [&](f32x16* acc, const char* from, const f32x16& weight, int bit) {
-                bool odd = false;
+            auto add = [&](auto carefully, f32x16* acc, const char* from, const f32x16& weight, int bit) {
+                constexpr bool careful = decltype(carefully)::value;
                 if constexpr (F32) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
 #pragma unroll
                         for (int x = 0; x < NC; ++x) {
                             T y = single(from, x, e);
-                            if (!whole && !finite_of(y)) y = 0.f, odd = true;
+                            if (careful && !finite_of(y)) y = 0.f;
                             acc[x] = M::mul(y, weight[e], acc[x]);
                         }
                 } else {
@@ -439,43 +512,50 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
 #pragma unroll
                         for (int x = 0; x < NC; ++x) {
                             typename M::V y = turned(from, x, m);
-                            if (!whole)
+                            if constexpr (careful)
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
-                                    if (!finite_of((T)y[e])) y[e] = (T)0.f, odd = true;
+                                    if (!finite_of((T)y[e])) y[e] = (T)0.f;
                             acc[x] = M::mul(y, w, acc[x]);
                         }
                     }
                 }
-                if (whole || !__any(odd)) return;
+                if constexpr (careful) {
 #pragma unroll
-                for (int x = 0; x < NC; ++x) {
-                    f32x16 kinds;
+                    for (int x = 0; x < NC; ++x) {
+                        asm volatile("" : "+v"(v_at));             // (one at a time)
+                        f32x16 kinds;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) kinds[e] = 0.f;
-                    if constexpr (F32) {
+                        for (int e = 0; e < 16; ++e) kinds[e] = 0.f;
+                        if constexpr (F32) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            kinds = M::mul(finite_of(single(from, x, e)) ? 0.f : 1.f, (float)(seen >> (8 * (e / 4) + e % 4) & 1), kinds);
-                    } else {
+                            for (int e = 0; e < 16; ++e)
+                                kinds = M::mul(finite_of(single(from, x, e)) ? 0.f : 1.f, (float)(seen >> (8 * (e / 4) + e % 4) & 1), kinds);
+                        } else {
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            typename M::V y = turned(from, x, m), w;
+                            for (int m = 0; m < 2; ++m) {
+                                typename M::V y = turned(from, x, m), w;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int i8 = 8 * m + e;
-                                y[e] = finite_of((T)y[e]) ? (T)0.f : (T)1.f;
-                                w[e] = (T)(float)(seen >> (8 * (i8 / 4) + i8 % 4) & 1);
+                                for (int e = 0; e < 8; ++e) {
+                                    const int i8 = 8 * m + e;
+                                    y[e] = finite_of((T)y[e]) ? (T)0.f : (T)1.f;
+                                    w[e] = (T)(float)(seen >> (8 * (i8 / 4) + i8 % 4) & 1);
+                                }
+                                kinds = M::mul(y, w, kinds);
                             }
-                            kinds = M::mul(y, w, kinds);
                         }
-                    }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) met[x] |= kinds[e] != 0.f ? 1u << (bit + e) : 0u;
+                        for (int e = 0; e < 16; ++e) met[x] |= kinds[e] != 0.f ? 1u << (bit + e) : 0u;
+                    }
                 }
             };
-            if constexpr (SUM_B) add(acc_b, bb, s, 16);
-            if constexpr (SUM_A) add(acc_a, ab, dp, 0);
+            if (__builtin_expect(odd && !whole, 0)) {
+                if constexpr (SUM_B) add(std::true_type(), acc_b, bb, s, 16);
+                if constexpr (SUM_A) add(std::true_type(), acc_a, ab, dp, 0);
+            } else {
+                if constexpr (SUM_B) add(std::false_type(), acc_b, bb, s, 16);
+                if constexpr (SUM_A) add(std::false_type(), acc_a, ab, dp, 0);
+            }
             // The compiler has been seen to read a sum right behind its product, on the other side of a branch, without the 18 wait states of fp32
             // products (one element of 16 was wrong): they are here.
             if constexpr (F32) {
@@ -485,8 +565,34 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
             }
         }
     }
-    if (wx0 + c32 >= count) return;
-    auto put = [&](const Heads<T>& to, f32x16* acc, float scale, int which) {
+    // (the lane's place once more: kept, it would take registers from the walk)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int to = wx0 + (lane & 31), half = lane >> 5, token = KEYS ? to : to / shared;
+    // far workgroups: the waves' sums of the same keys, through LDS, in two steps
+    auto together = [&](f32x16* acc) {
+        float4* const sums = (float4*)as[0] + lane;
+#pragma unroll
+        for (int step = 2; step; step >>= 1) {
+            __syncthreads();
+            if (wave >= step && wave < 2 * step)
+#pragma unroll
+                for (int x = 0; x < NC; ++x)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4)
+                        sums[(((wave - step) * NC + x) * 4 + e / 4) * 64] = make_float4(acc[x][e], acc[x][e + 1], acc[x][e + 2], acc[x][e + 3]);
+            __syncthreads();
+            if (wave < step)
+#pragma unroll
+                for (int x = 0; x < NC; ++x)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 y = sums[((wave * NC + x) * 4 + e / 4) * 64];
+                        acc[x][e] += y.x; acc[x][e + 1] += y.y; acc[x][e + 2] += y.z; acc[x][e + 3] += y.w;
+                    }
+        }
+    };
+    auto put = [&](const Heads<T>& out, f32x16* acc, float scale, int which) {
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
@@ -494,17 +600,23 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
                 if (met[x] >> (16 * which + e) & 1) acc[x][e] = NAN;
                 else acc[x][e] *= scale;
             }
+        if (KEYS && far) {
+            together(acc);
+            if (wave) return;
+        }
+        if (to >= count) return;
         const bool parts = far || a.splits > 1 || (KEYS && tile < a.first_tiles);
-        T* const y = KEYS ? to.row(k0 + mine, hk) : to.row(q0 + mine / shared, hk * shared + mine % shared);
-        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones, a wave's 32 keys each
+        T* const y = KEYS ? out.row(k0 + to, hk) : out.row(q0 + token, hk * shared + to - token * shared);
+        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones, 32 keys each
         const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles;
-        const long long part = bh * (owns + a.far_tiles * a.far) + (far ? owns + tile * a.far + split : tile * a.splits + split);
-        float* const z = a.parts + ((part * (KEYS ? 2 : 1) + which) * BACK_LANES + (far ? 32 * wave : 0) + (mine - x0)) * a.D;
+        const long long keys = (long long)bh * (owns * BACK_LANES + a.far_tiles * a.far * 32);
+        const long long row = keys + (far ? owns * BACK_LANES + (tile * a.far + split) * 32 : (tile * a.splits + split) * BACK_LANES) + (to - x0);
+        float* const z = a.parts + (row * (KEYS ? 2 : 1) + which) * a.D;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                const int d = 32 * x + 2 * e + 4 * h;
+                const int d = 32 * x + 2 * e + 4 * half;
                 if (d >= a.D) continue;
                 if (parts) {
                     *(float4*)(z + d) = make_float4(acc[x][e], acc[x][e + 1], acc[x][e + 2], acc[x][e + 3]);
@@ -525,28 +637,34 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
 template <typename T, bool KEYS>
 __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles, Heads<T> da, Heads<T> db)
 {
-    const long long id = group_id() * 8 + (threadIdx.x >> 5);
-    const int d = (threadIdx.x & 31) * 4, shared = a.Hq / a.Hk;
-    const long long across = (long long)tiles * BACK_LANES;
-    const int x = (int)(id % across), tile = x / BACK_LANES;
-    const long long bh = id / across;
-    const int b = (int)(bh / a.Hk), hk = (int)(bh % a.Hk);
+    const int d = (threadIdx.x & 31) * 4, shared = a.Hq / a.Hk, across = tiles * (BACK_LANES / 8);
+    const int id = (int)group_id(), bh = id / across, b = bh / a.Hk, hk = bh - b * a.Hk, x = (id - bh * across) * 8 + (threadIdx.x >> 5);
     if (b >= B || d >= a.D) return;
     const int x0 = KEYS ? a.cu_k[b] : a.cu_q[b];
     const int count = KEYS ? min(a.cu_k[b + 1] - x0, a.max_k) : min(a.cu_q[b + 1] - x0, a.max_q) * shared;
     if (x >= count) return;
     const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles, N = KEYS ? 2 : 1;
-    const long long head = bh * (owns + a.far_tiles * a.far);
-    const int more = KEYS && x / 32 < a.far_tiles ? 4 * a.far : 0;
+    const int far = KEYS && x / 32 < a.far_tiles ? a.far : 0;
+    const long long keys = (long long)bh * (owns * BACK_LANES + a.far_tiles * a.far * 32);
+    const float* const own = a.parts + (keys + x / BACK_LANES * a.splits * BACK_LANES + x % BACK_LANES) * N * a.D + d;
+    const float* const others = a.parts + (keys + owns * BACK_LANES + x / 32 * a.far * 32 + x % 32) * N * a.D + d;
 #pragma unroll
     for (int which = 0; which < N; ++which) {
         float4 s = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < a.splits + more; ++i) {
-            const int f = i - a.splits;
-            const long long part = head + (f < 0 ? tile * a.splits + i : owns + x / 32 * a.far + f / 4);
-            const float4 p = *(const float4*)(a.parts + ((part * N + which) * BACK_LANES + (f < 0 ? x % BACK_LANES : f % 4 * 32 + x % 32)) * a.D + d);
-            s.x += p.x; s.y += p.y; s.z += p.z; s.w += p.w;
-        }
+        auto add = [&](const float* from, int n, int step) {
+            for (int i = 0; i < n; i += 16) {
+                float4 p[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) p[j] = *(const float4*)(from + (long long)min(i + j, n - 1) * step);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (i + j >= n) break;
+                    s.x += p[j].x; s.y += p[j].y; s.z += p[j].z; s.w += p[j].w;
+                }
+            }
+        };
+        add(own + which * a.D, a.splits, BACK_LANES * N * a.D);
+        add(others + which * a.D, far, 32 * N * a.D);
         const Heads<T>& to = which ? db : da;
         typedef T T4 __attribute__((ext_vector_type(4)));
         T* const y = KEYS ? to.row(x0 + x, hk) : to.row(x0 + x / shared, hk * shared + x % shared);
@@ -555,7 +673,7 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles,
 }
 
 struct BackPlan {
-    int tiles, splits, first_tiles, far_tiles, far;
+    int tiles, splits, first_tiles, far_tiles, far, cycle;
     long long groups;
     size_t parts;                          // elements
 };
@@ -582,21 +700,24 @@ static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int
     if (keys) {
         walk = (wide < max_q ? wide : max_q) * G;
         const int lanes = sinks < max_k ? sinks : max_k;
-        // rows past the window of first tokens: as many workgroups as keep each at the length of the others
+        // rows past the window of first tokens: so many workgroups that each is done in a small part of the others' time
         if (lanes > 0 && (long long)left + 1 < max_k) {
             p.first_tiles = (lanes + BACK_LANES - 1) / BACK_LANES;
             p.far_tiles = (lanes + 31) / 32;
-            const long long n = ((long long)max_q + wide - 1) / wide;
+            // (each eight tiles at least)
+            long long n = 8 * ((long long)max_q + wide - 1) / wide;
+            if (n > (long long)max_q * G / (8 * rt)) n = (long long)max_q * G / (8 * rt);
             p.far = n < 1 ? 1 : n > 64 ? 64 : (int)n;
         }
     } else {
         walk = wide + sinks < max_k ? wide + sinks : max_k;
     }
     p.splits = back_splits(groups, walk, rt);
+    p.cycle = p.splits == 1 ? (int)((walk + rt - 1) / rt) : 0;
     const long long per_head = (long long)p.tiles * p.splits + (long long)p.far_tiles * p.far;
     p.groups = per_head * Hk * B;
     const long long owns = p.splits > 1 ? (long long)p.tiles * p.splits : p.first_tiles;
-    p.parts = (size_t)(owns + (long long)p.far_tiles * p.far) * Hk * B * (keys ? 2 : 1) * BACK_LANES * D;
+    p.parts = (size_t)(owns * BACK_LANES + (long long)p.far_tiles * p.far * 32) * Hk * B * (keys ? 2 : 1) * D;
     return p;
 }
 
@@ -609,7 +730,7 @@ static BackSizes back_sizes(int type, int B, int Hq, int Hk, int D, int max_q, i
 {
     BackSizes s = {};
     s.pitch = ((long long)max_q * (Hq / Hk) + 63) / 64 * 64;
-    s.rows = 256 + ((size_t)3 * B * Hk * s.pitch * sizeof(float) + 255) & ~(size_t)255;
+    s.rows = PEAKS * sizeof(float2) + ((size_t)2 * B * Hk * s.pitch * (type == ZNNI_F32 ? sizeof(float) : sizeof(Pieces)) + 255) & ~(size_t)255;
     const size_t p0 = back_plan(true, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
     const size_t p1 = back_plan(false, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
     s.parts = (p0 > p1 ? p0 : p1) * sizeof(float);
@@ -623,6 +744,7 @@ static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<cons
     a.tiles = p.tiles;
     a.splits = p.splits;
     a.first_tiles = p.first_tiles;
+    a.cycle = p.cycle;
     a.far_tiles = p.far_tiles;
     a.far = p.far;
     a.groups = p.groups;
@@ -630,11 +752,11 @@ static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<cons
     const dim3 grid = launch_of(p.groups), block(BACK_THREADS);
     auto launch = [&](auto what) {
         constexpr int WHAT = decltype(what)::value;
-        constexpr bool NARROW = WHAT == BACK_DQ || WHAT == (BACK_DK | BACK_DV), WIDE = sizeof(T) == 4 || WHAT != (BACK_DK | BACK_DV);   // that calls reach
+        constexpr bool NARROW = WHAT == BACK_DQ || WHAT == (BACK_DK | BACK_DV), WIDE = sizeof(T) == 4 || WHAT != (BACK_DK | BACK_DV);   // (what calls reach)
         switch ((a.D + 31) / 32) {
             case 1: if constexpr (NARROW) k_back<T, 1, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
             case 2: if constexpr (NARROW) k_back<T, 2, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-            case 3: if constexpr (NARROW) k_back<T, 3, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
+            case 3: if constexpr (WIDE) k_back<T, 3, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
             default: if constexpr (WIDE) k_back<T, 4, WHAT><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
         }
     };
@@ -644,12 +766,12 @@ static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<cons
         launch(std::integral_constant<int, BACK_DQ>());
     } else {
         if constexpr (sizeof(T) == 2) {
-            if (a.D > 96) {
+            if (a.D > 64) {
                 launch(std::integral_constant<int, BACK_DK>());
                 launch(std::integral_constant<int, BACK_DV>());
             }
         }
-        if (sizeof(T) == 4 || a.D <= 96) launch(std::integral_constant<int, BACK_DK | BACK_DV>());
+        if (sizeof(T) == 4 || a.D <= 64) launch(std::integral_constant<int, BACK_DK | BACK_DV>());
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     const int tiles = p.splits > 1 ? p.tiles : p.first_tiles;
@@ -664,16 +786,13 @@ static znni_status launch_back(BackArgs a, int type, int B, const znni_heads* q,
                                hipStream_t st)
 {
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v), gi = heads_of<const T>(dout);
-    if (std::is_same<T, f16>::value) {
-        k_back_clear<<<dim3(1), dim3(64), 0, st>>>((unsigned*)a.peaks);
-        if (a.max_k > 0) {
-            const long long n = ((long long)a.max_k * a.Hk * (a.D / 8) + 2047) / 2048;
-            k_back_peak<<<dim3((unsigned)(n < 512 ? n : 512), (unsigned)B), dim3(256), 0, st>>>(a, B, heads_of<const f16>(v), (unsigned*)a.peaks);
-        }
-        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    }
-    if (a.max_q > 0) {
-        k_back_rows<T><<<launch_of((a.all_rows + 15) / 16), dim3(256), 0, st>>>(a, B, gi, heads_of<const T>(out), (const float2*)stats, (float*)a.rows);
+    constexpr bool F16 = std::is_same<T, f16>::value;
+    const long long all = a.all_rows, keys = F16 ? (long long)B * a.Hk * a.max_k : 0;
+    long long groups = ((all > keys ? all : keys) + 15) / 16;
+    if (F16 && groups > PEAKS) groups = PEAKS;
+    a.peak_count = F16 ? (int)groups : 0;
+    if (groups) {
+        k_back_rows<T><<<launch_of(groups), dim3(256), 0, st>>>(a, B, gi, heads_of<const T>(out), vi, (const float2*)stats, (typename RowNumber<T>::type*)a.rows);
         if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     }
     const BackPlan pk = back_plan(true, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
@@ -689,11 +808,14 @@ static znni_status back_shape(int type, int B, int Hq, int Hk, int D, int max_q,
     if (B < 0 || B > 65535 || max_q < 0 || max_k < 0 || left < 0 || right < 0 || sinks < 0) return ZNNI_ERR_SHAPE;
     const znni_status rc = heads_shape(Hq, Hk, D);
     if (rc) return rc;
-    // (tiles' ends, a tile past the last, are 32 bits)
+    // (tiles' ends, a tile past the last, and workgroups are 32 bits)
     const long long rows = (long long)max_q * (Hq / Hk), most = INT_MAX - 2 * BACK_LANES;
     if (rows > most || max_k > most) return ZNNI_ERR_SHAPE;
     const long long tiles = ((rows > max_k ? rows : max_k) + BACK_LANES - 1) / BACK_LANES;
-    return tiles * Hk > INT_MAX / (B ? B : 1) ? ZNNI_ERR_SHAPE : ZNNI_OK;
+    if (tiles * Hk > INT_MAX / (B ? B : 1)) return ZNNI_ERR_SHAPE;
+    for (const bool keys : {false, true})
+        if (back_plan(keys, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).groups > INT_MAX) return ZNNI_ERR_SHAPE;
+    return ZNNI_OK;
 }
 
 }  // namespace znni
@@ -738,9 +860,10 @@ znni_status znni_attn_window_backward(int type, int B, int Hq, int Hk, int D, co
     a.scale = scale;
     a.max_q = max_q; a.max_k = max_k;
     a.pitch = s.pitch;
+    a.heads = B * Hk;
     a.all_rows = (long long)B * Hk * s.pitch;
-    a.peaks = (const unsigned*)workspace;
-    a.rows = (const float*)workspace + 64;
+    a.peaks = (float2*)workspace;
+    a.rows = (const char*)workspace + PEAKS * sizeof(float2);
     a.parts = (float*)((char*)workspace + s.rows);
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
