@@ -651,15 +651,15 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles,
 #pragma unroll
     for (int which = 0; which < N; ++which) {
         float4 s = {0.f, 0.f, 0.f, 0.f};
+        // (eight parts on their way at once)
         auto add = [&](const float* from, int n, int step) {
-            for (int i = 0; i < n; i += 16) {
-                float4 p[16];
+            for (int i = 0; i < n; i += 8) {
+                float4 p[8];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) p[j] = *(const float4*)(from + (long long)min(i + j, n - 1) * step);
+                for (int j = 0; j < 8; ++j) p[j] = *(const float4*)(from + (long long)min(i + j, n - 1) * step);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (i + j >= n) break;
-                    s.x += p[j].x; s.y += p[j].y; s.z += p[j].z; s.w += p[j].w;
+                for (int j = 0; j < 8; ++j) {
+                    s.x += i + j < n ? p[j].x : 0.f; s.y += i + j < n ? p[j].y : 0.f; s.z += i + j < n ? p[j].z : 0.f; s.w += i + j < n ? p[j].w : 0.f;
                 }
             }
         };
