@@ -11,12 +11,31 @@ namespace znni {
 
 // ---- activations ----------------------------------------------------------------------------------------------------
 
+// The normal distribution up to z, and e^(-z^2/2).  Below zero it is e^(-z^2/2) t P(t), t = 1 / (1 + p |z|): P fitted to erfcx, which has no
+// steep part, with a relative error of 9e-8 up to |z| = 14; so the tail, where 1 + erf has no bits left, keeps its own.
+__device__ inline float normal_up_to(float z, float* bell)
+{
+    const float e = __builtin_amdgcn_exp2f(-0.72134752044448170368f * z * z), t = __builtin_amdgcn_rcpf(fmaf(0.23333333333f, fabsf(z), 1.f));
+    float p = fmaf(t, -0.0677811997f, 0.230613793f);
+    p = fmaf(t, p, -0.176407345f);
+    p = fmaf(t, p, 0.205008941f);
+    p = fmaf(t, p, 0.0232055263f);
+    p = fmaf(t, p, 0.100732062f);
+    p = fmaf(t, p, 0.0914526451f);
+    p = fmaf(t, p, 0.0931755651f);
+    const float tail = e * t * p;
+    *bell = e;
+    return z > 0.f ? 1.f - tail : tail;
+}
+__device__ inline float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z)); }
+
 template <int ACT>
 __device__ inline float activated(float z)
 {
+    float bell;
     if constexpr (ACT == ZNNI_ACT_RELU) return z < 0.f ? 0.f : z;            // (NaN stays)
-    if constexpr (ACT == ZNNI_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752440f * z);
-    if constexpr (ACT == ZNNI_ACT_SILU) return z / (1.f + expf(-z));
+    if constexpr (ACT == ZNNI_ACT_GELU) return z * normal_up_to(z, &bell);
+    if constexpr (ACT == ZNNI_ACT_SILU) return z * logistic(z);
     return z;
 }
 
@@ -24,10 +43,14 @@ template <int ACT>
 __device__ inline float slope(float z)
 {
     if constexpr (ACT == ZNNI_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    if constexpr (ACT == ZNNI_ACT_GELU) return 0.5f * erfcf(-0.70710678118654752440f * z) + z * expf(-0.5f * z * z) * 0.39894228040143267794f;
+    if constexpr (ACT == ZNNI_ACT_GELU) {
+        float bell;
+        const float up = normal_up_to(z, &bell);
+        return fmaf(z * 0.39894228040143267794f, bell, up);
+    }
     if constexpr (ACT == ZNNI_ACT_SILU) {
-        const float p = 1.f / (1.f + expf(-z));
-        return p * (1.f + z * (1.f - p));
+        const float p = logistic(z);
+        return p * fmaf(z, 1.f - p, 1.f);
     }
     return 1.f;
 }
@@ -104,6 +127,16 @@ struct ProductArgs {
     int tiles_m, tiles_n, splits, per;      // steps of the sum that a split takes
 };
 
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: runs of 32 tiles, eight rows by four columns, to the same one.
+__device__ inline void tile_of(int id, int tiles_m, int tiles_n, int* tm, int* tn)
+{
+    const int n = tiles_m * tiles_n;
+    if (id < n / 256 * 256) id = (id / 256 * 8 + id % 8) * 32 + id / 8 % 32;
+    const int band = id / (8 * tiles_n), first = band * 8, high = min(8, tiles_m - first), at = id - band * 8 * tiles_n;
+    *tm = first + at % high;
+    *tn = at / high;
+}
+
 // out^T [n][m] += W^T X: the columns of the result are the left operand, so that a lane holds four consecutive columns of a row.
 // WAVES_N x WAVES_M waves of NB x MB products of 32 x 32.
 template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES, int ACT>
@@ -119,7 +152,8 @@ __global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductAr
     if (group >= groups) return;
     long long id = group;
     const int split = (int)(id % a.splits); id /= a.splits;
-    const int tm = (int)(id % a.tiles_m), tn = (int)(id / a.tiles_m);
+    int tm, tn;
+    tile_of((int)id, a.tiles_m, a.tiles_n, &tm, &tn);
     const int m0 = tm * TM, n0 = tn * TN;
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wn = wave % WAVES_N * NB * 32, wm = wave / WAVES_N * MB * 32;
@@ -173,6 +207,18 @@ __global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductAr
                     }
                 }
         }
+#ifndef NOSGB
+        // reads of a step run ahead of the products of the one before
+        if constexpr (sizeof(T) == 2) {
+            constexpr int READS = NB * (LI ? 1 : 2) + MB * (RI ? 1 : 2), PRODUCTS = NB * MB;
+            __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+            for (int i = 0; i < 4 * PRODUCTS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
+            }
+        }
+#endif
     }
     const int h = l >> 5, c32 = l & 31;
 #pragma unroll
@@ -209,18 +255,110 @@ __global__ __launch_bounds__(256) void k_product_join(int M, int N, int splits, 
     end_four<T, ACT>(d, m, n, N - n, v);
 }
 
+// ---- few rows -------------------------------------------------------------------------------------------------------
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ inline f32x4 mul16(Mfma<bf16>::V a, Mfma<bf16>::V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mul16(Mfma<f16>::V a, Mfma<f16>::V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mul16(Mfma<float>::V a, Mfma<float>::V b, f32x4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+constexpr int FEW_WAVES = 8;
+
+// Up to 16 MB rows: bound by reading the weights.  A workgroup has 16 columns of the result, whose weights its waves read straight into
+// registers, each a part of the steps, several loads on their way at once; their sums meet in LDS.
+template <typename T, int MB, int ACT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void k_few(ProductArgs a, Side<T> w, Side<T> x, End<T> d)
+{
+    constexpr int EC = 16 / sizeof(T), STEP = 4 * EC, AHEAD = MB == 1 ? 8 : 4;
+    typedef typename Mfma<T>::V V;
+    __shared__ f32x4 sums[FEW_WAVES][MB][64];
+    const long long group = group_id();
+    const int split = (int)(group % a.splits), n0 = (int)(group / a.splits) * 16;
+    if (n0 >= a.N) return;
+    const int l = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = l & 15, c = (l >> 4) * EC;
+    const int begin = split * a.per, end = min(a.K, begin + a.per);
+    const int mine = ((end - begin + STEP - 1) / STEP + FEW_WAVES - 1) / FEW_WAVES * STEP;
+    const int k0 = begin + wave * mine, k1 = min(end, k0 + mine);
+    const T* const wp = w.p + (long long)min(n0 + c16, a.N - 1) * w.ld + c;
+    const T* xp[MB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) xp[j] = x.p + (long long)min(16 * j + c16, a.M - 1) * x.ld + c;
+    f32x4 acc[MB] = {};
+    for (int k = k0; k < k1; k += STEP * AHEAD) {
+        V y[AHEAD], z[MB][AHEAD];
+        if (w.wide && x.wide && k + STEP * AHEAD <= k1) {
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s) {
+                y[s] = *(const V*)(wp + k + s * STEP);
+#pragma unroll
+                for (int j = 0; j < MB; ++j) z[j][s] = *(const V*)(xp[j] + k + s * STEP);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < AHEAD; ++s) {
+                const int there = k1 - (k + s * STEP + c);
+                auto bring = [&](V& to, const T* p, bool wide) {
+                    if (wide && there >= EC) to = *(const V*)(p + k + s * STEP);
+                    else
+#pragma unroll
+                        for (int e = 0; e < EC; ++e) to[e] = e < there ? p[k + s * STEP + e] : (T)0.f;
+                };
+                bring(y[s], wp, w.wide);
+#pragma unroll
+                for (int j = 0; j < MB; ++j) bring(z[j][s], xp[j], x.wide);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[j] = mul16(y[s], z[j][s], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < MB; ++j) sums[wave][j][l] = acc[j];
+    __syncthreads();
+    if (wave >= MB) return;
+    const int m = 16 * wave + c16, n = n0 + 4 * (l >> 4);
+    if (m >= a.M || n >= a.N) return;
+    f32x4 s = sums[0][wave][l];
+#pragma unroll
+    for (int i = 1; i < FEW_WAVES; ++i) s += sums[i][wave][l];
+    const float4 v = make_float4(s[0], s[1], s[2], s[3]);
+    if (a.splits > 1) *(float4*)(d.parts + ((long long)split * a.M + m) * d.Np + n) = v;
+    else end_four<T, ACT>(d, m, n, a.N - n, v);
+}
+
 constexpr int SPLITS_MOST = 32;
+constexpr int FEW = 32;                  // rows that k_few takes
 
 struct ProductPlan {
-    int kind;                    // 0: tiles of 64 x 64, 1: 128 x 128, 2: 256 x 256
+    int kind;                    // 0: tiles of 64 x 64, 1: 128 x 128, 2: 256 x 256, -1: few rows
     int splits, per;
     size_t parts;                // elements
 };
 
-static ProductPlan product_plan(int type, int M, int N, int K)
+// both_inner: the sum's index is the contiguous one on both sides.
+static ProductPlan product_plan(int type, int M, int N, int K, bool both_inner)
 {
     ProductPlan p;
     const int bk = type == ZNNI_F32 ? 32 : 64;
+    if (both_inner && M <= FEW) {
+        // workgroups share the steps while there are fewer than compute units, each wave with 16 loads at least
+        p.kind = -1;
+        const long long n = ((long long)N + 15) / 16, most = (long long)K / (FEW_WAVES * 16 * (bk / 2));
+        long long s = 256 / (n ? n : 1);
+        if (s > most) s = most;
+        if (s > SPLITS_MOST) s = SPLITS_MOST;
+        if (s < 1) s = 1;
+        p.per = (int)(((K + s - 1) / s + bk - 1) / bk * bk);
+        p.splits = K ? (int)(((long long)K + p.per - 1) / p.per) : 1;
+        p.parts = p.splits > 1 ? (size_t)p.splits * M * ((N + 3) / 4 * 4) : 0;
+        return p;
+    }
     auto tiles = [&](long long e) { return ((M + e - 1) / e) * ((N + e - 1) / e); };
     p.kind = type != ZNNI_F32 && tiles(256) >= 256 ? 2 : tiles(128) >= 256 ? 1 : 0;
     const long long n = tiles(64 << p.kind), steps = ((long long)K + bk - 1) / bk;
@@ -238,9 +376,17 @@ template <typename T, bool LI, bool RI, int ACT>
 static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> right, End<T> d, hipStream_t st)
 {
     const int type = sizeof(T) == 4 ? ZNNI_F32 : ZNNI_BF16;
-    const ProductPlan p = product_plan(type, M, N, K);
+    const ProductPlan p = product_plan(type, M, N, K, LI && RI);
     d.Np = (N + 3) / 4 * 4;
     ProductArgs a = {M, N, K, 0, 0, p.splits, p.per};
+    if constexpr (LI && RI) {
+        if (p.kind < 0) {
+            const dim3 grid = launch_of((long long)((N + 15) / 16) * p.splits), block(64 * FEW_WAVES);
+            if (M <= 16) k_few<T, 1, ACT><<<grid, block, 0, st>>>(a, left, right, d);
+            else k_few<T, 2, ACT><<<grid, block, 0, st>>>(a, left, right, d);
+        }
+    }
+    if (p.kind >= 0) {
     const int edge = 64 << p.kind;
     a.tiles_m = (M + edge - 1) / edge;
     a.tiles_n = (N + edge - 1) / edge;
@@ -248,6 +394,7 @@ static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> rig
     if (p.kind == 0) k_product<T, LI, RI, 2, 2, 1, 1, 4, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
     else if (p.kind == 1) k_product<T, LI, RI, 2, 2, 2, 2, 2, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
     else if constexpr (sizeof(T) == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(512), 0, st>>>(a, left, right, d);
+    }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     if (p.splits == 1) return ZNNI_OK;
     k_product_join<T, ACT><<<launch_of(((long long)M * d.Np / 4 + 255) / 256), dim3(256), 0, st>>>(M, N, p.splits, d);
@@ -330,9 +477,9 @@ static BackwardPlan backward_plan(int type, int M, int N, int K, int act, bool d
     if (act != ZNNI_ACT_NONE && (products || dbias)) p.dz = up((size_t)M * p.dz_row * type_size(type));
     if (dbias) p.sums = up((size_t)slope_parts(M, N) * N * sizeof(float));
     size_t parts = 0;
-    if (dx) parts = product_plan(type, M, K, N).parts;
+    if (dx) parts = product_plan(type, M, K, N, false).parts;
     if (dw) {
-        const size_t q = product_plan(type, N, K, M).parts;
+        const size_t q = product_plan(type, N, K, M, false).parts;
         if (q > parts) parts = q;
     }
     p.parts = up(parts * sizeof(float));
@@ -443,7 +590,7 @@ znni_status znni_linear_workspace(int type, int M, int N, int K, size_t* bytes)
     if (!bytes) return ZNNI_ERR_NULL;
     const znni_status rc = linear_shape(type, M, N, K);
     if (rc) return rc;
-    *bytes = M > 0 && N > 0 ? up(product_plan(type, M, N, K).parts * sizeof(float)) : 0;
+    *bytes = M > 0 && N > 0 ? up(product_plan(type, M, N, K, true).parts * sizeof(float)) : 0;
     return ZNNI_OK;
 }
 
