@@ -75,7 +75,7 @@ struct End {
     T* z;
     T* out;
     long long residual_row, z_row, out_row;
-    bool wide;                  // four elements of every row are aligned
+    bool wide, whole;           // four elements of every row are aligned, 16 bytes are
     float* parts;               // sums of a part of the steps, [split][M][Np], instead of all that
     int Np;
 };
@@ -118,6 +118,28 @@ __device__ inline void end_four(const End<T>& d, long long m, int n, int there, 
             d.out[m * d.out_row + n + e] = o[e];
         }
     }
+}
+
+// 16 bytes of a row, all there and aligned.
+template <typename T, int ACT>
+__device__ inline void end_chunk(const End<T>& d, long long m, int n, const float* v)
+{
+    constexpr int EC = 16 / sizeof(T);
+    typedef T V __attribute__((ext_vector_type(EC)));
+    V b, r, z, o;
+    if (d.bias) b = *(const V*)(d.bias + n);
+    if (d.residual) r = *(const V*)(d.residual + m * d.residual_row + n);
+#pragma unroll
+    for (int e = 0; e < EC; ++e) {
+        float y = v[e];
+        if (d.bias) y += (float)b[e];
+        z[e] = (T)y;
+        y = activated<ACT>(y);
+        if (d.residual) y += (float)r[e];
+        o[e] = (T)y;
+    }
+    if (d.z) *(V*)(d.z + m * d.z_row + n) = z;
+    *(V*)(d.out + m * d.out_row + n) = o;
 }
 
 // ---- products over tiles --------------------------------------------------------------------------------------------
@@ -221,20 +243,52 @@ __global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductAr
 #endif
     }
     const int h = l >> 5, c32 = l & 31;
+    if (a.splits > 1) {
+#pragma unroll
+        for (int j = 0; j < MB; ++j) {
+            const int m = m0 + wm + 32 * j + c32;
+            if (m >= a.M) continue;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = n0 + wn + 32 * i + 8 * q + 4 * h;
+                    if (col < a.N)
+                        *(float4*)(d.parts + ((long long)split * a.M + m) * d.Np + col) =
+                            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                }
+        }
+        return;
+    }
+    // A lane has four columns of a row, 32 rows side by side: through LDS, a wave's 32 rows at a time, they become whole lines of memory.
+    // (Chunk c of row r at c ^ r: lanes that write have a row each, lanes that read consecutive chunks.)
+    constexpr int EC = 16 / sizeof(T), COLS = 32 * NB, CHUNKS = COLS / 4, LANES = COLS / EC;
+    static_assert(WAVES_N * WAVES_M * 32 * COLS * 4 <= STAGES * (L::BYTES + R::BYTES), "a wave's rows fit its part of LDS");
+    __syncthreads();
+    float4* const mine = (float4*)&tiles[0][0] + wave * 32 * CHUNKS;
 #pragma unroll
     for (int j = 0; j < MB; ++j) {
-        const int m = m0 + wm + 32 * j + c32;
-        if (m >= a.M) continue;
 #pragma unroll
         for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = n0 + wn + 32 * i + 8 * q + 4 * h;
-                if (col >= a.N) continue;
-                const float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                if (a.splits > 1) *(float4*)(d.parts + ((long long)split * a.M + m) * d.Np + col) = v;
-                else end_four<T, ACT>(d, m, col, a.N - col, v);
+            for (int q = 0; q < 4; ++q)
+                mine[c32 * CHUNKS + ((8 * i + 2 * q + h) ^ (c32 & (CHUNKS - 1)))] =
+                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 64 / LANES) {
+            const int r = r0 + l / LANES, c = l % LANES * EC, m = m0 + wm + 32 * j + r, col = n0 + wn + c;
+            float4 v[EC / 4];
+#pragma unroll
+            for (int e = 0; e < EC / 4; ++e) v[e] = mine[r * CHUNKS + ((c / 4 + e) ^ (r & (CHUNKS - 1)))];
+            if (m >= a.M || col >= a.N) continue;
+            if (d.whole && col + EC <= a.N) {
+                end_chunk<T, ACT>(d, m, col, (const float*)v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < EC / 4; ++e)
+                    if (col + 4 * e < a.N) end_four<T, ACT>(d, m, col + 4 * e, a.N - col - 4 * e, v[e]);
             }
+        }
     }
 }
 
@@ -360,7 +414,11 @@ static ProductPlan product_plan(int type, int M, int N, int K, bool both_inner)
         return p;
     }
     auto tiles = [&](long long e) { return ((M + e - 1) / e) * ((N + e - 1) / e); };
-    p.kind = type != ZNNI_F32 && tiles(256) >= 256 ? 2 : tiles(128) >= 256 ? 1 : 0;
+    // Tiles of 256 x 256 have a compute unit each, of 128 x 128 two share one; a round of the latter, half the work, takes 0.57 of the time (8192^3
+    // bf16: 864 us and 985).  So whichever fills its last round better: 13824 x 2048 x 4096 (4 rounds, 7 half ones) 242 us and 248, its dw, 2048 x
+    // 4096 outputs (1, 1) 300 and 203.  With less than half a round of the smaller tiles, 64 x 64 and the steps split.
+    const long long r2 = 100 * ((tiles(256) + 255) / 256), r1 = 57 * ((tiles(128) + 511) / 512);
+    p.kind = tiles(128) < 256 ? 0 : type != ZNNI_F32 && r2 <= r1 + r1 / 20 ? 2 : 1;
     const long long n = tiles(64 << p.kind), steps = ((long long)K + bk - 1) / bk;
     long long s = p.kind == 0 && n < 256 ? 512 / (n ? n : 1) : 1;
     if (s > steps / 2) s = steps / 2;
@@ -499,6 +557,7 @@ static End<T> end_of(const znni_rows* out)
     d.out = (T*)out->data;
     d.out_row = out->row;
     d.wide = rows_wide(out->data, out->row, sizeof(T), 4 * sizeof(T));
+    d.whole = rows_wide(out->data, out->row, sizeof(T), 16);
     return d;
 }
 
@@ -510,15 +569,18 @@ static znni_status forward(int M, int N, int K, const znni_rows* x, const znni_r
     const int four = 4 * sizeof(T);
     d.bias = (const T*)bias;
     d.wide = d.wide && !((uintptr_t)bias % four);
+    d.whole = d.whole && !((uintptr_t)bias & 15u);
     if (residual) {
         d.residual = (const T*)residual->data;
         d.residual_row = residual->row;
         d.wide = d.wide && rows_wide(residual->data, residual->row, sizeof(T), four);
+        d.whole = d.whole && rows_wide(residual->data, residual->row, sizeof(T), 16);
     }
     if (z) {
         d.z = (T*)z->data;
         d.z_row = z->row;
         d.wide = d.wide && rows_wide(z->data, z->row, sizeof(T), four);
+        d.whole = d.whole && rows_wide(z->data, z->row, sizeof(T), 16);
     }
     d.parts = (float*)workspace;
     return with_act(act, [&](auto k) {
