@@ -48,40 +48,54 @@ struct Row {
                 for (int e = 0; e < VEC; ++e) y[v][e] = (T)0.f;
         }
     }
-    __device__ static float sum(float x, float* shared)
+    __device__ static void clear(V (&y)[NV])
     {
 #pragma unroll
-        for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-        if constexpr (W > 1) {
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
-            __syncthreads();
-            x = 0.f;
-#pragma unroll
-            for (int i = 0; i < W; ++i) x += shared[i];
-        }
-        return x;
+        for (int i = 0; i < E; ++i) y[i / VEC][i % VEC] = (T)0.f;
     }
+    // Sums of a pair over the row.  Waves meet once: a sum's place in LDS is written again two sums later.
+    struct Sums {
+        float2 (*place)[W];
+        int turn;
+        __device__ float2 operator()(float2 x)
+        {
+#pragma unroll
+            for (int o = 32; o; o >>= 1) x.x += __shfl_xor(x.x, o), x.y += __shfl_xor(x.y, o);
+            if constexpr (W > 1) {
+                turn ^= 1;
+                if ((threadIdx.x & 63) == 0) place[turn][threadIdx.x >> 6] = x;
+                __syncthreads();
+                x = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < W; ++i) x.x += place[turn][i].x, x.y += place[turn][i].y;
+            }
+            return x;
+        }
+    };
 };
 
-// Mean (or 0) and factor of a row; lanes past its end hold zeros.
-template <typename R, int E, typename F>
-__device__ inline void moments(F at, const NormArgs& a, int lane, int vec, float* shared, float* mean, float* r)
+// Means (or 0) and factors of two rows, `first` and `second` (as far as they are normed); lanes past their end hold zeros.
+template <typename R, int E, int VEC, typename F, typename G>
+__device__ inline void moments(F first, G second, const NormArgs& a, bool one, bool two, int lane, typename R::Sums& sum, float2* mean, float2* r)
 {
-    float s = 0.f, m = 0.f;
+    float2 m = {0.f, 0.f}, s = {0.f, 0.f};
     if (a.centred) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) s += at(i);
-        m = R::sum(s, shared) / a.C;
-        s = 0.f;
+        for (int i = 0; i < E; ++i) s.x += first(i), s.y += second(i);
+        s = sum(s);
+        m = make_float2(one ? s.x / a.C : 0.f, two ? s.y / a.C : 0.f);
+        s = make_float2(0.f, 0.f);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        const float d = R::column(lane, i / vec) < a.C ? at(i) - m : 0.f;
-        s += d * d;
+        const bool there = R::column(lane, i / VEC) < a.C;
+        const float x = there ? first(i) - m.x : 0.f, y = there ? second(i) - m.y : 0.f;
+        s.x = fmaf(x, x, s.x);
+        s.y = fmaf(y, y, s.y);
     }
+    s = sum(s);
     *mean = m;
-    *r = 1.f / sqrtf(R::sum(s, shared) / a.C + a.eps);
+    *r = make_float2(one ? 1.f / sqrtf(s.x / a.C + a.eps) : 1.f, two ? 1.f / sqrtf(s.y / a.C + a.eps) : 1.f);
 }
 
 template <typename T, int VEC, int E, int W>
@@ -91,7 +105,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows
     using R = Row<T, VEC, E, W>;
     typedef typename R::V V;
     constexpr int NV = R::NV;
-    __shared__ float shared[W];
+    __shared__ float2 place[2][W];
+    typename R::Sums sum = {place, 0};
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
     const long long t = W == 1 ? group_id() * 4 + (threadIdx.x >> 6) : group_id();
     if (t >= a.T) return;
@@ -100,18 +115,17 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows
     float s[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) s[i] = (float)xv[i / VEC][i % VEC];
-    float mean, r;
+    const auto none = [](int) { return 0.f; };
+    float2 mean = {0.f, 0.f}, r = {1.f, 1.f};
     if (y.p) {
         V yv[NV], w[NV], g[NV];
         R::load(yv, y.p + t * y.row, lane, a.C);
         if (gate.p) R::load(g, gate.p + t * gate.row, lane, a.C);
         if (post) R::load(w, post, lane, a.C);
-        mean = 0.f;
-        r = 1.f;
-        if (a.post) moments<R, E>([&](int i) { return (float)yv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
+        if (a.post) moments<R, E, VEC>([&](int i) { return (float)yv[i / VEC][i % VEC]; }, none, a, true, false, lane, sum, &mean, &r);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            float u = ((float)yv[i / VEC][i % VEC] - mean) * r;
+            float u = ((float)yv[i / VEC][i % VEC] - mean.x) * r.x;
             if (post) u *= (float)w[i / VEC][i % VEC];
             if (gate.p) u *= (float)g[i / VEC][i % VEC];
             s[i] += a.scale * u;
@@ -131,14 +145,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows
     if (!a.pre) return;
     V w[NV];
     if (pre) R::load(w, pre, lane, a.C);
-    moments<R, E>([&](int i) { return s[i]; }, a, lane, VEC, shared, &mean, &r);
+    moments<R, E, VEC>([&](int i) { return s[i]; }, none, a, true, false, lane, sum, &mean, &r);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if (R::column(lane, v) >= a.C) continue;
         V o;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            float n = (s[v * VEC + e] - mean) * r;
+            float n = (s[v * VEC + e] - mean.x) * r.x;
             if (pre) n *= (float)w[v][e];
             o[e] = (T)n;
         }
@@ -159,45 +173,41 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
     using R = Row<T, VEC, E, W>;
     typedef typename R::V V;
     constexpr int NV = R::NV, AT_ONCE = W == 1 ? 4 : 1;
-    __shared__ float shared[W];
+    __shared__ float2 place[2][W];
     __shared__ float joined[W == 1 ? 4 * 64 * E : 1];
+    typename R::Sums sum = {place, 0};
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x, mine = W == 1 ? threadIdx.x >> 6 : 0;
     const long long t0 = group_id() * a.per, t1 = min((long long)a.T, t0 + a.per);
     float sg[E], sp[E], sq[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) sg[i] = sp[i] = sq[i] = 0.f;
+    // What a call does not have takes part as what changes nothing (ones, and zeros for means and sums): every element goes the same way.
+    V wq[NV], wp[NV];
+    auto weights = [&](V (&w)[NV], const T* p) {
+        if (p) R::load(w, p, lane, a.C);
+        else
+#pragma unroll
+            for (int i = 0; i < E; ++i) w[i / VEC][i % VEC] = (T)(R::column(lane, i / VEC) < a.C ? 1.f : 0.f);
+    };
+    weights(wq, pre);
+    weights(wp, post);
+    V one[NV];                                         // a gate that all tokens share, or none
+    if (!gate.p || a.shared) weights(one, gate.p);
+    const bool block = y.p || dy.p;
     for (long long t = t0 + mine; t < t1; t += AT_ONCE) {
-        float d[E];
+        // all of the row's reads first
+        V hv[NV], zv[NV], xv[NV], yv[NV], gv[NV];
+        if (a.pre) R::load(hv, h.p + t * h.row, lane, a.C), R::load(zv, dz.p + t * dz.row, lane, a.C);
+        else R::clear(hv), R::clear(zv);
+        if (dh.p) R::load(xv, dh.p + t * dh.row, lane, a.C);
+        else R::clear(xv);
+        if (y.p) R::load(yv, y.p + t * y.row, lane, a.C);
+        else R::clear(yv);
+        if (gate.p && !a.shared) R::load(gv, gate.p + t * gate.row, lane, a.C);
+        else
 #pragma unroll
-        for (int i = 0; i < E; ++i) d[i] = 0.f;
-        if (a.pre) {
-            V hv[NV], gv[NV], w[NV];
-            R::load(hv, h.p + t * h.row, lane, a.C);
-            R::load(gv, dz.p + t * dz.row, lane, a.C);
-            if (pre) R::load(w, pre, lane, a.C);
-            float mean, r, both = 0.f, only = 0.f;
-            moments<R, E>([&](int i) { return (float)hv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float n = ((float)hv[i / VEC][i % VEC] - mean) * r;
-                float g = (float)gv[i / VEC][i % VEC];
-                sq[i] += g * n;
-                if (pre) g *= (float)w[i / VEC][i % VEC];
-                d[i] = g;
-                both += g * n;
-                only += g;
-            }
-            both = R::sum(both, shared) / a.C;
-            only = a.centred ? R::sum(only, shared) / a.C : 0.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[i] = r * (d[i] - ((float)hv[i / VEC][i % VEC] - mean) * r * both - only);
-        }
-        if (dh.p) {
-            V gv[NV];
-            R::load(gv, dh.p + t * dh.row, lane, a.C);
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[i] += (float)gv[i / VEC][i % VEC];
-        }
+            for (int v = 0; v < NV; ++v) gv[v] = one[v];
+        auto of = [](const V (&x)[NV], int i) { return (float)x[i / VEC][i % VEC]; };
         auto put = [&](const Rows<T>& to, auto at) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
@@ -208,42 +218,51 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
                 *(V*)(to.p + t * to.row + R::column(lane, v)) = o;
             }
         };
+        float2 mean = {0.f, 0.f}, r = {1.f, 1.f};
+        if (a.pre || a.post) moments<R, E, VEC>([&](int i) { return of(hv, i); }, [&](int i) { return of(yv, i); }, a, a.pre, a.post, lane, sum, &mean, &r);
+        const float hm = mean.x, hr = r.x, ym = mean.y, yr = r.y;
+        float d[E];
+        float2 over = {0.f, 0.f};                          // of the gradient times the normed row, of the gradient
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float n = (of(hv, i) - hm) * hr, z = of(zv, i);
+            sq[i] = fmaf(z, n, sq[i]);
+            d[i] = z * of(wq, i);
+            over.x = fmaf(d[i], n, over.x);
+            over.y += d[i];
+        }
+        if (a.pre) {
+            over = sum(over);
+            over = make_float2(over.x / a.C, a.centred ? over.y / a.C : 0.f);
+        } else {
+            over = make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] = fmaf(hr, d[i] - (of(hv, i) - hm) * hr * over.x - over.y, of(xv, i));
         if (dx.p) put(dx, [&](int i) { return d[i]; });
-        if (!y.p && !dy.p) continue;
-        V yv[NV], w[NV], gv[NV];
-        if (y.p) R::load(yv, y.p + t * y.row, lane, a.C);
-        if (post) R::load(w, post, lane, a.C);
-        if (gate.p) R::load(gv, gate.p + t * gate.row, lane, a.C);
-        float mean = 0.f, r = 1.f, both = 0.f, only = 0.f;
-        if (a.post) moments<R, E>([&](int i) { return (float)yv[i / VEC][i % VEC]; }, a, lane, VEC, shared, &mean, &r);
-        auto normed = [&](int i) { return ((float)yv[i / VEC][i % VEC] - mean) * r; };
+        if (!block) continue;
+        auto normed = [&](int i) { return (of(yv, i) - ym) * yr; };
 #pragma unroll
         for (int i = 0; i < E; ++i) d[i] *= a.scale;
-        if (gate.p) {
-            auto of_gate = [&](int i) { return d[i] * normed(i) * (post ? (float)w[i / VEC][i % VEC] : 1.f); };
-            if (dgate.p) put(dgate, of_gate);
-            if (sums.gate)
+        if (dgate.p) put(dgate, [&](int i) { return d[i] * (normed(i) * of(wp, i)); });
+        over = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < E; ++i) sg[i] += of_gate(i);
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[i] *= (float)gv[i / VEC][i % VEC];
+        for (int i = 0; i < E; ++i) {
+            const float n = normed(i);
+            sg[i] = fmaf(d[i], n * of(wp, i), sg[i]);
+            d[i] *= of(gv, i);
+            sp[i] = fmaf(d[i], n, sp[i]);
+            d[i] *= of(wp, i);
+            over.x = fmaf(d[i], n, over.x);
+            over.y += d[i];
         }
         if (a.post) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float n = normed(i);
-                sp[i] += d[i] * n;
-                if (post) d[i] *= (float)w[i / VEC][i % VEC];
-                if (R::column(lane, i / VEC) >= a.C) d[i] = 0.f;
-                both += d[i] * n;
-                only += d[i];
-            }
-            both = R::sum(both, shared) / a.C;
-            only = a.centred ? R::sum(only, shared) / a.C : 0.f;
-#pragma unroll
-            for (int i = 0; i < E; ++i) d[i] = r * (d[i] - normed(i) * both - only);
+            over = sum(over);
+            over = make_float2(over.x / a.C, a.centred ? over.y / a.C : 0.f);
+        } else {
+            over = make_float2(0.f, 0.f);
         }
-        if (dy.p) put(dy, [&](int i) { return d[i]; });
+        if (dy.p) put(dy, [&](int i) { return yr * (d[i] - normed(i) * over.x - over.y); });
     }
     auto write = [&](float* to, const float (&s)[E]) {
         if (!to) return;
@@ -272,9 +291,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
 }
 
 constexpr int NORM_MOST = 16384;          // channels
-constexpr int NORM_GROUPS = 512;          // workgroups that share the rows, where sums over tokens are wanted
+constexpr int NORM_GROUPS = 1024;         // workgroups that share the rows, where sums over tokens are wanted
 
-// Elements a lane and waves a row: 8 and 1, 8 and 4, 32 and 1, 2, 4 or 8.
+// Elements a lane and waves a row.
 struct NormShape {
     int E, W;
 };
@@ -284,26 +303,43 @@ static NormShape norm_shape(int T, int C)
     if (C <= 2048) return T <= 1024 ? NormShape{8, 4} : NormShape{32, 1};
     return {32, C <= 4096 ? 2 : C <= 8192 ? 4 : 8};
 }
-
-static int norm_rows(int T, int C, bool sums)
+// Gradients hold five rows and three sums.
+static NormShape norm_back_shape(int C)
 {
-    const int once = norm_shape(T, C).W == 1 ? 4 : 1;
+    return C <= 512 ? NormShape{8, 1} : C <= 2048 ? NormShape{8, 4} : C <= 4096 ? NormShape{8, 8} : NormShape{16, C <= 8192 ? 8 : 16};
+}
+
+// Rows of a workgroup: with sums over tokens, all those that make NORM_GROUPS workgroups.
+static int norm_rows(int T, int W, bool sums)
+{
+    const int once = W == 1 ? 4 : 1;
     if (!sums) return once;
     const long long n = ((long long)T + NORM_GROUPS - 1) / NORM_GROUPS;
     return (int)((n + once - 1) / once * once);
 }
 
 template <typename T, typename F>
-static znni_status with_row(int n, int C, bool wide, F f)
+static znni_status with_row(NormShape s, bool wide, F f)
 {
-    constexpr int VEC = 16 / sizeof(T);
-    const NormShape s = norm_shape(n, C);
     auto go = [&](auto vec) {
         constexpr int V = decltype(vec)::value;
         if (s.E == 8) return s.W == 1 ? f(Row<T, V, 8, 1>()) : f(Row<T, V, 8, 4>());
         return s.W == 1 ? f(Row<T, V, 32, 1>()) : s.W == 2 ? f(Row<T, V, 32, 2>()) : s.W == 4 ? f(Row<T, V, 32, 4>()) : f(Row<T, V, 32, 8>());
     };
-    if (wide) go(std::integral_constant<int, VEC>());
+    if (wide) go(std::integral_constant<int, 16 / sizeof(T)>());
+    else go(std::integral_constant<int, 1>());
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+}
+
+template <typename T, typename F>
+static znni_status with_back_row(NormShape s, bool wide, F f)
+{
+    auto go = [&](auto vec) {
+        constexpr int V = decltype(vec)::value;
+        if (s.E == 8) return s.W == 1 ? f(Row<T, V, 8, 1>()) : s.W == 4 ? f(Row<T, V, 8, 4>()) : f(Row<T, V, 8, 8>());
+        return s.W == 8 ? f(Row<T, V, 16, 8>()) : f(Row<T, V, 16, 16>());
+    };
+    if (wide) go(std::integral_constant<int, 16 / sizeof(T)>());
     else go(std::integral_constant<int, 1>());
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }
@@ -339,7 +375,7 @@ static znni_status norm_forward(NormArgs a, const znni_rows* x, const znni_rows*
     Rows<const T> g = rows_of<const T>(gate);
     if (a.shared) g.row = 0;
     const znni_rows one = {(void*)g.p, g.row};
-    return with_row<T>(a.T, a.C, all_wide<T>(a.C, {x, y, gate ? &one : nullptr, h, z}, {post, pre}), [&](auto row) {
+    return with_row<T>(norm_shape(a.T, a.C), all_wide<T>(a.C, {x, y, gate ? &one : nullptr, h, z}, {post, pre}), [&](auto row) {
         launch_norm(row, grid, st, a, rows_of<const T>(x), rows_of<const T>(y), g, (const T*)post, (const T*)pre, rows_of<T>(h), rows_of<T>(z));
         return 0;
     });
@@ -372,7 +408,7 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
     if (a.T > 0) {
         const Rows<T> dg = summed ? Rows<T>{nullptr, 0} : rows_of<T>(dgate);
         const bool wide = all_wide<T>(a.C, {dh, dz, h, y, gate ? &one : nullptr, dx, dy, summed ? nullptr : dgate}, {post, pre});
-        const znni_status rc = with_row<T>(a.T, a.C, wide, [&](auto row) {
+        const znni_status rc = with_back_row<T>(norm_back_shape(a.C), wide, [&](auto row) {
             launch_norm_back(row, launch_of(((long long)a.T + a.per - 1) / a.per), st, a, rows_of<const T>(dh), rows_of<const T>(dz), rows_of<const T>(h), rows_of<const T>(y), g,
                              (const T*)post, (const T*)pre, rows_of<T>(dx), rows_of<T>(dy), dg, sums);
             return 0;
@@ -410,7 +446,7 @@ znni_status znni_block_norm(int type, int T, int C, const znni_rows* x, const zn
     if (y && ((rc = rows_fine(y, type, T, C, false)) || (rc = rows_fine(h, type, T, C, true)))) return rc;
     if (gate && (rc = rows_fine(gate, type, shared ? 1 : T, C, false))) return rc;
     if (((uintptr_t)post | (uintptr_t)pre) % type_size(type)) return ZNNI_ERR_ALIGN;
-    const NormArgs a = {T, C, norm_rows(T, C, false), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
+    const NormArgs a = {T, C, norm_rows(T, norm_shape(T, C).W, false), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
         case ZNNI_F32: return norm_forward<float>(a, x, y, gate, post, pre, h, z, st);
@@ -455,7 +491,7 @@ znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh
         if ((uintptr_t)workspace & 255u) return ZNNI_ERR_ALIGN;
         if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
     }
-    const NormArgs a = {T, C, norm_rows(T, C, summed), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
+    const NormArgs a = {T, C, norm_rows(T, norm_back_shape(C).W, summed), scale, eps, has_post, has_pre, (flags & ZNNI_NORM_CENTRED) != 0, shared};
     float* const ws = (float*)workspace;
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {

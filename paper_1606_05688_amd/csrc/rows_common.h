@@ -24,7 +24,7 @@ static inline znni_status rows_fine(const znni_rows* r, int type, int rows, int 
     return ZNNI_OK;
 }
 
-// Sums of `parts` rows of n sums, eight lanes a column.  blockIdx.y: which of the outputs.
+// Sums of `parts` rows of n sums, 32 lanes a column, four reads of a lane on their way at once.  blockIdx.y: which of the outputs.
 template <typename T>
 struct SumOut {
     T* to[3];
@@ -32,27 +32,30 @@ struct SumOut {
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_sum_parts(int n, int parts, SumOut<T> o)
+__global__ __launch_bounds__(1024) void k_sum_parts(int n, int parts, SumOut<T> o)
 {
-    __shared__ float part[8][32];
+    __shared__ float part[32][33];
     T* const out = o.to[blockIdx.y];
     const float* const sums = o.from[blockIdx.y];
     const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c;
-    float s = 0.f;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (col < n)
-        for (int i = r; i < parts; i += 8) s += sums[(long long)i * n + col];
-    part[r][c] = s;
-    __syncthreads();
-    if (r || col >= n) return;
+        for (int i = r; i < parts; i += 128)
 #pragma unroll
-    for (int q = 1; q < 8; ++q) s += part[q][c];
-    out[col] = (T)s;
+            for (int j = 0; j < 4; ++j) s[j] += i + 32 * j < parts ? sums[(long long)(i + 32 * j) * n + col] : 0.f;
+    part[c][r] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    // a column's 32 sums by 32 lanes of a wave
+    float y = part[r][c];
+#pragma unroll
+    for (int x = 16; x; x >>= 1) y += __shfl_xor(y, x, 32);
+    if (c == 0 && (int)blockIdx.x * 32 + r < n) out[blockIdx.x * 32 + r] = (T)y;
 }
 
 template <typename T>
 static znni_status launch_sum_parts(int n, int parts, const SumOut<T>& o, int outputs, hipStream_t st)
 {
-    k_sum_parts<T><<<dim3((unsigned)((n + 31LL) / 32), (unsigned)outputs), dim3(256), 0, st>>>(n, parts, o);
+    k_sum_parts<T><<<dim3((unsigned)((n + 31LL) / 32), (unsigned)outputs), dim3(1024), 0, st>>>(n, parts, o);
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }
 
