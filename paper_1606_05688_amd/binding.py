@@ -4,6 +4,7 @@ PyTorch is used for device memory and streams; every step of the layer runs in t
 There is no fallback: if the compiled library is missing, loading raises.
 """
 import ctypes
+import functools
 import os
 import struct
 
@@ -452,6 +453,14 @@ def _scratch(need, workspace, x):
     return workspace.data_ptr(), workspace.numel(), workspace
 
 
+@functools.lru_cache(4096)
+def _need(L, query, *args):
+    """Bytes that a workspace query of the library answers for these sizes."""
+    b = ctypes.c_size_t(0)
+    _check(getattr(L, query)(*args, _byref(b)))
+    return b.value
+
+
 def znni_rope_axes(q, k, pos, freq, sections, pairing="halves", out_q=None, out_k=None, stream=None):
     """Rotary positions with several axes on q [T, Hq, D] and k [T, Hk, D] (k may be None): pair j is turned by
     pos[t, a] * freq[j], a the axis whose section holds j.  pairing: "halves" (j, R + j) or "neighbours" (2j, 2j + 1), R the sum
@@ -518,14 +527,8 @@ def _stats(stats, Tq, Hq, kind):
     return stats.data_ptr()
 
 
-def _attn_window_backward_need(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks):
-    b = ctypes.c_size_t(0)
-    _check(lib().znni_attn_window_backward_workspace(type, B, Hq, Hk, D, max_q, max_k, left, right, sinks, _byref(b)))
-    return b.value
-
-
 def znni_attn_window_backward_workspace(dtype, B, Hq, Hk, D, max_q, max_k, left=None, right=0, sinks=0):
-    return _attn_window_backward_need(_TYPES[dtype], int(B), int(Hq), int(Hk), int(D), int(max_q), int(max_k), _window(left), _window(right), int(sinks))
+    return _need(lib(), "znni_attn_window_backward_workspace", _TYPES[dtype], int(B), int(Hq), int(Hk), int(D), int(max_q), int(max_k), _window(left), _window(right), int(sinks))
 
 
 def znni_attn_window_backward(dout, q, k, v, out, stats, cu_q, cu_k, max_q, max_k, left=None, right=0, sinks=0, scale=None, dq=None, dk=None,
@@ -544,7 +547,7 @@ def znni_attn_window_backward(dout, q, k, v, out, stats, cu_q, cu_k, max_q, max_
     dq, do_q = _result(q, dq, shape, kind)
     dk, do_k = _result(k, dk, kshape, kind)
     dv, do_v = _result(v, dv, kshape, kind)
-    w, n, held = _scratch(_attn_window_backward_need(kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
+    w, n, held = _scratch(_need(lib(), "znni_attn_window_backward_workspace", kind[0], B, Hq, Hk, D, max_q, max_k, left, right, sinks), workspace, q)
     _check(lib().znni_attn_window_backward(kind[0], B, Hq, Hk, D, _heads(q, shape, kind), _heads(k, kshape, kind), _heads(v, kshape, kind),
                                            _heads(out, shape, kind), _stats(stats, Tq, Hq, kind), _heads(dout, shape, kind), _ints(cu_q, kind, B + 1),
                                            _ints(cu_k, kind, B + 1), max_q, max_k, left, right, sinks, D ** -0.5 if scale is None else scale,
@@ -626,11 +629,14 @@ def znni_kv8_attn(q, kcodes, vcodes, scales, table, lens, max_len, left=None, si
 _rows_descriptor = struct.Struct("Pq").pack      # a znni_rows (data, row stride) as bytes
 
 
-def _rows(x, rows, cols, kind):
-    """The znni_rows of a [rows, cols] tensor of this kind whose last index is contiguous; None for None."""
+def _rows(x, shape, kind):
+    """The znni_rows of a [rows, columns] tensor of this shape and kind whose last index is contiguous; None for None."""
     if x is None:
         return None
-    assert x.shape == (rows, cols) and x.dtype == kind[1] and x.get_device() == kind[2], f"need {kind[1]} rows ({rows}, {cols}) on GPU {kind[2]}"
+    assert x.shape == shape and x.dtype == kind[1] and x.get_device() == kind[2], f"need {kind[1]} rows {tuple(shape)} on GPU {kind[2]}"
+    rows, cols = shape
+    if x.is_contiguous():
+        return _rows_descriptor(x.data_ptr(), cols)
     row, unit = x.stride()
     assert unit == 1 or cols < 2, "matrices are [rows, columns], columns contiguous"
     return _rows_descriptor(x.data_ptr(), row if rows > 1 else cols)
@@ -644,18 +650,8 @@ def _vector(x, n, kind):
     return x.data_ptr()
 
 
-def _new(x, *shape):
-    return torch.empty(shape, dtype=x.dtype, device=x.device)
-
-
-def _need(call, *args):
-    b = ctypes.c_size_t(0)
-    _check(call(*args, _byref(b)))
-    return b.value
-
-
 def znni_linear_workspace(dtype, M, N, K):
-    return _need(lib().znni_linear_workspace, _TYPES[dtype], int(M), int(N), int(K))
+    return _need(lib(), "znni_linear_workspace", _TYPES[dtype], int(M), int(N), int(K))
 
 
 def znni_linear(x, w, bias=None, act=None, residual=None, keep=False, out=None, workspace=None, stream=None):
@@ -664,18 +660,19 @@ def znni_linear(x, w, bias=None, act=None, residual=None, keep=False, out=None, 
     if stream is not None:
         return _on(stream, x, znni_linear, x, w, bias, act, residual, keep, out, workspace)
     kind = _kind(x)
-    M, K = x.shape
+    M, K = xs = x.shape
     N = w.shape[0]
-    out = _new(x, M, N) if out is None else out
-    z = None if keep is False else _new(x, M, N) if keep is True else keep
-    p, n, held = _scratch(_need(lib().znni_linear_workspace, kind[0], M, N, K), workspace, x)
-    _check(lib().znni_linear(kind[0], M, N, K, _rows(x, M, K, kind), _rows(w, N, K, kind), _vector(bias, N, kind), _ACTIVATIONS[act],
-                             _rows(residual, M, N, kind), _rows(z, M, N, kind), _rows(out, M, N, kind), p, n, _current(x)))
+    shape = (M, N)
+    out = x.new_empty(M, N) if out is None else out
+    z = None if keep is False else x.new_empty(M, N) if keep is True else keep
+    p, n, held = _scratch(_need(lib(), "znni_linear_workspace", kind[0], M, N, K), workspace, x)
+    _check(lib().znni_linear(kind[0], M, N, K, _rows(x, xs, kind), _rows(w, (N, K), kind), _vector(bias, N, kind), _ACTIVATIONS[act],
+                             _rows(residual, shape, kind), _rows(z, shape, kind), _rows(out, shape, kind), p, n, _current(x)))
     return out if z is None else (out, z)
 
 
 def znni_linear_backward_workspace(dtype, M, N, K, act=None, wanted=LINEAR_DX | LINEAR_DW | LINEAR_DBIAS):
-    return _need(lib().znni_linear_backward_workspace, _TYPES[dtype], int(M), int(N), int(K), _ACTIVATIONS[act], int(wanted))
+    return _need(lib(), "znni_linear_backward_workspace", _TYPES[dtype], int(M), int(N), int(K), _ACTIVATIONS[act], int(wanted))
 
 
 def znni_linear_backward(dout, x, w, z=None, act=None, bias=True, inputs=True, weights=True, dx=None, dw=None, dbias=None, workspace=None,
@@ -685,27 +682,27 @@ def znni_linear_backward(dout, x, w, z=None, act=None, bias=True, inputs=True, w
     if stream is not None:
         return _on(stream, dout, znni_linear_backward, dout, x, w, z, act, bias, inputs, weights, dx, dw, dbias, workspace)
     kind = _kind(dout)
-    M, N = dout.shape
-    K = w.shape[1]
-    dx = (_new(dout, M, K) if dx is None else dx) if inputs else None
-    dw = (_new(dout, N, K) if dw is None else dw) if weights else None
-    dbias = (_new(dout, N) if dbias is None else dbias) if bias else None
+    M, N = shape = dout.shape
+    K = (x if w is None else w).shape[1]
+    dx = (dout.new_empty(M, K) if dx is None else dx) if inputs else None
+    dw = (dout.new_empty(N, K) if dw is None else dw) if weights else None
+    dbias = (dout.new_empty(N) if dbias is None else dbias) if bias else None
     wanted = (LINEAR_DX if inputs else 0) | (LINEAR_DW if weights else 0) | (LINEAR_DBIAS if bias else 0)
     a = _ACTIVATIONS[act]
-    p, n, held = _scratch(_need(lib().znni_linear_backward_workspace, kind[0], M, N, K, a, wanted), workspace, dout)
-    _check(lib().znni_linear_backward(kind[0], M, N, K, _rows(dout, M, N, kind), _rows(x, M, K, kind), _rows(w, N, K, kind),
-                                      _rows(z, M, N, kind), a, _rows(dx, M, K, kind), _rows(dw, N, K, kind), _vector(dbias, N, kind), p, n,
+    p, n, held = _scratch(_need(lib(), "znni_linear_backward_workspace", kind[0], M, N, K, a, wanted), workspace, dout)
+    _check(lib().znni_linear_backward(kind[0], M, N, K, _rows(dout, shape, kind), _rows(x, (M, K), kind), _rows(w, (N, K), kind),
+                                      _rows(z, shape, kind), a, _rows(dx, (M, K), kind), _rows(dw, (N, K), kind), _vector(dbias, N, kind), p, n,
                                       _current(dout)))
     return dx, dw, dbias
 
 
-def _gate(gate, T, C, kind):
+def _gate(gate, shape, kind):
     """(whether one gate is for all tokens, its znni_rows)."""
     if gate is None:
         return 0, None
     if gate.dim() == 1:
-        return NORM_GATE_SHARED, _rows_descriptor(_vector(gate, C, kind), C)
-    return 0, _rows(gate, T, C, kind)
+        return NORM_GATE_SHARED, _rows_descriptor(_vector(gate, shape[1], kind), shape[1])
+    return 0, _rows(gate, shape, kind)
 
 
 def znni_block_norm(x, y=None, gate=None, post=None, pre=None, scale=1.0, eps=1e-5, centred=False, norm_post=True, norm_pre=True, h=None,
@@ -716,19 +713,19 @@ def znni_block_norm(x, y=None, gate=None, post=None, pre=None, scale=1.0, eps=1e
     if stream is not None:
         return _on(stream, x, znni_block_norm, x, y, gate, post, pre, scale, eps, centred, norm_post, norm_pre, h, z)
     kind = _kind(x)
-    T, C = x.shape
-    shared, dg = _gate(gate, T, C, kind)
+    T, C = shape = x.shape
+    shared, dg = _gate(gate, shape, kind)
     norm_post = norm_post and y is not None
     flags = (NORM_POST if norm_post else 0) | (NORM_PRE if norm_pre else 0) | (NORM_CENTRED if centred else 0) | shared
-    h = x if y is None else _new(x, T, C) if h is None else h
-    z = (_new(x, T, C) if z is None else z) if norm_pre else None
-    _check(lib().znni_block_norm(kind[0], T, C, _rows(x, T, C, kind), _rows(y, T, C, kind), dg, _vector(post, C, kind), _vector(pre, C, kind), scale, eps,
-                                 flags, _rows(h, T, C, kind) if y is not None else None, _rows(z, T, C, kind), _current(x)))
+    h = x if y is None else x.new_empty(T, C) if h is None else h
+    z = (x.new_empty(T, C) if z is None else z) if norm_pre else None
+    _check(lib().znni_block_norm(kind[0], T, C, _rows(x, shape, kind), _rows(y, shape, kind), dg, _vector(post, C, kind), _vector(pre, C, kind), scale, eps,
+                                 flags, _rows(h, shape, kind) if y is not None else None, _rows(z, shape, kind), _current(x)))
     return h, z
 
 
 def znni_block_norm_backward_workspace(dtype, T, C):
-    return _need(lib().znni_block_norm_backward_workspace, _TYPES[dtype], int(T), int(C), 0)
+    return _need(lib(), "znni_block_norm_backward_workspace", _TYPES[dtype], int(T), int(C), 0)
 
 
 def znni_block_norm_backward(dh, dz, h, y=None, gate=None, post=None, pre=None, scale=1.0, eps=1e-5, centred=False, norm_post=True,
@@ -738,19 +735,19 @@ def znni_block_norm_backward(dh, dz, h, y=None, gate=None, post=None, pre=None, 
     if stream is not None:
         return _on(stream, h, znni_block_norm_backward, dh, dz, h, y, gate, post, pre, scale, eps, centred, norm_post, norm_pre, dx, dy, dgate, dpost, dpre, workspace)
     kind = _kind(h)
-    T, C = h.shape
-    shared, dg = _gate(gate, T, C, kind)
+    T, C = shape = h.shape
+    shared, dg = _gate(gate, shape, kind)
     norm_post = norm_post and y is not None
     flags = (NORM_POST if norm_post else 0) | (NORM_PRE if norm_pre else 0) | (NORM_CENTRED if centred else 0) | shared
-    dx = _new(h, T, C) if dx is None else dx
-    dy = (_new(h, T, C) if dy is None else dy) if y is not None else None
-    dgate = (_new(h, *gate.shape) if dgate is None else dgate) if gate is not None else None
-    dpost = (_new(h, C) if dpost is None else dpost) if post is not None else None
-    dpre = (_new(h, C) if dpre is None else dpre) if pre is not None else None
+    dx = h.new_empty(T, C) if dx is None else dx
+    dy = (h.new_empty(T, C) if dy is None else dy) if y is not None else None
+    dgate = (h.new_empty(gate.shape) if dgate is None else dgate) if gate is not None else None
+    dpost = (h.new_empty(C) if dpost is None else dpost) if post is not None else None
+    dpre = (h.new_empty(C) if dpre is None else dpre) if pre is not None else None
     summed = shared or dpost is not None or dpre is not None
-    p, n, held = _scratch(_need(lib().znni_block_norm_backward_workspace, kind[0], T, C, flags) if summed else 0, workspace, h)
-    _check(lib().znni_block_norm_backward(kind[0], T, C, _rows(dh, T, C, kind), _rows(dz, T, C, kind), _rows(h, T, C, kind), _rows(y, T, C, kind), dg,
-                                          _vector(post, C, kind), _vector(pre, C, kind), scale, eps, flags, _rows(dx, T, C, kind),
-                                          _rows(dy, T, C, kind), _gate(dgate, T, C, kind)[1], _vector(dpost, C, kind), _vector(dpre, C, kind), p, n,
+    p, n, held = _scratch(_need(lib(), "znni_block_norm_backward_workspace", kind[0], T, C, flags) if summed else 0, workspace, h)
+    _check(lib().znni_block_norm_backward(kind[0], T, C, _rows(dh, shape, kind), _rows(dz, shape, kind), _rows(h, shape, kind), _rows(y, shape, kind), dg,
+                                          _vector(post, C, kind), _vector(pre, C, kind), scale, eps, flags, _rows(dx, shape, kind),
+                                          _rows(dy, shape, kind), _gate(dgate, shape, kind)[1], _vector(dpost, C, kind), _vector(dpre, C, kind), p, n,
                                           _current(h)))
     return dx, dy, dgate, dpost, dpre

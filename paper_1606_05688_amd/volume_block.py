@@ -1,4 +1,4 @@
-"""An attention block behind a convolutional stem, over the voxels of a volume as tokens.
+"""An attention block behind a convolutional stem, over the voxels of a volume as tokens, and a whole layer around it with its gradients.
 
     python -m paper_1606_05688_amd.volume_block
 
@@ -77,6 +77,64 @@ class VolumeBlock:
                     table[i] = -1                                 # no row will look there again
 
 
+class VolumeLayer:
+    """A layer of width C = Hq * D on tokens: attention between norms, with a gate on the way back into the stream, then two products
+    with an activation between them.  Random weights; `forward` returns what `backward` needs besides the result.
+
+        a = n(x) pre1,   y = attention(rotary(a wqkv^T + bqkv)) wo^T,   h = x + gate post n(y),   b = n(h) pre2,
+        out = h + gelu(b w1^T + b1) w2^T + b2
+    """
+
+    def __init__(self, Hq=8, Hk=2, D=32, hidden=4, sections=(6, 5, 5), dtype=torch.float32, device="cuda", seed=0):
+        g = torch.Generator(device=device).manual_seed(seed)
+        C = Hq * D
+
+        def normal(*shape, by=None, around=0.0):
+            by = shape[-1] ** -0.5 if by is None else by
+            return (around + by * torch.randn(shape, generator=g, device=device)).to(dtype)
+
+        self.Hq, self.Hk, self.D, self.sections = Hq, Hk, D, sections
+        self.freq = torch.cat([100.0 ** (-torch.arange(n, device=device) / n) for n in sections]).float()
+        self.weights = {"pre1": normal(C, by=0.1, around=1.0), "wqkv": normal((Hq + 2 * Hk) * D, C), "bqkv": normal((Hq + 2 * Hk) * D, by=0.1),
+                        "wo": normal(C, C), "gate": normal(C, by=0.1, around=0.5), "post": normal(C, by=0.1, around=1.0),
+                        "pre2": normal(C, by=0.1, around=1.0), "w1": normal(hidden * C, C), "b1": normal(hidden * C, by=0.1),
+                        "w2": normal(C, hidden * C), "b2": normal(C, by=0.1)}
+
+    def _heads(self, rows):
+        """Rows [T, (Hq + 2 Hk) D] as heads of queries, keys and values, where they lie."""
+        T, Hq, Hk, D = rows.shape[0], self.Hq, self.Hk, self.D
+        x = rows.view(T, Hq + 2 * Hk, D)
+        return x[:, :Hq], x[:, Hq:Hq + Hk], x[:, Hq + Hk:]
+
+    def forward(self, x, pos, cu, longest, **window):
+        """x [T, C], the sequences of cu [B + 1] one behind the other, pos [T, 3]; window: left, right, sinks of znni_attn_window."""
+        w = self.weights
+        a = znni.znni_block_norm(x, pre=w["pre1"])[1]
+        q, k, v = self._heads(znni.znni_linear(a, w["wqkv"], w["bqkv"]))
+        q, k = znni.znni_rope_axes(q, k, pos, self.freq, self.sections)
+        o, stats = znni.znni_attn_window(q, k, v, cu, cu, longest, longest, stats=True, **window)
+        y = znni.znni_linear(o.view(x.shape), w["wo"])
+        h, b = znni.znni_block_norm(x, y, gate=w["gate"], post=w["post"], pre=w["pre2"])
+        u, z = znni.znni_linear(b, w["w1"], w["b1"], act="gelu", keep=True)
+        return znni.znni_linear(u, w["w2"], w["b2"], residual=h), (x, pos, cu, longest, window, a, q, k, v, o, stats, y, h, b, u, z)
+
+    def backward(self, dout, kept):
+        """Gradients of x and, by name, of the weights."""
+        x, pos, cu, longest, window, a, q, k, v, o, stats, y, h, b, u, z = kept
+        w, d = self.weights, {}
+        du, d["w2"], d["b2"] = znni.znni_linear_backward(dout, u, w["w2"])
+        db, d["w1"], d["b1"] = znni.znni_linear_backward(du, b, w["w1"], z=z, act="gelu")
+        dh, dy, d["gate"], d["post"], d["pre2"] = znni.znni_block_norm_backward(dout, db, h, y, gate=w["gate"], post=w["post"], pre=w["pre2"])
+        do, d["wo"], _ = znni.znni_linear_backward(dy, o.view(x.shape), w["wo"], bias=False)
+        dqkv = x.new_empty(x.shape[0], (self.Hq + 2 * self.Hk) * self.D)
+        dq, dk, dv = self._heads(dqkv)
+        gq, gk, _ = znni.znni_attn_window_backward(do.view(o.shape), q, k, v, o, stats, cu, cu, longest, longest, dv=dv, **window)
+        znni.znni_rope_axes(gq, gk, -pos, self.freq, self.sections, out_q=dq, out_k=dk)          # turned back
+        da, d["wqkv"], d["bqkv"] = znni.znni_linear_backward(dqkv, a, w["wqkv"])
+        dx, _, _, _, d["pre1"] = znni.znni_block_norm_backward(dh, da, x, pre=w["pre1"])
+        return dx, d
+
+
 def main():
     block = VolumeBlock(dtype=torch.bfloat16)
     g = torch.Generator(device="cuda").manual_seed(1)
@@ -85,6 +143,13 @@ def main():
     parts = torch.cat(list(block.scan(volume, 1))).float()
     off = ((parts - whole).norm() / whole.norm()).item()
     print(f"{whole.shape[0]} voxels, {block.Hq} heads of {block.D}: plane by plane over the 8-bit cache, {100 * off:.1f} % off the whole volume's")
+    layer, n = VolumeLayer(dtype=torch.bfloat16), whole.shape[0]
+    x = whole.reshape(n, -1).to(torch.bfloat16)
+    pos = torch.stack(torch.meshgrid(*(torch.arange(e, device="cuda") for e in (32, 16, 16)), indexing="ij"), -1).reshape(n, 3).to(torch.int32)
+    out, kept = layer.forward(x, pos, torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, left=2 * 256, sinks=4)
+    dx, grads = layer.backward(out, kept)                          # of half the sum of squares
+    print(f"a layer of {sum(w.numel() for w in layer.weights.values())} weights on them: gradients of size {dx.float().norm().item():.3g} (tokens), "
+          + ", ".join(f"{g.float().norm().item():.3g} ({k})" for k, g in grads.items()))
 
 
 if __name__ == "__main__":
