@@ -54,6 +54,19 @@ struct Tile {
             for (int i = 0; i < PER; ++i) to_lds(base, at[i], to + i * THREADS * 16);
             return;
         }
+        if (plain && (!SUM_INNER || (end - k0) % EC == 0)) {
+            // the last steps, in whole chunks: direct loads of those that are there
+            const T* base = SUM_INNER ? s.p + row0 * s.ld + k0 : s.p + k0 * s.ld + row0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int slot = i * THREADS + t, j = slot / CR;
+                if (k0 + (SUM_INNER ? (slot % CR ^ swizzle(j)) * EC : j) < end)
+                    to_lds((const char*)base + at[i], lds_address(lds) + (unsigned)__builtin_amdgcn_readfirstlane(t >> 6) * 1024 + i * THREADS * 16);
+                else *(uint4*)(lds + slot * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            return;
+        }
         Chunk y[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
