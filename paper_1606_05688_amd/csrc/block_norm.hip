@@ -42,10 +42,7 @@ struct Row {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = column(lane, v);
-            if (c < C) y[v] = *(const V*)(p + c);
-            else
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) y[v][e] = (T)0.f;
+            y[v] = Loose<T, VEC>::load(p + c, C - c);
         }
     }
     __device__ static void clear(V (&y)[NV])
@@ -88,7 +85,7 @@ __device__ inline void moments(F first, G second, const NormArgs& a, bool one, b
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        const bool there = R::column(lane, i / VEC) < a.C;
+        const bool there = R::column(lane, i / VEC) + i % VEC < a.C;
         const float x = there ? first(i) - m.x : 0.f, y = there ? second(i) - m.y : 0.f;
         s.x = fmaf(x, x, s.x);
         s.y = fmaf(y, y, s.y);
@@ -135,11 +132,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows
             V o;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) o[e] = (T)s[v * VEC + e];
-            if (R::column(lane, v) < a.C) *(V*)(h.p + t * h.row + R::column(lane, v)) = o;
-            // (lanes past the row's end: whatever a mean taken off has left)
-            else
+            const int c = R::column(lane, v);
+            if (c < a.C) Loose<T, VEC>::store(h.p + t * h.row + c, o, a.C - c);
+            // (past the row's end: whatever a mean taken off has left)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s[v * VEC + e] = 0.f;
+            for (int e = 0; e < VEC; ++e) s[v * VEC + e] = c + e < a.C ? s[v * VEC + e] : 0.f;
         }
     }
     if (!a.pre) return;
@@ -156,7 +153,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(NormArgs a, Rows
             if (pre) n *= (float)w[v][e];
             o[e] = (T)n;
         }
-        *(V*)(z.p + t * z.row + R::column(lane, v)) = o;
+        Loose<T, VEC>::store(z.p + t * z.row + R::column(lane, v), o, a.C - R::column(lane, v));
     }
 }
 
@@ -187,7 +184,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
         if (p) R::load(w, p, lane, a.C);
         else
 #pragma unroll
-            for (int i = 0; i < E; ++i) w[i / VEC][i % VEC] = (T)(R::column(lane, i / VEC) < a.C ? 1.f : 0.f);
+            for (int i = 0; i < E; ++i) w[i / VEC][i % VEC] = (T)(R::column(lane, i / VEC) + i % VEC < a.C ? 1.f : 0.f);
     };
     weights(wq, pre);
     weights(wp, post);
@@ -215,7 +212,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
                 V o;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) o[e] = (T)at(v * VEC + e);
-                *(V*)(to.p + t * to.row + R::column(lane, v)) = o;
+                Loose<T, VEC>::store(to.p + t * to.row + R::column(lane, v), o, a.C - R::column(lane, v));
             }
         };
         float2 mean = {0.f, 0.f}, r = {1.f, 1.f};
@@ -319,40 +316,21 @@ static int norm_rows(int T, int W, bool sums)
 }
 
 template <typename T, typename F>
-static znni_status with_row(NormShape s, bool wide, F f)
+static znni_status with_row(NormShape s, F f)
 {
-    auto go = [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        if (s.E == 8) return s.W == 1 ? f(Row<T, V, 8, 1>()) : f(Row<T, V, 8, 4>());
-        return s.W == 1 ? f(Row<T, V, 32, 1>()) : s.W == 2 ? f(Row<T, V, 32, 2>()) : s.W == 4 ? f(Row<T, V, 32, 4>()) : f(Row<T, V, 32, 8>());
-    };
-    if (wide) go(std::integral_constant<int, 16 / sizeof(T)>());
-    else go(std::integral_constant<int, 1>());
+    constexpr int V = 16 / sizeof(T);
+    if (s.E == 8) s.W == 1 ? f(Row<T, V, 8, 1>()) : f(Row<T, V, 8, 4>());
+    else s.W == 1 ? f(Row<T, V, 32, 1>()) : s.W == 2 ? f(Row<T, V, 32, 2>()) : s.W == 4 ? f(Row<T, V, 32, 4>()) : f(Row<T, V, 32, 8>());
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }
 
 template <typename T, typename F>
-static znni_status with_back_row(NormShape s, bool wide, F f)
+static znni_status with_back_row(NormShape s, F f)
 {
-    auto go = [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        if (s.E == 8) return s.W == 1 ? f(Row<T, V, 8, 1>()) : s.W == 4 ? f(Row<T, V, 8, 4>()) : f(Row<T, V, 8, 8>());
-        return s.W == 8 ? f(Row<T, V, 16, 8>()) : f(Row<T, V, 16, 16>());
-    };
-    if (wide) go(std::integral_constant<int, 16 / sizeof(T)>());
-    else go(std::integral_constant<int, 1>());
+    constexpr int V = 16 / sizeof(T);
+    if (s.E == 8) s.W == 1 ? f(Row<T, V, 8, 1>()) : s.W == 4 ? f(Row<T, V, 8, 4>()) : f(Row<T, V, 8, 8>());
+    else s.W == 8 ? f(Row<T, V, 16, 8>()) : f(Row<T, V, 16, 16>());
     return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
-}
-
-template <typename T>
-static bool all_wide(int C, std::initializer_list<const znni_rows*> rows, std::initializer_list<const void*> vectors)
-{
-    if (C % (16 / (int)sizeof(T))) return false;
-    for (const znni_rows* r : rows)
-        if (r && !rows_wide(r->data, r->row, sizeof(T), 16)) return false;
-    for (const void* p : vectors)
-        if ((uintptr_t)p & 15u) return false;
-    return true;
 }
 
 template <typename T, int VEC, int E, int W, typename... A>
@@ -374,8 +352,7 @@ static znni_status norm_forward(NormArgs a, const znni_rows* x, const znni_rows*
     const dim3 grid = launch_of(((long long)a.T + a.per - 1) / a.per);
     Rows<const T> g = rows_of<const T>(gate);
     if (a.shared) g.row = 0;
-    const znni_rows one = {(void*)g.p, g.row};
-    return with_row<T>(norm_shape(a.T, a.C), all_wide<T>(a.C, {x, y, gate ? &one : nullptr, h, z}, {post, pre}), [&](auto row) {
+    return with_row<T>(norm_shape(a.T, a.C), [&](auto row) {
         launch_norm(row, grid, st, a, rows_of<const T>(x), rows_of<const T>(y), g, (const T*)post, (const T*)pre, rows_of<T>(h), rows_of<T>(z));
         return 0;
     });
@@ -388,7 +365,6 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
 {
     Rows<const T> g = rows_of<const T>(gate);
     if (a.shared) g.row = 0;
-    const znni_rows one = {(void*)g.p, g.row};
     const bool summed = a.shared && dgate;
     const int groups = a.T ? (int)(((long long)a.T + a.per - 1) / a.per) : 0;
     const size_t step = up((size_t)NORM_GROUPS * a.C * sizeof(float)) / sizeof(float);
@@ -407,8 +383,7 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
     sums.pre = wants(dpre, dpre);
     if (a.T > 0) {
         const Rows<T> dg = summed ? Rows<T>{nullptr, 0} : rows_of<T>(dgate);
-        const bool wide = all_wide<T>(a.C, {dh, dz, h, y, gate ? &one : nullptr, dx, dy, summed ? nullptr : dgate}, {post, pre});
-        const znni_status rc = with_back_row<T>(norm_back_shape(a.C), wide, [&](auto row) {
+        const znni_status rc = with_back_row<T>(norm_back_shape(a.C), [&](auto row) {
             launch_norm_back(row, launch_of(((long long)a.T + a.per - 1) / a.per), st, a, rows_of<const T>(dh), rows_of<const T>(dz), rows_of<const T>(h), rows_of<const T>(y), g,
                              (const T*)post, (const T*)pre, rows_of<T>(dx), rows_of<T>(dy), dg, sums);
             return 0;

@@ -75,62 +75,20 @@ struct End {
     T* z;
     T* out;
     long long residual_row, z_row, out_row;
-    bool wide, whole;           // four elements of every row are aligned, 16 bytes are
     float* parts;               // sums of a part of the steps, [split][M][Np], instead of all that
     int Np;
 };
 
-// Four consecutive elements of a row, of which n are there.
-template <typename T, int ACT>
-__device__ inline void end_four(const End<T>& d, long long m, int n, int there, float4 v)
+// N consecutive elements of a row, as far as they are there.
+template <typename T, int ACT, int N>
+__device__ inline void end_row(const End<T>& d, long long m, int n, int there, const float* v)
 {
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    float y[4] = {v.x, v.y, v.z, v.w};
-    const bool whole = d.wide && there >= 4;
-    T4 b = {}, r = {}, z, o;
-    if (whole) {
-        if (d.bias) b = *(const T4*)(d.bias + n);
-        if (d.residual) r = *(const T4*)(d.residual + m * d.residual_row + n);
-    } else {
+    using L = Loose<T, N>;
+    typename L::V b, r, z, o;
+    if (d.bias) b = L::load(d.bias + n, there);
+    if (d.residual) r = L::load(d.residual + m * d.residual_row + n, there);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (e >= there) break;
-            if (d.bias) b[e] = d.bias[n + e];
-            if (d.residual) r[e] = d.residual[m * d.residual_row + n + e];
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (d.bias) y[e] += (float)b[e];
-        z[e] = (T)y[e];
-        y[e] = activated<ACT>(y[e]);
-        if (d.residual) y[e] += (float)r[e];
-        o[e] = (T)y[e];
-    }
-    if (whole) {
-        if (d.z) *(T4*)(d.z + m * d.z_row + n) = z;
-        *(T4*)(d.out + m * d.out_row + n) = o;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (e >= there) break;
-            if (d.z) d.z[m * d.z_row + n + e] = z[e];
-            d.out[m * d.out_row + n + e] = o[e];
-        }
-    }
-}
-
-// 16 bytes of a row, all there and aligned.
-template <typename T, int ACT>
-__device__ inline void end_chunk(const End<T>& d, long long m, int n, const float* v)
-{
-    constexpr int EC = 16 / sizeof(T);
-    typedef T V __attribute__((ext_vector_type(EC)));
-    V b, r, z, o;
-    if (d.bias) b = *(const V*)(d.bias + n);
-    if (d.residual) r = *(const V*)(d.residual + m * d.residual_row + n);
-#pragma unroll
-    for (int e = 0; e < EC; ++e) {
+    for (int e = 0; e < N; ++e) {
         float y = v[e];
         if (d.bias) y += (float)b[e];
         z[e] = (T)y;
@@ -138,8 +96,14 @@ __device__ inline void end_chunk(const End<T>& d, long long m, int n, const floa
         if (d.residual) y += (float)r[e];
         o[e] = (T)y;
     }
-    if (d.z) *(V*)(d.z + m * d.z_row + n) = z;
-    *(V*)(d.out + m * d.out_row + n) = o;
+    if (d.z) L::store(d.z + m * d.z_row + n, z, there);
+    L::store(d.out + m * d.out_row + n, o, there);
+}
+template <typename T, int ACT>
+__device__ inline void end_four(const End<T>& d, long long m, int n, int there, float4 v)
+{
+    const float y[4] = {v.x, v.y, v.z, v.w};
+    end_row<T, ACT, 4>(d, m, n, there, y);
 }
 
 // ---- products over tiles --------------------------------------------------------------------------------------------
@@ -281,13 +245,7 @@ __global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductAr
 #pragma unroll
             for (int e = 0; e < EC / 4; ++e) v[e] = mine[r * CHUNKS + ((c / 4 + e) ^ (r & (CHUNKS - 1)))];
             if (m >= a.M || col >= a.N) continue;
-            if (d.whole && col + EC <= a.N) {
-                end_chunk<T, ACT>(d, m, col, (const float*)v);
-            } else {
-#pragma unroll
-                for (int e = 0; e < EC / 4; ++e)
-                    if (col + 4 * e < a.N) end_four<T, ACT>(d, m, col + 4 * e, a.N - col - 4 * e, v[e]);
-            }
+            end_row<T, ACT, EC>(d, m, col, a.N - col, (const float*)v);
         }
     }
 }
@@ -328,7 +286,7 @@ constexpr int FEW_WAVES = 8;
 template <typename T, int MB, int ACT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void k_few(ProductArgs a, Side<T> w, Side<T> x, End<T> d)
 {
-    constexpr int EC = 16 / sizeof(T), STEP = 4 * EC, AHEAD = MB == 1 ? 8 : 4;
+    constexpr int EC = 16 / sizeof(T), STEP = 4 * EC, AHEAD = MB == 1 ? 8 : MB == 2 ? 4 : 2;
     typedef typename Mfma<T>::V V;
     __shared__ f32x4 sums[FEW_WAVES][MB][64];
     const long long group = group_id();
@@ -345,26 +303,20 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_few(ProductArgs a, Side<T> w
     f32x4 acc[MB] = {};
     for (int k = k0; k < k1; k += STEP * AHEAD) {
         V y[AHEAD], z[MB][AHEAD];
-        if (w.wide && x.wide && k + STEP * AHEAD <= k1) {
+        if (k + STEP * AHEAD <= k1) {
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) {
-                y[s] = *(const V*)(wp + k + s * STEP);
+                y[s] = Loose<T, EC>::load(wp + k + s * STEP);
 #pragma unroll
-                for (int j = 0; j < MB; ++j) z[j][s] = *(const V*)(xp[j] + k + s * STEP);
+                for (int j = 0; j < MB; ++j) z[j][s] = Loose<T, EC>::load(xp[j] + k + s * STEP);
             }
         } else {
 #pragma unroll
             for (int s = 0; s < AHEAD; ++s) {
                 const int there = k1 - (k + s * STEP + c);
-                auto bring = [&](V& to, const T* p, bool wide) {
-                    if (wide && there >= EC) to = *(const V*)(p + k + s * STEP);
-                    else
+                y[s] = Loose<T, EC>::load(wp + k + s * STEP, there);
 #pragma unroll
-                        for (int e = 0; e < EC; ++e) to[e] = e < there ? p[k + s * STEP + e] : (T)0.f;
-                };
-                bring(y[s], wp, w.wide);
-#pragma unroll
-                for (int j = 0; j < MB; ++j) bring(z[j][s], xp[j], x.wide);
+                for (int j = 0; j < MB; ++j) z[j][s] = Loose<T, EC>::load(xp[j] + k + s * STEP, there);
             }
         }
 #pragma unroll
@@ -420,10 +372,13 @@ static ProductPlan product_plan(int type, int M, int N, int K, bool both_inner)
     const long long r2 = 100 * ((tiles(256) + 255) / 256), r1 = 57 * ((tiles(128) + 511) / 512);
     p.kind = tiles(128) < 256 ? 0 : type != ZNNI_F32 && r2 <= r1 + r1 / 20 ? 2 : 1;
     const long long n = tiles(64 << p.kind), steps = ((long long)K + bk - 1) / bk;
+    // Few tiles: workgroups share the steps, if that saves more than the second launch costs: a step takes 0.6 us (fp32 1.2) where a compute unit has
+    // one workgroup, joining the parts 4.5 (bf16, 336 columns, 400 steps of the sum, 1300 rows: 9.3 us with four parts, 6.0 with one); where rows
+    // of odd lengths come by way of registers, three times that.
     long long s = p.kind == 0 && n < 256 ? 512 / (n ? n : 1) : 1;
     if (s > steps / 2) s = steps / 2;
     if (s > SPLITS_MOST) s = SPLITS_MOST;
-    if (s < 1) s = 1;
+    if (s < 1 || (steps - steps / s) * (type == ZNNI_F32 ? 12 : 6) * (K % (bk / 8) || N % (bk / 8) ? 3 : 1) < 45) s = 1;
     p.per = (int)((steps + s - 1) / s * bk);
     p.splits = K ? (int)(((long long)K + p.per - 1) / p.per) : 1;
     p.parts = p.splits > 1 ? (size_t)p.splits * M * ((N + 3) / 4 * 4) : 0;
@@ -441,7 +396,8 @@ static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> rig
         if (p.kind < 0) {
             const dim3 grid = launch_of((long long)((N + 15) / 16) * p.splits), block(64 * FEW_WAVES);
             if (M <= 16) k_few<T, 1, ACT><<<grid, block, 0, st>>>(a, left, right, d);
-            else k_few<T, 2, ACT><<<grid, block, 0, st>>>(a, left, right, d);
+            else if (M <= 32) k_few<T, 2, ACT><<<grid, block, 0, st>>>(a, left, right, d);
+            else k_few<T, 4, ACT><<<grid, block, 0, st>>>(a, left, right, d);
         }
     }
     if (p.kind >= 0) {
@@ -465,11 +421,12 @@ constexpr int SLOPE_ROWS = 8;             // rows of a workgroup at a time
 constexpr int SLOPE_PARTS = 256;          // parts of a sum over all tokens at most
 
 // dz = dout act'(z) (written if there is an activation), and its sum over `per` rows, 32 chunks of columns by 8 rows a workgroup.
-template <typename T, int ACT, int VEC>
+template <typename T, int ACT>
 __global__ __launch_bounds__(256) void k_slope(int M, int N, int per, const T* __restrict__ dout, long long dout_row, const T* __restrict__ z,
                                                long long z_row, T* __restrict__ dz, int dz_row, float* __restrict__ sums)
 {
-    typedef T V __attribute__((ext_vector_type(VEC)));
+    constexpr int VEC = 16 / sizeof(T);
+    using L = Loose<T, VEC>;
     __shared__ float part[SLOPE_ROWS][32 * VEC];
     const int c = threadIdx.x & 31, r = threadIdx.x >> 5, n = ((int)blockIdx.x * 32 + c) * VEC;
     const int m0 = (int)blockIdx.y * per, m1 = (int)min((long long)M, (long long)m0 + per);
@@ -478,17 +435,17 @@ __global__ __launch_bounds__(256) void k_slope(int M, int N, int per, const T* _
     for (int e = 0; e < VEC; ++e) s[e] = 0.f;
     if (n < N)
         for (int m = m0 + r; m < m1; m += SLOPE_ROWS) {
-            V g = *(const V*)(dout + m * dout_row + n);
+            const typename L::V g = L::load(dout + m * dout_row + n, N - n);
             if constexpr (ACT != ZNNI_ACT_NONE) {
-                const V y = *(const V*)(z + m * z_row + n);
-                V o;
+                const typename L::V y = L::load(z + m * z_row + n, N - n);
+                typename L::V o;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const float f = (float)g[e] * slope<ACT>((float)y[e]);
                     s[e] += f;
                     o[e] = (T)f;
                 }
-                *(V*)(dz + (long long)m * dz_row + n) = o;
+                *(typename L::V*)(dz + (long long)m * dz_row + n) = o;           // (rows of dz are padded)
             } else {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) s[e] += (float)g[e];
@@ -556,8 +513,6 @@ static End<T> end_of(const znni_rows* out)
     End<T> d = {};
     d.out = (T*)out->data;
     d.out_row = out->row;
-    d.wide = rows_wide(out->data, out->row, sizeof(T), 4 * sizeof(T));
-    d.whole = rows_wide(out->data, out->row, sizeof(T), 16);
     return d;
 }
 
@@ -566,22 +521,15 @@ static znni_status forward(int M, int N, int K, const znni_rows* x, const znni_r
                            const znni_rows* z, const znni_rows* out, void* workspace, hipStream_t st)
 {
     End<T> d = end_of<T>(out);
-    const int four = 4 * sizeof(T);
     d.bias = (const T*)bias;
-    d.wide = d.wide && !((uintptr_t)bias % four);
-    d.whole = d.whole && !((uintptr_t)bias & 15u);
     if (residual) {
         d.residual = (const T*)residual->data;
         d.residual_row = residual->row;
-        d.wide = d.wide && rows_wide(residual->data, residual->row, sizeof(T), four);
-        d.whole = d.whole && rows_wide(residual->data, residual->row, sizeof(T), 16);
-    }
+            }
     if (z) {
         d.z = (T*)z->data;
         d.z_row = z->row;
-        d.wide = d.wide && rows_wide(z->data, z->row, sizeof(T), four);
-        d.whole = d.whole && rows_wide(z->data, z->row, sizeof(T), 16);
-    }
+            }
     d.parts = (float*)workspace;
     return with_act(act, [&](auto k) {
         return launch_product<T, true, true, decltype(k)::value>(M, N, K, side_of<T>(w, N), side_of<T>(x, M), d, st);
@@ -602,14 +550,10 @@ static znni_status backward(int type, int M, int N, int K, const znni_rows* dout
         const int n = slope_parts(M, N), per = (int)(((long long)M + n - 1) / n);
         const T* y = z ? (const T*)z->data : nullptr;
         const long long yr = z ? z->row : 0;
-        constexpr int WIDE = 16 / sizeof(T);
-        const bool wide = N % WIDE == 0 && rows_wide(dout->data, dout->row, sizeof(T), 16) && (!z || rows_wide(y, yr, sizeof(T), 16));
         with_act(act, [&](auto k) {
-            constexpr int ACT = decltype(k)::value;
-            const int across = wide ? 32 * WIDE : 32;
+            constexpr int ACT = decltype(k)::value, across = 32 * 16 / sizeof(T);
             const dim3 grid((unsigned)((N + (long long)across - 1) / across), (unsigned)n);
-            if (wide) k_slope<T, ACT, WIDE><<<grid, dim3(256), 0, st>>>(M, N, per, (const T*)dout->data, dout->row, y, yr, dz, p.dz_row, sums);
-            else k_slope<T, ACT, 1><<<grid, dim3(256), 0, st>>>(M, N, per, (const T*)dout->data, dout->row, y, yr, dz, p.dz_row, sums);
+            k_slope<T, ACT><<<grid, dim3(256), 0, st>>>(M, N, per, (const T*)dout->data, dout->row, y, yr, dz, p.dz_row, sums);
             return 0;
         });
         if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;

@@ -1,6 +1,7 @@
 // product_tile.h -- tiles of two matrices in LDS and their product on the matrix cores, for sums over either index of each.
 #pragma once
 #include "attn_tile.h"
+#include "rows_common.h"
 
 namespace znni {
 
@@ -11,7 +12,7 @@ struct Side {
     const T* p;
     long long ld;
     int rows;
-    bool wide;            // 16-byte loads from whole chunks: address and rows are aligned
+    bool wide;            // direct loads of 16 bytes: address and rows are aligned
 };
 
 // ROWS rows by BK steps of the sum in LDS, in chunks of 16 bytes.  SUM_INNER: rows of 8 chunks along the sum; else BK rows of the
@@ -75,12 +76,7 @@ struct Tile {
             const T* p = SUM_INNER ? s.p + r * s.ld + k : s.p + k * s.ld + r;
             // how many elements are there
             const int n = SUM_INNER ? (r < s.rows ? end - k : 0) : (k < end ? s.rows - r : 0);
-            if (n >= EC && s.wide) {
-                y[i] = *(const Chunk*)p;
-            } else {
-#pragma unroll
-                for (int e = 0; e < EC; ++e) y[i][e] = e < n ? p[e] : (T)0.f;
-            }
+            y[i] = Loose<T, EC>::load(p, n);
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) *(Chunk*)(lds + (i * THREADS + t) * 16) = y[i];

@@ -8,6 +8,34 @@ constexpr int ROWS_MOST = 1 << 30, COLS_MOST = 1 << 26;
 
 static inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
+// N elements that begin anywhere an element may: one access, which the hardware takes at any address (16 bytes apart it is the faster).
+template <typename T, int N>
+struct Loose {
+    typedef T V __attribute__((ext_vector_type(N)));
+    typedef T Anywhere __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    __device__ static V load(const T* p) { return *(const Anywhere*)p; }
+    __device__ static void store(T* p, V y) { *(Anywhere*)p = y; }
+    // Those of them that are there, zeros for others.
+    __device__ static V load(const T* p, int there)
+    {
+        if (there >= N) return load(p);
+        V y;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = e < there ? p[e] : (T)0.f;
+        return y;
+    }
+    __device__ static void store(T* p, V y, int there)
+    {
+        if (there >= N) {
+            store(p, y);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < there) p[e] = y[e];
+    }
+};
+
 // Whether rows are aligned to `bytes`.
 static inline bool rows_wide(const void* p, long long row, int size, int bytes)
 {
