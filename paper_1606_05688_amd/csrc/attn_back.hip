@@ -188,26 +188,33 @@ __device__ inline bool finite_of(T x)
 enum { BACK_DQ = 0, BACK_DK = 1, BACK_DV = 2 };
 
 // WHAT & (BACK_DK | BACK_DV): lanes are keys, the walk is over rows; else lanes are rows, the walk is over keys.
+template <typename T, int NC>
+struct BackMemory {
+    typedef typename RowNumber<T>::type Number;
+    static constexpr int RT = BackTile<T, NC>::RT;
+    __align__(1024) char as[2][BackTile<T, NC>::BYTES];
+    __align__(1024) char bs[2][BackTile<T, NC>::BYTES];
+    __align__(16) Number rc[2][2 * RT + 4];                          // of the rows walked; then zeros
+    __align__(16) int odds[4];
+};
+
 // TWICE (16-bit types): weights and their gradients as two values of the type.
 template <typename T, int NC, int WHAT, bool TWICE>
-__global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(BackArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v,
-                                                                              Heads<const T> dout, Heads<T> da, Heads<T> db)
+__device__ __forceinline__ void back_walk(const BackArgs& a, const int group, BackMemory<T, NC>& memory, Heads<const T> q, Heads<const T> k,
+                                          Heads<const T> v, Heads<const T> dout, Heads<T> da, Heads<T> db)
 {
     constexpr bool KEYS = WHAT != BACK_DQ, SUM_A = WHAT != BACK_DV, SUM_B = WHAT & BACK_DV;
     using G = BackTile<T, NC>;
     using M = Mfma<T>;
     constexpr bool F32 = G::F32;
     constexpr int RT = G::RT, EC = G::EC, RS = G::RS, CR = G::CR, PER = G::PER, QS = F32 ? 4 * NC : 2 * NC;
-    __shared__ __align__(1024) char as[2][G::BYTES];
-    __shared__ __align__(1024) char bs[2][G::BYTES];
     using N = RowNumber<T>;
     typedef typename N::type Number;
-    __shared__ __align__(16) int odds[4];
-    __shared__ __align__(1024) Number rc[2][KEYS ? 2 * RT + 4 : 1];  // of the rows walked; then zeros
+    auto& as = memory.as;
+    auto& bs = memory.bs;
+    auto& odds = memory.odds;
+    auto& rc = memory.rc;
 
-    const long long all_groups = group_id();
-    if (all_groups >= a.groups) return;
-    const int group = (int)all_groups;                              // (fits: checked by the host)
     const int t = threadIdx.x, l = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c32 = l & 31, h = l >> 5;
     // far workgroups of all heads first: others have the chip to the end
     const int shared = a.Hq / a.Hk, fars = a.far_tiles * a.far, per_head = a.tiles * a.splits, heads = a.heads;
@@ -654,13 +661,31 @@ __global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(B
     if constexpr (SUM_B) put(db, acc_b, F16 ? 1.f / (1 << WEIGHT_POWER) : 1.f, 1);
 }
 
+// All walks of a call at once, since none waits for another: keys' (dk and dv together, or one after the other), then rows'.  16-bit types, wide heads:
+// sums of both gradients would leave a SIMD one wave (bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 2700 us at once, 850 and 660 apart, the
+// scores twice).
+template <typename T, int NC, bool TWICE>
+__global__ __launch_bounds__(BACK_THREADS, sizeof(T) == 4 ? 1 : 2) void k_back(BackArgs ak, BackArgs aq, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+                                                                              Heads<const T> dout, Heads<T> dq, Heads<T> dk, Heads<T> dv)
+{
+    __shared__ BackMemory<T, NC> memory;
+    const long long group = group_id();
+    constexpr bool APART = sizeof(T) == 2 && NC > 2;
+    const long long keys = APART ? 2 * ak.groups : ak.groups;
+    if (group >= keys + aq.groups) return;
+    if (group >= keys) back_walk<T, NC, BACK_DQ, TWICE>(aq, (int)(group - keys), memory, q, k, v, dout, dq, dq);
+    else if constexpr (!APART) back_walk<T, NC, BACK_DK | BACK_DV, TWICE>(ak, (int)group, memory, q, k, v, dout, dk, dv);
+    else if (group < ak.groups) back_walk<T, NC, BACK_DK, TWICE>(ak, (int)group, memory, q, k, v, dout, dk, dv);
+    else back_walk<T, NC, BACK_DV, TWICE>(ak, (int)(group - ak.groups), memory, q, k, v, dout, dk, dv);
+}
+
 // Sums of the parts of a tile: 32 lanes a key (or row), four elements a lane.
 template <typename T, bool KEYS>
-__global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles, Heads<T> da, Heads<T> db)
+__device__ __forceinline__ void back_join(const BackArgs& a, const int id, int tiles, Heads<T> da, Heads<T> db)
 {
     const int d = (threadIdx.x & 31) * 4, shared = a.Hq / a.Hk, across = tiles * (BACK_LANES / 8);
-    const int id = (int)group_id(), bh = id / across, b = bh / a.Hk, hk = bh - b * a.Hk, x = (id - bh * across) * 8 + (threadIdx.x >> 5);
-    if (b >= B || d >= a.D) return;
+    const int bh = id / across, b = bh / a.Hk, hk = bh - b * a.Hk, x = (id - bh * across) * 8 + (threadIdx.x >> 5);
+    if (d >= a.D) return;
     const int x0 = KEYS ? a.cu_k[b] : a.cu_q[b];
     const int count = KEYS ? min(a.cu_k[b + 1] - x0, a.max_k) : min(a.cu_q[b + 1] - x0, a.max_q) * shared;
     if (x >= count) return;
@@ -691,6 +716,16 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs a, int B, int tiles,
         T* const y = KEYS ? to.row(x0 + x, hk) : to.row(x0 + x / shared, hk * shared + x % shared);
         *(T4*)(y + d) = T4{(T)s.x, (T)s.y, (T)s.z, (T)s.w};
     }
+}
+
+// Tiles of keys and of rows whose sums are in parts.
+template <typename T>
+__global__ __launch_bounds__(256) void k_back_join(BackArgs ak, BackArgs aq, int tiles_k, int tiles_q, Heads<T> dq, Heads<T> dk, Heads<T> dv)
+{
+    const long long id = group_id(), keys = (long long)tiles_k * (BACK_LANES / 8) * ak.heads, all = keys + (long long)tiles_q * (BACK_LANES / 8) * aq.heads;
+    if (id >= all) return;
+    if (id < keys) back_join<T, true>(ak, (int)id, tiles_k, dk, dv);
+    else back_join<T, false>(aq, (int)(id - keys), tiles_q, dq, dq);
 }
 
 constexpr int BACK_TWICE = 512;            // keys that a row sees at most for weights to be two values
@@ -758,13 +793,11 @@ static BackSizes back_sizes(int type, int B, int Hq, int Hk, int D, int max_q, i
     s.rows = PEAKS * sizeof(float2) + ((size_t)2 * B * Hk * s.pitch * (type == ZNNI_F32 ? sizeof(float) : sizeof(Pieces)) + 255) & ~(size_t)255;
     const size_t p0 = back_plan(true, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
     const size_t p1 = back_plan(false, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
-    s.parts = (p0 > p1 ? p0 : p1) * sizeof(float);
+    s.parts = (p0 + p1) * sizeof(float);
     return s;
 }
 
-template <typename T, bool KEYS>
-static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> dout,
-                                Heads<T> da, Heads<T> db, hipStream_t st)
+static BackArgs planned(BackArgs a, const BackPlan& p, float* parts)
 {
     a.tiles = p.tiles;
     a.splits = p.splits;
@@ -773,48 +806,8 @@ static znni_status launch_walks(BackArgs a, const BackPlan& p, int B, Heads<cons
     a.far_tiles = p.far_tiles;
     a.far = p.far;
     a.groups = p.groups;
-    if (p.groups == 0) return ZNNI_OK;
-    const dim3 grid = launch_of(p.groups), block(BACK_THREADS);
-    auto launch_as = [&](auto what, auto doubled) {
-        constexpr bool TWICE = decltype(doubled)::value;
-        constexpr int WHAT = decltype(what)::value;
-        constexpr bool NARROW = WHAT == BACK_DQ || WHAT == (BACK_DK | BACK_DV), WIDE = sizeof(T) == 4 || WHAT != (BACK_DK | BACK_DV);   // (what calls reach)
-        switch ((a.D + 31) / 32) {
-            case 1: if constexpr (NARROW) k_back<T, 1, WHAT, TWICE><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-            case 2: if constexpr (NARROW) k_back<T, 2, WHAT, TWICE><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-            case 3: if constexpr (WIDE) k_back<T, 3, WHAT, TWICE><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-            default: if constexpr (WIDE) k_back<T, 4, WHAT, TWICE><<<grid, block, 0, st>>>(a, q, k, v, dout, da, db); break;
-        }
-    };
-    // Rounding dS to 16 bits costs as much as rounding the result, and rows of few keys get as much again from `out`, whose rounding is in delta.  Where
-    // rows see few keys, products are few too: dS and P as two values there.  (fp16, ragged 300 tokens, window of 100: error 0.00031 of the result
-    // and 0.00021 where products in fp32 leave 0.00021.)
-    auto launch = [&](auto what) {
-        if constexpr (sizeof(T) == 2) {
-            if (p.twice) launch_as(what, std::true_type());
-            else launch_as(what, std::false_type());
-        } else {
-            launch_as(what, std::false_type());
-        }
-    };
-    // 16-bit types, wide heads: sums of both gradients leave a SIMD one wave; one at a time, at the cost of the scores again, two (bf16, 16384
-    // tokens, window of 4096, heads 16 of 4 x 128: 2700 us at once, XXX one after the other).
-    if constexpr (!KEYS) {
-        launch(std::integral_constant<int, BACK_DQ>());
-    } else {
-        if constexpr (sizeof(T) == 2) {
-            if (a.D > 64) {
-                launch(std::integral_constant<int, BACK_DK>());
-                launch(std::integral_constant<int, BACK_DV>());
-            }
-        }
-        if (sizeof(T) == 4 || a.D <= 64) launch(std::integral_constant<int, BACK_DK | BACK_DV>());
-    }
-    if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    const int tiles = p.splits > 1 ? p.tiles : p.first_tiles;
-    if (!tiles) return ZNNI_OK;
-    k_back_join<T, KEYS><<<launch_of((long long)tiles * (BACK_LANES / 8) * a.Hk * B), dim3(256), 0, st>>>(a, B, tiles, da, db);
-    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+    a.parts = parts;
+    return a;
 }
 
 template <typename T>
@@ -834,9 +827,33 @@ static znni_status launch_back(BackArgs a, int type, int B, const znni_heads* q,
     }
     const BackPlan pk = back_plan(true, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
     const BackPlan pq = back_plan(false, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
-    const znni_status rc = launch_walks<T, true>(a, pk, B, qi, ki, vi, gi, heads_of<T>(dk), heads_of<T>(dv), st);
-    if (rc) return rc;
-    return launch_walks<T, false>(a, pq, B, qi, ki, vi, gi, heads_of<T>(dq), heads_of<T>(dq), st);
+    const BackArgs ak = planned(a, pk, a.parts), aq = planned(a, pq, a.parts + pk.parts);
+    const Heads<T> oq = heads_of<T>(dq), ok = heads_of<T>(dk), ov = heads_of<T>(dv);
+    const int NC = (a.D + 31) / 32;
+    const dim3 grid = launch_of((sizeof(T) == 2 && NC > 2 ? 2 : 1) * pk.groups + pq.groups), block(BACK_THREADS);
+    // Rounding dS to 16 bits costs as much as rounding the result, and rows of few keys get as much again from `out`, whose rounding is in delta.  Where
+    // rows see few keys, products are few too: dS and P as two values there.  (fp16, ragged 300 tokens, window of 100: error 0.00031 of the result
+    // and 0.00022, where products in fp32 leave 0.00021; 56 us and 64.)
+    auto launch = [&](auto doubled) {
+        constexpr bool TWICE = decltype(doubled)::value;
+        switch (NC) {
+            case 1: k_back<T, 1, TWICE><<<grid, block, 0, st>>>(ak, aq, qi, ki, vi, gi, oq, ok, ov); break;
+            case 2: k_back<T, 2, TWICE><<<grid, block, 0, st>>>(ak, aq, qi, ki, vi, gi, oq, ok, ov); break;
+            case 3: k_back<T, 3, TWICE><<<grid, block, 0, st>>>(ak, aq, qi, ki, vi, gi, oq, ok, ov); break;
+            default: k_back<T, 4, TWICE><<<grid, block, 0, st>>>(ak, aq, qi, ki, vi, gi, oq, ok, ov); break;
+        }
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (pk.twice) launch(std::true_type());
+        else launch(std::false_type());
+    } else {
+        launch(std::false_type());
+    }
+    if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+    const int tk = pk.splits > 1 ? pk.tiles : pk.first_tiles, tq = pq.splits > 1 ? pq.tiles : 0;
+    if (!tk && !tq) return ZNNI_OK;
+    k_back_join<T><<<launch_of((long long)(tk + tq) * (BACK_LANES / 8) * a.heads), dim3(256), 0, st>>>(ak, aq, tk, tq, oq, ok, ov);
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
 }
 
 static znni_status back_shape(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks)
@@ -850,8 +867,11 @@ static znni_status back_shape(int type, int B, int Hq, int Hk, int D, int max_q,
     if (rows > most || max_k > most) return ZNNI_ERR_SHAPE;
     const long long tiles = ((rows > max_k ? rows : max_k) + BACK_LANES - 1) / BACK_LANES;
     if (tiles * Hk > INT_MAX / (B ? B : 1)) return ZNNI_ERR_SHAPE;
-    for (const bool keys : {false, true})
-        if (back_plan(keys, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).groups > INT_MAX) return ZNNI_ERR_SHAPE;
+    for (const bool keys : {false, true}) {
+        const BackPlan p = back_plan(keys, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks);
+        const long long joined = (long long)(p.splits > 1 ? p.tiles : p.first_tiles) * (BACK_LANES / 8) * Hk * B;
+        if (p.groups > INT_MAX || joined > INT_MAX) return ZNNI_ERR_SHAPE;
+    }
     return ZNNI_OK;
 }
 
