@@ -251,3 +251,67 @@ def test_against_differences():
         off = abs((f[1] - f[0]).item() * 2.0 ** 6 - (grad.double() * way.double()).sum().item())
         # third derivatives: at most some ten times (scale |q| |way|)^3 of a row of values up to 4; sums of 960 results, each off by 2^-21
         assert off <= dout.abs().sum().item() * 4 * (10 * 4.0 ** 3 * 2.0 ** -14 / 6 + 2.0 ** -21 * 2.0 ** 6)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tokens_far_apart(dtype):
+    """Strides past what 32-bit offsets hold within a tile, tokens past 2^31 elements."""
+    lens = [(600, 600)]
+    (q, k, v, dout), where = make(lens, 2, 2, 32, dtype, 12)
+    out, stats, got = call((q, k, v, dout), where, 100, 0, 2)
+
+    def apart(x):
+        y = torch.empty_strided(x.shape, ((1 << 22) + 64, 32, 1), dtype=dtype, device="cuda")
+        return y.copy_(x)
+
+    for i in range(3):                               # keys and values, queries and the result's gradient, what is written
+        a = [apart(x) if (i == 0 and n in (1, 2)) or (i == 1 and n in (0, 3)) else x for n, x in enumerate((q, k, v, dout))]
+        kw = dict(dq=apart(q), dk=apart(k), dv=apart(v)) if i == 2 else {}
+        again = B.znni_attn_window_backward(a[3], *a[:3], out, stats, *where, left=100, sinks=2, **kw)
+        assert all(torch.equal(x, y) for x, y in zip(again, got))
+        del a, kw, again
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tokens_and_heads_backwards(dtype):
+    """Strides below zero, in what is read."""
+    lens, Hq, Hk, D = [(70, 70), (40, 90)], 4, 2, 40
+    (q, k, v, dout), (cu_q, cu_k, mq, mk) = make(lens, Hq, Hk, D, dtype, 13)
+    out, stats, got = call((q, k, v, dout), (cu_q, cu_k, mq, mk), 30, 2, 3)
+    size = q.element_size()
+    held = []
+
+    def backwards(x):
+        y = x.flip(0, 1).contiguous()
+        held.append(y)
+        T, H, _ = x.shape
+        return B._descriptor(y.data_ptr() + (T * H - 1) * D * size, -H * D, -D)
+
+    new = [torch.empty_like(x) for x in (q, k, v)]
+    there = [B._descriptor(x.data_ptr(), x.shape[1] * D, D) for x in new]
+    ws = torch.empty(B.znni_attn_window_backward_workspace(dtype, 2, Hq, Hk, D, mq, mk, 30, 2, 3), dtype=torch.uint8, device="cuda")
+    status = B.lib().znni_attn_window_backward(B._TYPES[dtype], 2, Hq, Hk, D, backwards(q), backwards(k), backwards(v), backwards(out), stats.data_ptr(),
+                                               backwards(dout), cu_q.data_ptr(), cu_k.data_ptr(), mq, mk, 30, 2, 3, D ** -0.5, *there, ws.data_ptr(),
+                                               ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert status == 0
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(new, got))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_fewer_rows_and_keys_than_the_call_says(dtype):
+    """max_q and max_k are bounds: larger ones change the launch, not the result's meaning; rows past a smaller max_q take no part."""
+    lens = [(50, 80), (3, 3)]
+    tensors, (cu_q, cu_k, mq, mk) = make(lens, 4, 2, 64, dtype, 14)
+    out, stats, _ = call(tensors, (cu_q, cu_k, mq, mk), 20, 0, 2)
+    q, k, v, dout = tensors
+    got = B.znni_attn_window_backward(dout, q, k, v, out, stats, cu_q, cu_k, 5000, 9000, left=20, sinks=2)
+    compare(lens, tensors, 20, 0, 2, got)
+
+
+def test_a_call_of_keys_without_rows():
+    for dtype in TYPES:
+        (q, k, v, dout), where = make([(0, 70), (0, 0), (0, 5)], 2, 1, 64, dtype, 15)
+        out, stats, got = call((q, k, v, dout), where, 5, 0, 3)
+        assert got[0].shape == (0, 2, 64) and (got[1] == 0).all() and (got[2] == 0).all()

@@ -186,3 +186,49 @@ def test_gradients_against_differences():
             # second differences: a third derivative of order 1 times step^2, sums of 54 fp32 results over the step
             size = (dout.abs().sum() * way.abs().sum()).item()
             assert abs((f[1] - f[0]).item() * 2.0 ** 5 - (dt.double() * way.double()).sum().item()) <= size * (2.0 ** -12 + 2.0 ** -24 * 20 * 2.0 ** 6)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_far_apart(dtype):
+    """Row strides past what 32-bit offsets hold within a tile, elements past 2^31."""
+    M, N, K = 600, 72, 40
+    x, w, bias, residual, dout = inputs(M, N, K, dtype, 12)
+    far = torch.empty_strided((M, K), (1 << 22, 1), dtype=dtype, device="cuda").copy_(x)
+    assert torch.equal(B.znni_linear(far, w, bias), B.znni_linear(x, w, bias))
+    a, b = B.znni_linear_backward(dout, far, w), B.znni_linear_backward(dout, x, w)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    far.fill_(7)
+    assert torch.equal(B.znni_linear_backward(dout, x, w, dx=far)[0], b[0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_backwards(dtype):
+    """Row strides below zero, in what is read."""
+    M, N, K = 70, 40, 64
+    x, w, bias, _, dout = inputs(M, N, K, dtype, 13)
+    y = x.flip(0).contiguous()
+    out, dw = torch.empty_like(dout), torch.empty_like(w)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    back = B._rows_descriptor(y.data_ptr() + (M - 1) * K * y.element_size(), -K)
+    r = lambda t: B._rows_descriptor(t.data_ptr(), t.shape[1])  # noqa: E731
+    st = torch.cuda.current_stream().cuda_stream
+    assert B.lib().znni_linear(B._TYPES[dtype], M, N, K, back, r(w), bias.data_ptr(), 0, None, None, r(out), ws.data_ptr(), ws.numel(), st) == 0
+    assert B.lib().znni_linear_backward(B._TYPES[dtype], M, N, K, r(dout), back, None, None, 0, None, r(dw), None, ws.data_ptr(), ws.numel(), st) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, B.znni_linear(x, w, bias)) and torch.equal(dw, B.znni_linear_backward(dout, x, w)[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activations_over_their_range(dtype):
+    """Values from the smallest to the largest, through a product with ones."""
+    z = torch.cat([s * torch.logspace(-30, 30 if dtype != torch.float16 else 4, 401, base=10, dtype=torch.float64) for s in (1, -1)]
+                  + [torch.linspace(-16, 16, 2001, dtype=torch.float64)]).to(dtype).cuda()[:, None]
+    one = torch.ones((1, 1), dtype=dtype, device="cuda")
+    for kind in ("relu", "gelu", "silu"):
+        o, bo, _, _ = R.linear(d(z), d(one), None, kind, None, dtype)
+        R.check(B.znni_linear(z, one, act=kind), o, bo, kind)
+        dx, _, _ = B.znni_linear_backward(torch.ones_like(z), z, one, z=z, act=kind, weights=False, bias=False)
+        _, s = R.act(d(z), kind)
+        # a slope is made of functions off by 8 half steps of fp32, times |z| where it is not yet constant (|z| up to 100)
+        tol = R.UNIT[dtype] * s.abs() + 8 * R.E * (d(z).abs().clamp(max=100) + 1) + R.TINY[dtype]
+        R.check(dx, s, tol * (1 + R.UNIT[dtype]), kind + " slope")
