@@ -133,17 +133,23 @@ __device__ inline void tile_of(int id, int tiles_m, int tiles_n, int* tm, int* t
 
 // out^T [n][m] += W^T X: the columns of the result are the left operand, so that a lane holds four consecutive columns of a row.
 // WAVES_N x WAVES_M waves of NB x MB products of 32 x 32.
-template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES, int ACT>
-__global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductArgs a, Side<T> left, Side<T> right, End<T> d)
-{
-    constexpr int THREADS = 64 * WAVES_N * WAVES_M, TN = WAVES_N * NB * 32, TM = WAVES_M * MB * 32;
+template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES>
+struct ProductShape {
+    static constexpr int THREADS = 64 * WAVES_N * WAVES_M, TN = WAVES_N * NB * 32, TM = WAVES_M * MB * 32;
     using L = Tile<T, LI, TN, THREADS>;
     using R = Tile<T, RI, TM, THREADS>;
+    typedef char Tiles[STAGES][L::BYTES + R::BYTES];
+};
+
+template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES, int ACT>
+__device__ __forceinline__ void product(const ProductArgs& a, const Side<T>& left, const Side<T>& right, const End<T>& d, long long group,
+                                        typename ProductShape<T, LI, RI, WAVES_N, WAVES_M, NB, MB, STAGES>::Tiles& tiles)
+{
+    using S = ProductShape<T, LI, RI, WAVES_N, WAVES_M, NB, MB, STAGES>;
+    using L = typename S::L;
+    using R = typename S::R;
     using M = Mfma<T>;
-    __shared__ __align__(1024) char tiles[STAGES][L::BYTES + R::BYTES];
-    const long long groups = (long long)a.tiles_m * a.tiles_n * a.splits;
-    const long long group = group_id();
-    if (group >= groups) return;
+    constexpr int TN = S::TN, TM = S::TM;
     long long id = group;
     const int split = (int)(id % a.splits); id /= a.splits;
     int tm, tn;
@@ -258,6 +264,36 @@ __global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductAr
     }
 }
 
+template <typename T, bool LI, bool RI, int WAVES_N, int WAVES_M, int NB, int MB, int STAGES, int ACT>
+__global__ __launch_bounds__(64 * WAVES_N * WAVES_M, 2) void k_product(ProductArgs a, Side<T> left, Side<T> right, End<T> d)
+{
+    __shared__ __align__(1024) typename ProductShape<T, LI, RI, WAVES_N, WAVES_M, NB, MB, STAGES>::Tiles tiles;
+    const long long group = group_id();
+    if (group < (long long)a.tiles_m * a.tiles_n * a.splits) product<T, LI, RI, WAVES_N, WAVES_M, NB, MB, STAGES, ACT>(a, left, right, d, group, tiles);
+}
+
+// The gradients of a small layer in one launch, since none waits for another: dx, dw, and the sums of the bias's parts.
+template <typename T>
+struct Gradients {
+    ProductArgs x, w;
+    Side<T> x_left, x_right, w_left, w_right;
+    End<T> dx, dw;
+    int n, parts;
+    const float* sums;
+    T* dbias;                    // or NULL
+};
+template <typename T>
+__global__ __launch_bounds__(256, 2) void k_gradients(Gradients<T> g)
+{
+    typedef typename ProductShape<T, false, true, 2, 2, 1, 1, 4>::Tiles Tiles;
+    static_assert(sizeof(Tiles) == sizeof(typename ProductShape<T, false, false, 2, 2, 1, 1, 4>::Tiles), "one size for both");
+    __shared__ __align__(1024) Tiles tiles;
+    const long long group = group_id(), x = (long long)g.x.tiles_m * g.x.tiles_n * g.x.splits, w = (long long)g.w.tiles_m * g.w.tiles_n * g.w.splits;
+    if (group < x) product<T, false, true, 2, 2, 1, 1, 4, ZNNI_ACT_NONE>(g.x, g.x_left, g.x_right, g.dx, group, tiles);
+    else if (group < x + w) product<T, false, false, 2, 2, 1, 1, 4, ZNNI_ACT_NONE>(g.w, g.w_left, g.w_right, g.dw, group - x, tiles);
+    else if (g.dbias && (group - x - w) * 32 < g.n) sum_parts<T, 8>(g.n, g.parts, g.sums, g.dbias, (int)(group - x - w) * 32, *(float(*)[32][9])&tiles);
+}
+
 // Sums of the parts of the steps, then what an unsplit product does at its end.
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void k_product_join(int M, int N, int splits, End<T> d)
@@ -294,7 +330,7 @@ constexpr int FEW_WAVES = 8;
 template <typename T, int MB, int ACT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void k_few(ProductArgs a, Side<T> w, Side<T> x, End<T> d)
 {
-    constexpr int EC = 16 / sizeof(T), STEP = 4 * EC, AHEAD = MB == 1 ? 8 : MB == 2 ? 4 : 2;
+    constexpr int EC = 16 / sizeof(T), STEP = 4 * EC, AHEAD = MB == 1 ? 8 : 4;
     typedef typename Mfma<T>::V V;
     __shared__ f32x4 sums[FEW_WAVES][MB][64];
     const long long group = group_id();
@@ -393,34 +429,42 @@ static ProductPlan product_plan(int type, int M, int N, int K, bool both_inner)
     return p;
 }
 
+static ProductArgs product_args(const ProductPlan& p, int M, int N, int K)
+{
+    const int edge = 64 << (p.kind < 0 ? 0 : p.kind);
+    return {M, N, K, (int)((M + (long long)edge - 1) / edge), (int)((N + (long long)edge - 1) / edge), p.splits, p.per};
+}
+
+template <typename T, int ACT>
+static znni_status join_product(const ProductPlan& p, int M, int N, const End<T>& d, hipStream_t st)
+{
+    if (p.splits == 1) return ZNNI_OK;
+    k_product_join<T, ACT><<<launch_of(((long long)M * d.Np / 4 + 255) / 256), dim3(256), 0, st>>>(M, N, p.splits, d);
+    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+}
+
 template <typename T, bool LI, bool RI, int ACT>
 static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> right, End<T> d, hipStream_t st)
 {
     const int type = sizeof(T) == 4 ? ZNNI_F32 : ZNNI_BF16;
     const ProductPlan p = product_plan(type, M, N, K, LI && RI);
     d.Np = (N + 3) / 4 * 4;
-    ProductArgs a = {M, N, K, 0, 0, p.splits, p.per};
+    const ProductArgs a = product_args(p, M, N, K);
+    const dim3 grid = launch_of((long long)a.tiles_m * a.tiles_n * p.splits);
     if constexpr (LI && RI) {
         if (p.kind < 0) {
-            const dim3 grid = launch_of((long long)((N + 15) / 16) * p.splits), block(64 * FEW_WAVES);
-            if (M <= 16) k_few<T, 1, ACT><<<grid, block, 0, st>>>(a, left, right, d);
-            else if (M <= 32) k_few<T, 2, ACT><<<grid, block, 0, st>>>(a, left, right, d);
-            else k_few<T, 4, ACT><<<grid, block, 0, st>>>(a, left, right, d);
+            const dim3 few = launch_of((long long)((N + 15) / 16) * p.splits), block(64 * FEW_WAVES);
+            if (M <= 16) k_few<T, 1, ACT><<<few, block, 0, st>>>(a, left, right, d);
+            else k_few<T, 2, ACT><<<few, block, 0, st>>>(a, left, right, d);
         }
     }
-    if (p.kind >= 0) {
-    const int edge = 64 << p.kind;
-    a.tiles_m = (M + edge - 1) / edge;
-    a.tiles_n = (N + edge - 1) / edge;
-    const dim3 grid = launch_of((long long)a.tiles_m * a.tiles_n * p.splits);
     if (p.kind == 0) k_product<T, LI, RI, 2, 2, 1, 1, 4, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
     else if (p.kind == 1) k_product<T, LI, RI, 2, 2, 2, 2, 2, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
-    else if constexpr (sizeof(T) == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(512), 0, st>>>(a, left, right, d);
+    else if constexpr (sizeof(T) == 2) {
+        if (p.kind == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(512), 0, st>>>(a, left, right, d);
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
-    if (p.splits == 1) return ZNNI_OK;
-    k_product_join<T, ACT><<<launch_of(((long long)M * d.Np / 4 + 255) / 256), dim3(256), 0, st>>>(M, N, p.splits, d);
-    return hipGetLastError() == hipSuccess ? ZNNI_OK : ZNNI_ERR_HIP;
+    return join_product<T, ACT>(p, M, N, d, st);
 }
 
 // ---- gradient of what went into the activation, sums over tokens ----------------------------------------------------
@@ -486,9 +530,11 @@ static int slope_parts(int M, int N)
 // ---- what a call needs ----------------------------------------------------------------------------------------------
 
 struct BackwardPlan {
-    size_t dz, sums, parts;            // bytes
+    size_t dz, sums, parts, more;      // bytes; `more`: parts of dw, where dx and dw are made at once
     int dz_row;
-    size_t all() const { return dz + sums + parts; }
+    bool at_once;
+    ProductPlan x, w;
+    size_t all() const { return dz + sums + parts + more; }
 };
 
 static BackwardPlan backward_plan(int type, int M, int N, int K, int act, bool dx, bool dw, bool dbias)
@@ -499,12 +545,12 @@ static BackwardPlan backward_plan(int type, int M, int N, int K, int act, bool d
     const bool products = dx || dw;
     if (act != ZNNI_ACT_NONE && (products || dbias)) p.dz = up((size_t)M * p.dz_row * type_size(type));
     if (dbias) p.sums = up((size_t)slope_parts(M, N) * N * sizeof(float));
-    size_t parts = 0;
-    if (dx) parts = product_plan(type, M, K, N, false).parts;
-    if (dw) {
-        const size_t q = product_plan(type, N, K, M, false).parts;
-        if (q > parts) parts = q;
-    }
+    p.x = product_plan(type, M, K, N, false);
+    p.w = product_plan(type, N, K, M, false);
+    size_t parts = dx ? p.x.parts : 0;
+    p.at_once = dx && dw && M > 0 && N > 0 && K > 0 && p.x.kind == 0 && p.w.kind == 0;
+    if (p.at_once) p.more = up(p.w.parts * sizeof(float));
+    else if (dw && p.w.parts > parts) parts = p.w.parts;
     p.parts = up(parts * sizeof(float));
     return p;
 }
@@ -566,6 +612,29 @@ static znni_status backward(int type, int M, int N, int K, const znni_rows* dout
         });
         if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
         if (act != ZNNI_ACT_NONE) g = {dz, p.dz_row};
+    }
+    if (p.at_once) {
+        Gradients<T> y = {};
+        y.x = product_args(p.x, M, K, N);
+        y.w = product_args(p.w, N, K, M);
+        y.x_left = side_of<T>(w, K);
+        y.x_right = side_of<T>(&g, M);
+        y.w_left = side_of<T>(x, K);
+        y.w_right = side_of<T>(&g, N);
+        y.dx = end_of<T>(dx);
+        y.dw = end_of<T>(dw);
+        y.dx.Np = y.dw.Np = (K + 3) / 4 * 4;
+        y.dx.parts = parts;
+        y.dw.parts = (float*)(at + p.dz + p.sums + p.parts);
+        y.n = N;
+        y.parts = slope_parts(M, N);
+        y.sums = sums;
+        y.dbias = (T*)dbias;
+        const long long groups = (long long)y.x.tiles_m * y.x.tiles_n * p.x.splits + (long long)y.w.tiles_m * y.w.tiles_n * p.w.splits;
+        k_gradients<T><<<launch_of(groups + (dbias ? (N + 31) / 32 : 0)), dim3(256), 0, st>>>(y);
+        if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
+        const znni_status rc = join_product<T, ZNNI_ACT_NONE>(p.x, M, K, y.dx, st);
+        return rc ? rc : join_product<T, ZNNI_ACT_NONE>(p.w, N, K, y.dw, st);
     }
     if (dbias && N > 0) {
         const znni_status rc = launch_sum_parts<T>(N, M > 0 ? slope_parts(M, N) : 0, SumOut<T>{{(T*)dbias}, {sums}}, 1, st);

@@ -52,7 +52,27 @@ static inline znni_status rows_fine(const znni_rows* r, int type, int rows, int 
     return ZNNI_OK;
 }
 
-// Sums of `parts` rows of n sums, 32 lanes a column, four reads of a lane on their way at once.  blockIdx.y: which of the outputs.
+// Sums of `parts` rows of n sums: 32 columns from `col0` on, LANES lanes a column, four reads of a lane on their way at once.
+template <typename T, int LANES>
+__device__ inline void sum_parts(int n, int parts, const float* __restrict__ sums, T* __restrict__ out, int col0, float (*part)[LANES + 1])
+{
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = col0 + c;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (col < n)
+        for (int i = r; i < parts; i += 4 * LANES)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] += i + LANES * j < parts ? sums[(long long)(i + LANES * j) * n + col] : 0.f;
+    part[c][r] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    // a column's sums by as many lanes of a wave
+    const int mine = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    float y = part[mine][lane];
+#pragma unroll
+    for (int x = LANES / 2; x; x >>= 1) y += __shfl_xor(y, x, LANES);
+    if (lane == 0 && col0 + mine < n) out[col0 + mine] = (T)y;
+}
+
+// blockIdx.y: which of the outputs.
 template <typename T>
 struct SumOut {
     T* to[3];
@@ -63,21 +83,7 @@ template <typename T>
 __global__ __launch_bounds__(1024) void k_sum_parts(int n, int parts, SumOut<T> o)
 {
     __shared__ float part[32][33];
-    T* const out = o.to[blockIdx.y];
-    const float* const sums = o.from[blockIdx.y];
-    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (col < n)
-        for (int i = r; i < parts; i += 128)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[j] += i + 32 * j < parts ? sums[(long long)(i + 32 * j) * n + col] : 0.f;
-    part[c][r] = (s[0] + s[1]) + (s[2] + s[3]);
-    __syncthreads();
-    // a column's 32 sums by 32 lanes of a wave
-    float y = part[r][c];
-#pragma unroll
-    for (int x = 16; x; x >>= 1) y += __shfl_xor(y, x, 32);
-    if (c == 0 && (int)blockIdx.x * 32 + r < n) out[blockIdx.x * 32 + r] = (T)y;
+    sum_parts<T, 32>(n, parts, o.from[blockIdx.y], o.to[blockIdx.y], (int)blockIdx.x * 32, part);
 }
 
 template <typename T>
