@@ -471,7 +471,7 @@ znni_status znni_linear(int type, int M, int N, int K, const znni_rows* x, const
 
 /*
  * Its gradients:  dz = dout act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum over tokens of dz  (the residual's is dout itself).
- * dx, dw and dbias that are not wanted are NULL, and so may be what only they need (x, w); z is what the forward call kept (NULL without
+ * dx, dw and dbias that are not wanted are NULL (all three: nothing is done), and so may be what only they need (x, w); z is what the forward call kept (NULL without
  * an activation).  relu'(0) = 0.  dz is rounded to the type before the products of 16-bit types, as their operands are; dbias sums it unrounded.
  * Workspace as above; `wanted` says which of the three the call will ask for.
  */

@@ -724,6 +724,8 @@ znni_status znni_linear_backward(int type, int M, int N, int K, const znni_rows*
     if (act != ZNNI_ACT_NONE && (rc = rows_fine(z, type, M, N, false))) return rc;
     if (dw && ((rc = rows_fine(x, type, M, K, false)) || (rc = rows_fine(dw, type, N, K, true)))) return rc;
     if (dx && ((rc = rows_fine(w, type, N, K, false)) || (rc = rows_fine(dx, type, M, K, true)))) return rc;
+    // (nothing wanted: the workspace has no place for dz either)
+    if (!dx && !dw && !dbias) return ZNNI_OK;
     if (need && !workspace) return ZNNI_ERR_NULL;
     if ((uintptr_t)dbias % type_size(type) || (need && ((uintptr_t)workspace & 255u))) return ZNNI_ERR_ALIGN;
     if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;
