@@ -678,12 +678,12 @@ def znni_linear_backward_workspace(dtype, M, N, K, act=None, wanted=LINEAR_DX | 
 def znni_linear_backward(dout, x, w, z=None, act=None, bias=True, inputs=True, weights=True, dx=None, dw=None, dbias=None, workspace=None,
                          stream=None):
     """Gradients (dx, dw, dbias) of znni_linear from its result's, dout [M, N]; None for those that `inputs`, `weights` and `bias` do not ask
-    for.  z: what the forward call kept (with an activation).  The residual's gradient is dout."""
+    for; x and w may be None where only others need them.  z: what the forward call kept (with an activation).  The residual's gradient is dout."""
     if stream is not None:
         return _on(stream, dout, znni_linear_backward, dout, x, w, z, act, bias, inputs, weights, dx, dw, dbias, workspace)
     kind = _kind(dout)
     M, N = shape = dout.shape
-    K = (x if w is None else w).shape[1]
+    K = w.shape[1] if w is not None else x.shape[1] if x is not None else 0          # (the bias's gradient takes neither)
     dx = (dout.new_empty(M, K) if dx is None else dx) if inputs else None
     dw = (dout.new_empty(N, K) if dw is None else dw) if weights else None
     dbias = (dout.new_empty(N) if dbias is None else dbias) if bias else None

@@ -21,3 +21,25 @@ def test_none_wanted(dtype, act):
     assert B.znni_linear_backward(dout, x, w, workspace=ws, **kw) == (None, None, None)
     torch.cuda.synchronize()
     assert (ws == 77).all() and all(torch.equal(a, b) for a, b in zip(kept, (x, w, z, dout)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_bias_alone(dtype):
+    x, w, _, z, dout = inputs(70, 136, 72, dtype, 21)
+    for act in (None, "silu"):
+        kw = dict(z=None if act is None else z, act=act)
+        whole = B.znni_linear_backward(dout, x, w, **kw)
+        got = B.znni_linear_backward(dout, None, None, inputs=False, weights=False, **kw)
+        assert got[0] is None and got[1] is None and torch.equal(got[2], whole[2])
+        # and each product without the operand that only the other takes
+        dx, dw, _ = B.znni_linear_backward(dout, None, w, weights=False, bias=False, **kw)
+        assert dw is None and torch.equal(dx, whole[0])
+        dx, dw, _ = B.znni_linear_backward(dout, x, None, inputs=False, bias=False, **kw)
+        assert dx is None and torch.equal(dw, whole[1])
+
+
+def test_operands_that_are_missing_are_refused():
+    x, w, _, _, dout = inputs(8, 16, 24, torch.bfloat16, 22)
+    for a, b in ((None, w), (x, None), (None, None)):
+        with pytest.raises(RuntimeError):
+            B.znni_linear_backward(dout, a, b)
