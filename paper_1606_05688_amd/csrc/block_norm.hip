@@ -259,10 +259,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_back(NormArgs a,
         if (a.post) {
             over = sum(over);
             over = make_float2(over.x / a.C, a.centred ? over.y / a.C : 0.f);
-        } else {
-            over = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < E; ++i) d[i] = yr * (d[i] - normed(i) * over.x - over.y);
         }
-        if (dy.p) put(dy, [&](int i) { return yr * (d[i] - normed(i) * over.x - over.y); });
+        // (without a norm y has no part in its gradient: an infinity in it would make NaN of a product with zero)
+        if (dy.p) put(dy, [&](int i) { return d[i]; });
     }
     auto write = [&](float* to, const float (&s)[E]) {
         if (!to) return;
