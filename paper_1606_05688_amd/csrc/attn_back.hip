@@ -17,12 +17,13 @@
 #include <type_traits>
 
 #include "attn_tile.h"
+#include "back_parts.h"
 
 namespace znni {
 
-constexpr int BACK_THREADS = 256, BACK_LANES = 128;      // keys (or rows) of a workgroup
+constexpr int BACK_THREADS = 256;
 
-struct BackArgs {
+struct BackArgs : BackParts {
     int Hq, Hk, D;
     const int* cu_q;
     const int* cu_k;
@@ -31,9 +32,6 @@ struct BackArgs {
     int max_q, max_k;
     int cycle;                        // tiles that a workgroup walks, or 0: they start with their first
     int heads;                        // B * Hk
-    int tiles, splits;                // tiles of keys (or rows) of a sequence, workgroups that share a tile's walk
-    int first_tiles;                  // of keys: tiles that hold first tokens, which rows past their window see too:
-    int far_tiles, far;               // 32 keys at a time, so many workgroups that walk those rows
     long long groups;                 // of the launch
     long long pitch;                  // rows of a sequence and key head in `rows`
     const char* rows;                 // [2][B * Hk][pitch]: what is taken from a row's scores and its dP, as fp32 or in pieces
@@ -640,10 +638,7 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
         if (to >= count) return;
         const bool parts = far || a.splits > 1 || (KEYS && tile < a.first_tiles);
         T* const y = KEYS ? out.row(k0 + to, hk) : out.row(q0 + token, hk * shared + to - token * shared);
-        // parts of a sequence and head: the tiles' own (all, or those that hold first tokens), then the far ones, 32 keys each
-        const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles;
-        const long long keys = (long long)bh * (owns * BACK_LANES + a.far_tiles * a.far * 32);
-        const long long row = keys + (far ? owns * BACK_LANES + (tile * a.far + split) * 32 : (tile * a.splits + split) * BACK_LANES) + (to - x0);
+        const long long row = (far ? a.far_part(bh, tile, split) : a.own_part(bh, tile, split)) + (to - x0);
         float* const z = a.parts + (row * (KEYS ? 2 : 1) + which) * a.D;
 #pragma unroll
         for (int x = 0; x < NC; ++x)
@@ -694,11 +689,10 @@ __device__ __forceinline__ void back_join(const BackArgs& a, const int id, int t
     const int x0 = KEYS ? a.cu_k[b] : a.cu_q[b];
     const int count = KEYS ? min(a.cu_k[b + 1] - x0, a.max_k) : min(a.cu_q[b + 1] - x0, a.max_q) * shared;
     if (x >= count) return;
-    const int owns = a.splits > 1 ? a.tiles * a.splits : a.first_tiles, N = KEYS ? 2 : 1;
-    const int far = KEYS && x / 32 < a.far_tiles ? a.far : 0;
-    const long long keys = (long long)bh * (owns * BACK_LANES + a.far_tiles * a.far * 32);
-    const float* const own = a.parts + (keys + x / BACK_LANES * a.splits * BACK_LANES + x % BACK_LANES) * N * a.D + d;
-    const float* const others = a.parts + (keys + owns * BACK_LANES + x / 32 * a.far * 32 + x % 32) * N * a.D + d;
+    const int far = KEYS && x / FAR_LANES < a.far_tiles ? a.far : 0;
+    constexpr int N = KEYS ? 2 : 1;
+    const float* const own = a.parts + (a.own_part(bh, x / BACK_LANES, 0) + x % BACK_LANES) * N * a.D + d;
+    const float* const others = a.parts + (a.far_part(bh, x / FAR_LANES, 0) + x % FAR_LANES) * N * a.D + d;
 #pragma unroll
     for (int which = 0; which < N; ++which) {
         float4 s = {0.f, 0.f, 0.f, 0.f};
@@ -715,7 +709,7 @@ __device__ __forceinline__ void back_join(const BackArgs& a, const int id, int t
             }
         };
         add(own + which * a.D, a.splits, BACK_LANES * N * a.D);
-        add(others + which * a.D, far, 32 * N * a.D);
+        add(others + which * a.D, far, FAR_LANES * N * a.D);
         const Heads<T>& to = which ? db : da;
         typedef T T4 __attribute__((ext_vector_type(4)));
         T* const y = KEYS ? to.row(x0 + x, hk) : to.row(x0 + x / shared, hk * shared + x % shared);
@@ -735,8 +729,8 @@ __global__ __launch_bounds__(256) void k_back_join(BackArgs ak, BackArgs aq, int
 
 constexpr int BACK_TWICE = 512;            // keys that a row sees at most for weights to be two values
 
-struct BackPlan {
-    int tiles, splits, first_tiles, far_tiles, far, cycle;
+struct BackPlan : BackParts {
+    int cycle;
     bool twice;
     long long groups;
     size_t parts;                          // elements
@@ -768,7 +762,7 @@ static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int
         // rows past the window of first tokens: so many workgroups that each is done in a small part of the others' time
         if (lanes > 0 && (long long)left + 1 < max_k) {
             p.first_tiles = (lanes + BACK_LANES - 1) / BACK_LANES;
-            p.far_tiles = (lanes + 31) / 32;
+            p.far_tiles = (lanes + FAR_LANES - 1) / FAR_LANES;
             // (each eight tiles at least)
             long long n = 8 * ((long long)max_q + wide - 1) / wide;
             if (n > (long long)max_q * G / (8 * rt)) n = (long long)max_q * G / (8 * rt);
@@ -781,8 +775,7 @@ static BackPlan back_plan(bool keys, int type, int B, int Hq, int Hk, int D, int
     p.cycle = p.splits == 1 ? (int)((walk + rt - 1) / rt) : 0;
     const long long per_head = (long long)p.tiles * p.splits + (long long)p.far_tiles * p.far;
     p.groups = per_head * Hk * B;
-    const long long owns = p.splits > 1 ? (long long)p.tiles * p.splits : p.first_tiles;
-    p.parts = (size_t)(owns * BACK_LANES + (long long)p.far_tiles * p.far * 32) * Hk * B * (keys ? 2 : 1) * D;
+    p.parts = (size_t)p.per_head() * Hk * B * (keys ? 2 : 1) * D;
     return p;
 }
 
@@ -804,12 +797,8 @@ static BackSizes back_sizes(int type, int B, int Hq, int Hk, int D, int max_q, i
 
 static BackArgs planned(BackArgs a, const BackPlan& p, float* parts)
 {
-    a.tiles = p.tiles;
-    a.splits = p.splits;
-    a.first_tiles = p.first_tiles;
+    (BackParts&)a = p;
     a.cycle = p.cycle;
-    a.far_tiles = p.far_tiles;
-    a.far = p.far;
     a.groups = p.groups;
     a.parts = parts;
     return a;
