@@ -48,11 +48,12 @@ __host__ __device__ inline bool sees(long long p, int j, const Window& w)
     return j <= p + w.right && (j >= p - w.left || j < w.sinks);
 }
 
-// A dimension of a launch has fewer than 2^32 threads: workgroups (of up to 256) past this many go on in the second dimension.
+// A dimension of a launch has fewer than 2^32 threads: workgroups of 256 past this many, or of other sizes past as many threads, go on in the
+// second dimension.
 constexpr unsigned LAUNCH_X = 1u << 23;
-static inline dim3 launch_of(long long groups)
+static inline dim3 launch_of(long long groups, unsigned threads = 256)
 {
-    const unsigned x = groups < LAUNCH_X ? (unsigned)groups : LAUNCH_X;
+    const unsigned most = LAUNCH_X * 256 / threads, x = groups < most ? (unsigned)groups : most;
     return dim3(x, (unsigned)((groups + x - 1) / x));
 }
 __device__ inline long long group_id() { return (long long)blockIdx.y * gridDim.x + blockIdx.x; }

@@ -338,26 +338,28 @@ static znni_status with_back_row(NormShape s, F f)
 }
 
 template <typename T, int VEC, int E, int W, typename... A>
-static void launch_norm(Row<T, VEC, E, W>, dim3 grid, hipStream_t st, A... args)
+static void launch_norm(Row<T, VEC, E, W>, long long groups, hipStream_t st, A... args)
 {
-    k_norm<T, VEC, E, W><<<grid, dim3(W == 1 ? 256 : 64 * W), 0, st>>>(args...);
+    constexpr unsigned THREADS = W == 1 ? 256 : 64 * W;
+    k_norm<T, VEC, E, W><<<launch_of(groups, THREADS), dim3(THREADS), 0, st>>>(args...);
 }
 
 template <typename T, int VEC, int E, int W, typename... A>
-static void launch_norm_back(Row<T, VEC, E, W>, dim3 grid, hipStream_t st, A... args)
+static void launch_norm_back(Row<T, VEC, E, W>, long long groups, hipStream_t st, A... args)
 {
-    k_norm_back<T, VEC, E, W><<<grid, dim3(W == 1 ? 256 : 64 * W), 0, st>>>(args...);
+    constexpr unsigned THREADS = W == 1 ? 256 : 64 * W;
+    k_norm_back<T, VEC, E, W><<<launch_of(groups, THREADS), dim3(THREADS), 0, st>>>(args...);
 }
 
 template <typename T>
 static znni_status norm_forward(NormArgs a, const znni_rows* x, const znni_rows* y, const znni_rows* gate, const void* post, const void* pre,
                                 const znni_rows* h, const znni_rows* z, hipStream_t st)
 {
-    const dim3 grid = launch_of(((long long)a.T + a.per - 1) / a.per);
+    const long long groups = ((long long)a.T + a.per - 1) / a.per;
     Rows<const T> g = rows_of<const T>(gate);
     if (a.shared) g.row = 0;
     return with_row<T>(norm_shape(a.T, a.C), [&](auto row) {
-        launch_norm(row, grid, st, a, rows_of<const T>(x), rows_of<const T>(y), g, (const T*)post, (const T*)pre, rows_of<T>(h), rows_of<T>(z));
+        launch_norm(row, groups, st, a, rows_of<const T>(x), rows_of<const T>(y), g, (const T*)post, (const T*)pre, rows_of<T>(h), rows_of<T>(z));
         return 0;
     });
 }
@@ -370,7 +372,7 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
     Rows<const T> g = rows_of<const T>(gate);
     if (a.shared) g.row = 0;
     const bool summed = a.shared && dgate;
-    const int groups = a.T ? (int)(((long long)a.T + a.per - 1) / a.per) : 0;
+    const long long groups = a.T ? ((long long)a.T + a.per - 1) / a.per : 0;
     const size_t step = up((size_t)NORM_GROUPS * a.C * sizeof(float)) / sizeof(float);
     NormSums sums = {};
     SumOut<T> o = {};
@@ -388,13 +390,13 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
     if (a.T > 0) {
         const Rows<T> dg = summed ? Rows<T>{nullptr, 0} : rows_of<T>(dgate);
         const znni_status rc = with_back_row<T>(norm_back_shape(a.C), [&](auto row) {
-            launch_norm_back(row, launch_of(((long long)a.T + a.per - 1) / a.per), st, a, rows_of<const T>(dh), rows_of<const T>(dz), rows_of<const T>(h), rows_of<const T>(y), g,
+            launch_norm_back(row, groups, st, a, rows_of<const T>(dh), rows_of<const T>(dz), rows_of<const T>(h), rows_of<const T>(y), g,
                              (const T*)post, (const T*)pre, rows_of<T>(dx), rows_of<T>(dy), dg, sums);
             return 0;
         });
         if (rc) return rc;
     }
-    return n ? launch_sum_parts<T>(a.C, groups, o, n, st) : ZNNI_OK;
+    return n ? launch_sum_parts<T>(a.C, (int)groups, o, n, st) : ZNNI_OK;
 }
 
 static znni_status norm_shape_fine(int type, int T, int C, unsigned flags)

@@ -450,18 +450,19 @@ static znni_status launch_product(int M, int N, int K, Side<T> left, Side<T> rig
     const ProductPlan p = product_plan(type, M, N, K, LI && RI);
     d.Np = (N + 3) / 4 * 4;
     const ProductArgs a = product_args(p, M, N, K);
-    const dim3 grid = launch_of((long long)a.tiles_m * a.tiles_n * p.splits);
+    const unsigned threads = p.kind == 2 ? 512 : 256;
+    const dim3 grid = launch_of((long long)a.tiles_m * a.tiles_n * p.splits, threads);
     if constexpr (LI && RI) {
         if (p.kind < 0) {
-            const dim3 few = launch_of((long long)((N + 15) / 16) * p.splits), block(64 * FEW_WAVES);
+            const dim3 few = launch_of((long long)((N + 15) / 16) * p.splits, 64 * FEW_WAVES), block(64 * FEW_WAVES);
             if (M <= 16) k_few<T, 1, ACT><<<few, block, 0, st>>>(a, left, right, d);
             else k_few<T, 2, ACT><<<few, block, 0, st>>>(a, left, right, d);
         }
     }
-    if (p.kind == 0) k_product<T, LI, RI, 2, 2, 1, 1, 4, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
-    else if (p.kind == 1) k_product<T, LI, RI, 2, 2, 2, 2, 2, ACT><<<grid, dim3(256), 0, st>>>(a, left, right, d);
+    if (p.kind == 0) k_product<T, LI, RI, 2, 2, 1, 1, 4, ACT><<<grid, dim3(threads), 0, st>>>(a, left, right, d);
+    else if (p.kind == 1) k_product<T, LI, RI, 2, 2, 2, 2, 2, ACT><<<grid, dim3(threads), 0, st>>>(a, left, right, d);
     else if constexpr (sizeof(T) == 2) {
-        if (p.kind == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(512), 0, st>>>(a, left, right, d);
+        if (p.kind == 2) k_product<T, LI, RI, 2, 4, 4, 2, 2, ACT><<<grid, dim3(threads), 0, st>>>(a, left, right, d);
     }
     if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     return join_product<T, ACT>(p, M, N, d, st);

@@ -29,3 +29,26 @@ def test_gradients_that_nobody_wants(record, type):
     for wanted in range(1, 8):
         (status, launched), = record([linear_back(type, 8, 16, 64, 2, wanted)])
         assert status == 0 and "k_slope" in launched[0][0]
+
+
+def norm(type, T, C, back=False, sums=False):
+    if not back:
+        return ["znni_block_norm", [["i", type], ["i", T], ["i", C], ["rows", [P, C]], ["rows", [P, C]], ["rows", None], ["p", None], ["p", None], ["f", 1.0], ["f", 1e-5],
+                                    ["u", B.NORM_POST | B.NORM_PRE], ["rows", [P, C]], ["rows", [P, C]], ["p", None]]]
+    return ["znni_block_norm_backward", [["i", type], ["i", T], ["i", C], ["rows", [P, C]], ["rows", [P, C]], ["rows", [P, C]], ["rows", [P, C]], ["rows", None], ["p", None],
+                                         ["p", None], ["f", 1.0], ["f", 1e-5], ["u", B.NORM_POST | B.NORM_PRE], ["rows", [P, C]], ["rows", [P, C]], ["rows", None],
+                                         ["p", None], ["p", P if sums else None], ["p", WS], ["z", BIG], ["p", None]]]
+
+
+@pytest.mark.parametrize("T", [1, 1000, (1 << 22) - 1, 1 << 22, 1 << 23, (1 << 25) + 5, 1 << 30])
+def test_a_dimension_of_a_launch_has_fewer_than_2_32_threads(record, T):
+    """Many rows of one workgroup each, of up to 1024 threads; every row has its place."""
+    cases = [(C, back, sums) for C in (100, 2048, 2049, 4096, 8192, 9000, 16384) for back in (False, True) for sums in ((False, True) if back else (False,))]
+    for (C, back, sums), (status, launched) in zip(cases, record([norm(B.BF16, T, *c) for c in cases])):
+        assert status == 0 and len(launched) == (2 if sums else 1), (C, back, sums)
+        for name, grid, block in launched:
+            assert all(g * b < 1 << 32 for g, b in zip(grid, block)) and max(grid[1:]) < 1 << 16, (name, grid, block)
+        _, grid, block = launched[0]
+        if not sums:
+            rows = 4 if block[0] == 256 and C <= (512 if back else 2048) and (back or C <= 512 or T > 1024) else 1
+            assert grid[0] * grid[1] * rows >= T, (C, back, grid, block)
