@@ -252,6 +252,7 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Side<T>& lef
             for (int q = 0; q < 4; ++q)
                 mine[c32 * CHUNKS + ((8 * i + 2 * q + h) ^ (c32 & (CHUNKS - 1)))] =
                     make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        wave_meets();
 #pragma unroll
         for (int r0 = 0; r0 < 32; r0 += 64 / LANES) {
             const int r = r0 + l / LANES, c = l % LANES * EC, m = m0 + wm + 32 * j + r, col = n0 + wn + c;
@@ -261,6 +262,7 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Side<T>& lef
             if (m >= a.M || col >= a.N) continue;
             end_row<T, ACT, EC>(d, m, col, a.N - col, (const float*)v);
         }
+        wave_meets();
     }
 }
 

@@ -5,6 +5,15 @@
 
 namespace znni {
 
+// What lanes of this wave wrote to LDS is there for its other lanes, what they read there may be written over.  (The hardware keeps a wave's
+// accesses in order; this is what keeps the compiler from moving them past each other.)
+__device__ inline void wave_meets()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // A matrix in device memory as one side of a product: element (row r of the result's side, c of the sum) lies at p[r * ld + c] if
 // the sum's index is the contiguous one, at p[c * ld + r] if not.
 template <typename T>
