@@ -207,7 +207,6 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Side<T>& lef
                     }
                 }
         }
-#ifndef NOSGB
         // reads of a step run ahead of the products of the one before
         if constexpr (sizeof(T) == 2) {
             constexpr int READS = NB * (LI ? 1 : 2) + MB * (RI ? 1 : 2), PRODUCTS = NB * MB;
@@ -218,7 +217,6 @@ __device__ __forceinline__ void product(const ProductArgs& a, const Side<T>& lef
                 __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
             }
         }
-#endif
     }
     const int h = l >> 5, c32 = l & 31;
     if (a.splits > 1) {
@@ -582,11 +580,11 @@ static znni_status forward(int M, int N, int K, const znni_rows* x, const znni_r
     if (residual) {
         d.residual = (const T*)residual->data;
         d.residual_row = residual->row;
-            }
+    }
     if (z) {
         d.z = (T*)z->data;
         d.z_row = z->row;
-            }
+    }
     d.parts = (float*)workspace;
     return with_act(act, [&](auto k) {
         return launch_product<T, true, true, decltype(k)::value>(M, N, K, side_of<T>(w, N), side_of<T>(x, M), d, st);
