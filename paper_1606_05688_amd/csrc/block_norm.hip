@@ -319,6 +319,15 @@ static int norm_rows(int T, int W, bool sums)
     return (int)((n + once - 1) / once * once);
 }
 
+// Workgroups that leave sums over tokens, at most: of more rows never fewer, so that a workspace does for all smaller calls.
+static long long norm_parts(int T, int C)
+{
+    const int once = norm_back_shape(C).W == 1 ? 4 : 1;
+    const long long n = ((long long)T + once - 1) / once;
+    return n < NORM_GROUPS ? n : NORM_GROUPS;
+}
+static size_t norm_sums(int T, int C) { return up((size_t)norm_parts(T, C) * C * sizeof(float)); }
+
 template <typename T, typename F>
 static znni_status with_row(NormShape s, F f)
 {
@@ -373,7 +382,7 @@ static znni_status norm_backward(NormArgs a, const znni_rows* dh, const znni_row
     if (a.shared) g.row = 0;
     const bool summed = a.shared && dgate;
     const long long groups = a.T ? ((long long)a.T + a.per - 1) / a.per : 0;
-    const size_t step = up((size_t)NORM_GROUPS * a.C * sizeof(float)) / sizeof(float);
+    const size_t step = norm_sums(a.T, a.C) / sizeof(float);
     NormSums sums = {};
     SumOut<T> o = {};
     int n = 0;
@@ -441,7 +450,7 @@ znni_status znni_block_norm_backward_workspace(int type, int T, int C, unsigned 
     if (!bytes) return ZNNI_ERR_NULL;
     const znni_status rc = norm_shape_fine(type, T, C, flags);
     if (rc) return rc;
-    *bytes = 3 * up((size_t)NORM_GROUPS * C * sizeof(float));
+    *bytes = 3 * norm_sums(T, C);
     return ZNNI_OK;
 }
 
@@ -467,7 +476,7 @@ znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh
         if (o && (rc = rows_fine(o, type, T, C, true))) return rc;
     if (dgate && (rc = rows_fine(dgate, type, shared ? 1 : T, C, true))) return rc;
     if (((uintptr_t)post | (uintptr_t)pre | (uintptr_t)dpost | (uintptr_t)dpre) % type_size(type)) return ZNNI_ERR_ALIGN;
-    if (summed) {
+    if (summed && need) {
         if (!workspace) return ZNNI_ERR_NULL;
         if ((uintptr_t)workspace & 255u) return ZNNI_ERR_ALIGN;
         if (workspace_bytes < need) return ZNNI_ERR_WORKSPACE;

@@ -52,3 +52,15 @@ def test_a_dimension_of_a_launch_has_fewer_than_2_32_threads(record, T):
         if not sums:
             rows = 4 if block[0] == 256 and C <= (512 if back else 2048) and (back or C <= 512 or T > 1024) else 1
             assert grid[0] * grid[1] * rows >= T, (C, back, grid, block)
+
+
+@pytest.mark.parametrize("C", [1, 512, 513, 4096, 16384])
+def test_workspace_of_sums_over_tokens(record, C):
+    """As much as the workgroups leave, and never less for more tokens."""
+    import torch
+    tokens = [0, 1, 2, 3, 4, 5, 8, 100, 1023, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 1 << 20, 1 << 30]
+    sizes = [B.znni_block_norm_backward_workspace(torch.bfloat16, T, C) for T in tokens]
+    assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[1] <= 3 * (4 * C + 255) and sizes[-1] <= 3 * 1024 * (4 * C + 255)
+    for T, size, (status, launched) in zip(tokens[1:], sizes[1:], record([norm(B.BF16, T, C, True, True) for T in tokens[1:]])):
+        name, grid, _ = launched[0]
+        assert status == 0 and "k_norm_back" in name and size >= 3 * grid[0] * grid[1] * C * 4
