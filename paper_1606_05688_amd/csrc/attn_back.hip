@@ -587,13 +587,7 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
                 if constexpr (SUM_B) add(std::false_type(), acc_b, bb, s, 16);
                 if constexpr (SUM_A) add(std::false_type(), acc_a, ab, dp, 0);
             }
-            // The compiler has been seen to read a sum right behind its product, on the other side of a branch, without the 18 wait states of fp32
-            // products (one element of 16 was wrong): they are here.
-            if constexpr (F32) {
-                __builtin_amdgcn_sched_barrier(0);
-                asm volatile("s_nop 15\n\ts_nop 1");
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            if constexpr (F32) products_done<T>();
         }
     }
     // (the lane's place once more: kept, it would take registers from the walk)

@@ -102,6 +102,17 @@ struct Mfma<float> {
     __device__ static f32x16 mul(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 };
 
+// A product's result may be read this many wait states behind it: 18 in fp32, 12 in 16-bit types.  The compiler keeps them on straight code, and has been
+// seen to lose them where branches lie between (one element of 16 was wrong): they are here.
+template <typename T>
+__device__ inline void products_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (sizeof(T) == 4) asm volatile("s_nop 15\n\ts_nop 1");
+    else asm volatile("s_nop 11");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // What kind of number x is, so that a sum of up to 64 says which kinds were there: 1 for infinity, 128 for minus infinity, both for NaN, 0 else.
 __device__ inline float kind_of(float x)
 {

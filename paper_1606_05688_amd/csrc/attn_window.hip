@@ -260,6 +260,7 @@ __global__ __launch_bounds__(ATTN_THREADS, 2) void k_attn(AttnArgs a, Heads<cons
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
             }
+            products_done<T>();
             if constexpr (BY_D) {
                 // so far of this wave's elements of the head
                 float4* const mine = partial + part * 256 + l;
