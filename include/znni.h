@@ -515,9 +515,9 @@ znni_status znni_block_norm_backward(int type, int T, int C, const znni_rows* dh
  * dk = scale dS^T q,  dv = P^T dout, the last two summed over the query heads that share a key head.  Rows that see nothing have
  * gradients of zero, and so have keys that nothing sees.  What is not finite makes gradients that it enters not finite, and no others: a row's
  * q and dout those of what it sees, a key's k and v those of the rows that see it.
- * 16-bit types: P and dS are rounded to the type (fp16: scaled by powers of two, so that its range is none of theirs) before their
- * last product; sums stay fp32.  Tokens past max_q and keys past max_k, and those behind the last sequence, are not written.
- * max_q * Hq / Hk and max_k up to 2^31 - 257.  Workspace as for znni_attn_window, never of zero bytes.
+ * 16-bit types: P and dS are rounded to the type before their last product (fp16: P times 2^15, dS times a power of two of the row's, or
+ * key's, own, so that its range is none of theirs, whatever sizes others in the call have); sums stay fp32.  Tokens past max_q and keys past max_k, and
+ * those behind the last sequence, are not written.  max_q * Hq / Hk and max_k up to 2^31 - 257.  Workspace as for znni_attn_window.
  */
 znni_status znni_attn_window_backward_workspace(int type, int B, int Hq, int Hk, int D, int max_q, int max_k, int left, int right, int sinks,
                                                 size_t* bytes);

@@ -11,7 +11,7 @@
 //
 // bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 2100 us in all, 576 TFLOP/s of the five products that it takes, 920 of the eight that run
 // (scores twice for wide heads' dk and dv, and again for dq).  Bound by LDS reads, products and exponentials of two waves a SIMD that take turns but for
-// the meetings at each tile (matrix units 41 % busy, vector units 35 %), no bank conflicts.  fp16, ragged 300 tokens: 42 us, the chain of three launches.  fp32, 2744
+// the meetings at each tile (matrix units 41 % busy, vector units 35 %), no bank conflicts.  fp16, ragged 300 tokens: 37 us, the chain of three launches.  fp32, 2744
 // tokens: 151 us, matrix units of one or two workgroups a unit, 40 of 64 columns useful.
 #include <initializer_list>
 #include <type_traits>
@@ -36,28 +36,21 @@ struct BackArgs : BackParts {
     long long pitch;                  // rows of a sequence and key head in `rows`
     const char* rows;                 // [2][B * Hk][pitch]: what is taken from a row's scores and its dP, as fp32 or in pieces
     long long all_rows;               // B * Hk * pitch
-    float2* peaks;                    // fp16: largest finite magnitudes of dout and of v, of each workgroup that looked
-    int peak_count;
     float* parts;
 };
 
-// fp16 has no room for weights of long rows (2^-14 is its least normal number) nor for gradients of any size: P goes into its product times 2^15,
-// dS times a power of two for which |dout.v - delta| <= 2 D max|dout| max|v| stays below 2^15.  Other types have the range of fp32.
-constexpr int WEIGHT_POWER = 15;
-constexpr int PEAKS = 512;            // workgroups of the rows' kernel, which leave two maxima each
-__device__ inline int slope_power(const BackArgs& a)
+// fp16 has no room for weights of long rows (2^-14 is its least normal number) nor for gradients of any size: P goes into its product times 2^15, dS
+// times a power of two of the lane's own (a row's, or a key's), which its sums are divided by at the end.  The power falls when a value of the lane would
+// pass 2^15, to one that takes that value to 2^11, and the sums with it: so what is rounded has all its bits down to 2^-25 of the lane's largest, whatever
+// sizes other rows, keys, heads and sequences have, and a lane's results do not depend on them.
+constexpr int WEIGHT_POWER = 15, SLOPE_POWER = 11;
+constexpr float SLOPE_MOST = 0x1p15f, SLOPE_START = 0x1p100f;       // (what would need a larger factor than that leaves nothing in fp16)
+// The factor that takes x to 2^SLOPE_POWER .. 2^(SLOPE_POWER + 1).  (Infinities and what is next to them: 2^-117.)
+__device__ inline float slope_factor(float x)
 {
-    float2 most = {0.f, 0.f};
-    for (int i = threadIdx.x & 63; i < a.peak_count; i += 64) {
-        const float2 y = a.peaks[i];
-        most = make_float2(fmaxf(most.x, y.x), fmaxf(most.y, y.y));
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) most = make_float2(fmaxf(most.x, __shfl_xor(most.x, o)), fmaxf(most.y, __shfl_xor(most.y, o)));
-    const float both = most.x * most.y * (float)a.D;
-    return both > 0.f ? WEIGHT_POWER - 2 - ilogbf(both) : 0;
+    const int power = (int)(__float_as_uint(x) >> 23) - 127;
+    return __uint_as_float((unsigned)(127 + SLOPE_POWER - power) << 23);
 }
-__device__ inline float finite_size(float x) { return fabsf(x) <= 65504.f ? fabsf(x) : 0.f; }
 
 // What a score is multiplied by to count powers of two.
 // (At least 2^-120, so that the logarithm of a sum counts as a score: scales below that are 2^-120 for scores below 2^100.)
@@ -99,61 +92,33 @@ struct RowNumber {
 
 // Sixteen lanes a row, 16 bytes a lane at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, int B, Heads<const T> dout, Heads<const T> out, Heads<const T> v,
-                                                   const float2* __restrict__ stats, typename RowNumber<T>::type* __restrict__ rows)
+__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, Heads<const T> dout, Heads<const T> out, const float2* __restrict__ stats, typename RowNumber<T>::type* __restrict__ rows)
 {
     constexpr bool F16 = std::is_same<T, f16>::value;
     constexpr int EC = 16 / sizeof(T);
     typedef T V __attribute__((ext_vector_type(EC)));
     const int G = a.Hq / a.Hk, l = threadIdx.x & 15;
-    const long long step = (long long)gridDim.x * gridDim.y * 16, begin = group_id() * 16 + (threadIdx.x >> 4);
-    float2 most = {0.f, 0.f};
-    for (long long id = begin; id < a.all_rows; id += step) {
-        const int bh = (int)(id / a.pitch), r = (int)(id - bh * a.pitch), b = bh / a.Hk, hk = bh - b * a.Hk;
-        const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q);
-        if (r < nq * G) {                                // (fits: checked by the host)
-            const int i = r / G, head = hk * G + r - i * G;
-            const long long token = q0 + i;
-            float s = 0.f;
-            for (int d = l * EC; d < a.D; d += 16 * EC) {
-                const V x = *(const V*)(dout.row(token, head) + d), y = *(const V*)(out.row(token, head) + d);
+    const long long id = group_id() * 16 + (threadIdx.x >> 4);
+    if (id >= a.all_rows) return;
+    const int bh = (int)(id / a.pitch), r = (int)(id - bh * a.pitch), b = bh / a.Hk, hk = bh - b * a.Hk;
+    const int q0 = a.cu_q[b], nq = min(a.cu_q[b + 1] - q0, a.max_q);
+    if (r >= nq * G) return;                             // (fits: checked by the host)
+    const int i = r / G, head = hk * G + r - i * G;
+    const long long token = q0 + i;
+    float s = 0.f;
+    for (int d = l * EC; d < a.D; d += 16 * EC) {
+        const V x = *(const V*)(dout.row(token, head) + d), y = *(const V*)(out.row(token, head) + d);
 #pragma unroll
-                for (int e = 0; e < EC; ++e) {
-                    s += (float)x[e] * (float)y[e];
-                    if constexpr (F16) most.x = fmaxf(most.x, finite_size((float)x[e]));
-                }
-            }
-#pragma unroll
-            for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o, 16);
-            if (l == 0) {
-                const float2 st = stats[token * a.Hq + head];
-                // (a row without weights: none whatever the scores)
-                const float by = back_powers(a.scale), power = log2f(st.y) - (F16 ? WEIGHT_POWER : 0);
-                rows[id] = RowNumber<T>::of(st.y == 0.f ? INFINITY : sizeof(T) == 4 ? fmaf(st.x, by, power) : st.x + power / by);
-                rows[a.all_rows + id] = RowNumber<T>::of(s);
-            }
-        }
+        for (int e = 0; e < EC; ++e) s += (float)x[e] * (float)y[e];
     }
-    if constexpr (F16) {
-        const long long keys = (long long)B * a.Hk * a.max_k;
-        for (long long id = begin; id < keys; id += step) {
-            const int bh = (int)(id / a.max_k), j = (int)(id - (long long)bh * a.max_k), b = bh / a.Hk, k0 = a.cu_k[b];
-            if (j < a.cu_k[b + 1] - k0 && l * EC < a.D) {
-                const V x = *(const V*)(v.row(k0 + j, bh - b * a.Hk) + l * EC);
 #pragma unroll
-                for (int e = 0; e < EC; ++e) most.y = fmaxf(most.y, finite_size((float)x[e]));
-            }
-        }
-        __shared__ float2 waves[4];
-#pragma unroll
-        for (int o = 32; o; o >>= 1) most = make_float2(fmaxf(most.x, __shfl_xor(most.x, o)), fmaxf(most.y, __shfl_xor(most.y, o)));
-        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-#pragma unroll
-            for (int i = 1; i < 4; ++i) most = make_float2(fmaxf(most.x, waves[i].x), fmaxf(most.y, waves[i].y));
-            a.peaks[group_id()] = most;
-        }
+    for (int o = 8; o; o >>= 1) s += __shfl_xor(s, o, 16);
+    if (l == 0) {
+        const float2 st = stats[token * a.Hq + head];
+        // (a row without weights: none whatever the scores)
+        const float by = back_powers(a.scale), power = log2f(st.y) - (F16 ? WEIGHT_POWER : 0);
+        rows[id] = RowNumber<T>::of(st.y == 0.f ? INFINITY : sizeof(T) == 4 ? fmaf(st.x, by, power) : st.x + power / by);
+        rows[a.all_rows + id] = RowNumber<T>::of(s);
     }
 }
 
@@ -385,8 +350,7 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
         own1 = -N::value(rows_at[a.all_rows + mine]);
     }
     constexpr bool F16 = std::is_same<T, f16>::value;
-    const int power = F16 ? slope_power(a) : 0;
-    const float slope = F16 ? ldexpf(1.f, power - WEIGHT_POWER) : 1.f;
+    float slope = SLOPE_START;                        // fp16: what the lane's gradients of weights, 2^WEIGHT_POWER dS, are multiplied by
 
     const int r4 = l >> 2 & 3, c4 = l & 3, g16 = l >> 4 & 1;
     int k_at = (c32 * RS + (h ^ G::swizzle(c32)) * EC) * (int)sizeof(T);
@@ -507,7 +471,7 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
             }
             if constexpr (SUM_A)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] = (KEYS ? dp[e] : dp[e] + own1) * (F16 ? s[e] * slope : s[e]);
+                for (int e = 0; e < 16; ++e) dp[e] = (KEYS ? dp[e] : dp[e] + own1) * s[e];
             const bool whole = all(i);
             unsigned seen = ~0u;
             if (!whole) {
@@ -518,6 +482,24 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
                     if constexpr (SUM_B) s[e] = __int_as_float(__float_as_int(s[e]) & m);
                     if constexpr (SUM_A) dp[e] = __int_as_float(__float_as_int(dp[e]) & m);
                 }
+            }
+            if constexpr (F16 && SUM_A) {
+                float most = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(dp[e]));
+                if (__any(most * slope > SLOPE_MOST)) {
+                    // (both halves of the wave hold parts of a lane's sums)
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    const float now = most * slope > SLOPE_MOST ? slope_factor(most) : slope, less = now / slope;
+                    products_done<T>();
+#pragma unroll
+                    for (int x = 0; x < NC; ++x)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc_a[x][e] *= less;
+                    slope = now;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] *= slope;
             }
             auto add = [&](auto carefully, f32x16* acc, const char* from, const f32x16& weight, int bit) {
                 constexpr bool careful = decltype(carefully)::value;
@@ -651,7 +633,7 @@ __device__ __forceinline__ void back_walk(const BackArgs& a, const int group, Ba
                 }
             }
     };
-    if constexpr (SUM_A) put(da, acc_a, F16 ? ldexpf(a.scale, -power) : a.scale, 0);
+    if constexpr (SUM_A) put(da, acc_a, F16 ? a.scale * (1.f / (1 << WEIGHT_POWER)) / slope : a.scale, 0);
     if constexpr (SUM_B) put(db, acc_b, F16 ? 1.f / (1 << WEIGHT_POWER) : 1.f, 1);
 }
 
@@ -782,7 +764,7 @@ static BackSizes back_sizes(int type, int B, int Hq, int Hk, int D, int max_q, i
 {
     BackSizes s = {};
     s.pitch = ((long long)max_q * (Hq / Hk) + 63) / 64 * 64;
-    s.rows = PEAKS * sizeof(float2) + ((size_t)2 * B * Hk * s.pitch * (type == ZNNI_F32 ? sizeof(float) : sizeof(Pieces)) + 255) & ~(size_t)255;
+    s.rows = ((size_t)2 * B * Hk * s.pitch * (type == ZNNI_F32 ? sizeof(float) : sizeof(Pieces)) + 255) & ~(size_t)255;
     const size_t p0 = back_plan(true, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
     const size_t p1 = back_plan(false, type, B, Hq, Hk, D, max_q, max_k, left, right, sinks).parts;
     s.parts = (p0 + p1) * sizeof(float);
@@ -804,13 +786,8 @@ static znni_status launch_back(BackArgs a, int type, int B, const znni_heads* q,
                                hipStream_t st)
 {
     const Heads<const T> qi = heads_of<const T>(q), ki = heads_of<const T>(k), vi = heads_of<const T>(v), gi = heads_of<const T>(dout);
-    constexpr bool F16 = std::is_same<T, f16>::value;
-    const long long all = a.all_rows, keys = F16 ? (long long)B * a.Hk * a.max_k : 0;
-    long long groups = ((all > keys ? all : keys) + 15) / 16;
-    if (F16 && groups > PEAKS) groups = PEAKS;
-    a.peak_count = F16 ? (int)groups : 0;
-    if (groups) {
-        k_back_rows<T><<<launch_of(groups), dim3(256), 0, st>>>(a, B, gi, heads_of<const T>(out), vi, (const float2*)stats, (typename RowNumber<T>::type*)a.rows);
+    if (a.all_rows) {
+        k_back_rows<T><<<launch_of((a.all_rows + 15) / 16), dim3(256), 0, st>>>(a, gi, heads_of<const T>(out), (const float2*)stats, (typename RowNumber<T>::type*)a.rows);
         if (hipGetLastError() != hipSuccess) return ZNNI_ERR_HIP;
     }
     const BackPlan pk = back_plan(true, type, B, a.Hq, a.Hk, a.D, a.max_q, a.max_k, a.w.left, a.w.right, a.w.sinks);
@@ -907,8 +884,7 @@ znni_status znni_attn_window_backward(int type, int B, int Hq, int Hk, int D, co
     a.pitch = s.pitch;
     a.heads = B * Hk;
     a.all_rows = (long long)B * Hk * s.pitch;
-    a.peaks = (float2*)workspace;
-    a.rows = (const char*)workspace + PEAKS * sizeof(float2);
+    a.rows = (const char*)workspace;
     a.parts = (float*)((char*)workspace + s.rows);
     const hipStream_t st = (hipStream_t)stream;
     switch (type) {
