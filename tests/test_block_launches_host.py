@@ -1,8 +1,11 @@
 """What calls of products, norms and attention's gradients launch (a recorder stands in for the launches; addresses are made up and never used)."""
+import re
+
 import pytest
 
 import launches
 from paper_1606_05688_amd import binding as B
+from test_gpu_linear_tiles import CASES
 
 P, WS, BIG = 1 << 12, 1 << 20, 1 << 50
 
@@ -64,3 +67,27 @@ def test_workspace_of_sums_over_tokens(record, C):
     for T, size, (status, launched) in zip(tokens[1:], sizes[1:], record([norm(B.BF16, T, C, True, True) for T in tokens[1:]])):
         name, grid, _ = launched[0]
         assert status == 0 and "k_norm_back" in name and size >= 3 * grid[0] * grid[1] * C * 4
+
+
+def tile(name):
+    """Edge of the tiles of a launch's kernel."""
+    if "k_gradients" in name:
+        return 64
+    waves_n, waves_m, n, m = (int(x) for x in re.search(r"k_productI\w+?Lb[01]ELb[01]ELi(\d)ELi(\d)ELi(\d)ELi(\d)E", name).groups())
+    assert waves_n * n == waves_m * m
+    return 32 * waves_n * n
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_tiles_of_the_cases_that_name_them(record, case):
+    M, N, K, pad, shift, small, fp32 = CASES[case]
+    for type, kinds in ((B.BF16, small), (B.F16, small), (B.F32, fp32)):
+        forward = ["znni_linear", [["i", type], ["i", M], ["i", N], ["i", K], ["rows", [P, K + pad]], ["rows", [P, K + pad]], ["p", None], ["i", 0], ["rows", None], ["rows", None],
+                                   ["rows", [P, N + pad]], ["p", WS], ["z", BIG], ["p", None]]]
+        calls = [forward, linear_back(type, M, N, K, 0, B.LINEAR_DX), linear_back(type, M, N, K, 0, B.LINEAR_DW)]
+        got = record(calls)
+        assert [status for status, _ in got] == [0, 0, 0]
+        assert tuple(tile(next(n for n, _, _ in launched if "k_product" in n)) for _, launched in got) == kinds
+    # each size of tile is there in each form
+    for form in range(3):
+        assert {c[5][form] for c in CASES} == {64, 128, 256} and 128 in {c[6][form] for c in CASES}
