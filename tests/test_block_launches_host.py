@@ -5,6 +5,7 @@ import pytest
 
 import launches
 from paper_1606_05688_amd import binding as B
+from test_gpu_attn_back_single import CASES as SINGLE
 from test_gpu_linear_tiles import CASES
 
 P, WS, BIG = 1 << 12, 1 << 20, 1 << 50
@@ -91,3 +92,24 @@ def test_tiles_of_the_cases_that_name_them(record, case):
     # each size of tile is there in each form
     for form in range(3):
         assert {c[5][form] for c in CASES} == {64, 128, 256} and 128 in {c[6][form] for c in CASES}
+
+
+def attention_back(type, case):
+    lens, Hq, Hk, D, left, right, sinks = case
+    q, k = ["heads", [P, Hq * D, D]], ["heads", [P, Hk * D, D]]
+    most = [max(n) for n in zip(*lens)]
+    return ["znni_attn_window_backward", [["i", x] for x in (type, len(lens), Hq, Hk, D)] + [q, k, k, q, ["p", P], q, ["p", P], ["p", P]]
+            + [["i", x] for x in (*most, left, right, sinks)] + [["f", 1.0], q, k, k, ["p", WS], ["z", BIG], ["p", None]]]
+
+
+@pytest.mark.parametrize("type", [B.BF16, B.F16])
+def test_weights_of_attention_gradients_are_single_where_rows_see_many_keys(record, type):
+    got = record([attention_back(type, c) for c in SINGLE])
+    assert all(status == 0 for status, _ in got)
+    for case, (_, launched) in zip(SINGLE, got):
+        assert any(re.search(r"k_backI\w+?Lb0E", name) for name, _, _ in launched), case
+    # all widths of heads, dk and dv at once and apart, with a join and without
+    assert {(c[3] + 31) // 32 for c in SINGLE} == {1, 2, 3, 4}
+    assert {any("k_back_join" in name for name, _, _ in launched) for _, launched in got} == {True, False}
+    (_, few), = record([attention_back(type, ([(300, 300)], 2, 1, 64, 100, 0, 0))])
+    assert any(re.search(r"k_backI\w+?Lb1E", name) for name, _, _ in few)
