@@ -107,12 +107,14 @@ class VolumeLayer:
         return x[:, :Hq], x[:, Hq:Hq + Hk], x[:, Hq + Hk:]
 
     def forward(self, x, pos, cu, longest, **window):
-        """x [T, C], the sequences of cu [B + 1] one behind the other, pos [T, 3]; window: left, right, sinks of znni_attn_window."""
+        """x [T, C], the sequences of cu [B + 1] one behind the other (rows behind the last one see nothing), pos [T, 3]; window: left, right, sinks of
+        znni_attn_window."""
         w = self.weights
         a = znni.znni_block_norm(x, pre=w["pre1"])[1]
         q, k, v = self._heads(znni.znni_linear(a, w["wqkv"], w["bqkv"]))
         q, k = znni.znni_rope_axes(q, k, pos, self.freq, self.sections)
-        o, stats = znni.znni_attn_window(q, k, v, cu, cu, longest, longest, stats=True, **window)
+        # (attention leaves rows behind the last sequence as they were, and sums over tokens take them in: zeros, here and for the gradients)
+        o, stats = znni.znni_attn_window(q, k, v, cu, cu, longest, longest, stats=True, out=x.new_zeros(q.shape), **window)
         y = znni.znni_linear(o.view(x.shape), w["wo"])
         h, b = znni.znni_block_norm(x, y, gate=w["gate"], post=w["post"], pre=w["pre2"])
         u, z = znni.znni_linear(b, w["w1"], w["b1"], act="gelu", keep=True)
@@ -126,9 +128,10 @@ class VolumeLayer:
         db, d["w1"], d["b1"] = znni.znni_linear_backward(du, b, w["w1"], z=z, act="gelu")
         dh, dy, d["gate"], d["post"], d["pre2"] = znni.znni_block_norm_backward(dout, db, h, y, gate=w["gate"], post=w["post"], pre=w["pre2"])
         do, d["wo"], _ = znni.znni_linear_backward(dy, o.view(x.shape), w["wo"], bias=False)
-        dqkv = x.new_empty(x.shape[0], (self.Hq + 2 * self.Hk) * self.D)
+        dqkv = x.new_zeros(x.shape[0], (self.Hq + 2 * self.Hk) * self.D)
         dq, dk, dv = self._heads(dqkv)
-        gq, gk, _ = znni.znni_attn_window_backward(do.view(o.shape), q, k, v, o, stats, cu, cu, longest, longest, dv=dv, **window)
+        gq, gk, _ = znni.znni_attn_window_backward(do.view(o.shape), q, k, v, o, stats, cu, cu, longest, longest, dq=x.new_zeros(q.shape),
+                                                   dk=x.new_zeros(k.shape), dv=dv, **window)
         znni.znni_rope_axes(gq, gk, -pos, self.freq, self.sections, out_q=dq, out_k=dk)          # turned back
         da, d["wqkv"], d["bqkv"] = znni.znni_linear_backward(dqkv, a, w["wqkv"])
         dx, _, _, _, d["pre1"] = znni.znni_block_norm_backward(dh, da, x, pre=w["pre1"])
