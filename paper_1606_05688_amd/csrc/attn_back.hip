@@ -12,7 +12,8 @@
 // bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 2100 us in all, 576 TFLOP/s of the five products that it takes, 920 of the eight that run
 // (scores twice for wide heads' dk and dv, and again for dq).  Bound by LDS reads, products and exponentials of two waves a SIMD that take turns but for
 // the meetings at each tile (matrix units 41 % busy, vector units 35 %), no bank conflicts.  fp16, ragged 300 tokens: 37 us, the chain of three launches.  fp32, 2744
-// tokens: 151 us, matrix units of one or two workgroups a unit, 40 of 64 columns useful.
+// tokens: 151 us, matrix units of one or two workgroups a unit, 40 of 64 columns useful.  Registers run out in fp32 for heads of 97 to 128 (196 bytes of scratch a lane) and where
+// weights are two values for heads of 33 to 64 (8 and 48 bytes) and of 97 to 128 (40 and 56).
 #include <initializer_list>
 #include <type_traits>
 

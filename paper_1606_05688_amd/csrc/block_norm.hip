@@ -4,7 +4,8 @@
 //   gradients: dx = dh + n'(h)[pre dz],   n'(a)[g] = r (g - n(a) mean(g n(a)))   (centred: less its mean);
 //   dgate = scale dx post n(y),   dy = n'(y)[scale dx gate post],   dpost = sum over tokens of scale dx gate n(y),   dpre = of dz n(h)
 //
-// Bound by memory: every tensor is read or written once.  Rows stay in registers, 8 to 32 elements a lane, one to sixteen waves a row.
+// Bound by memory: every tensor is read or written once.  Rows stay in registers, 8 to 32 elements a lane, one to sixteen waves a row (but for gradients past
+// 8192 channels, whose rows, weights and sums are more than sixteen waves hold: 400 to 464 bytes of scratch a lane, 4096 x 16384 bf16 824 us, 1 TB/s).
 // bf16, 32768 x 2048, a gate for each token: 117 us, 5.7 TB/s (a large copy reaches 5.2 to 6.2 by card).  Gradients, one gate: 183 to 194 us, 4.2 to 4.4
 // TB/s, and 6 for the sums over tokens: a row over four waves, four workgroups a compute unit, three meetings a row; 32 elements a lane and a wave a
 // row leave two waves a SIMD and took 285; the next row's reads ahead of this one's work cost a workgroup and took 209.
