@@ -12,8 +12,8 @@
 // bf16, 16384 tokens, window of 4096, heads 16 of 4 x 128: 2100 us in all, 576 TFLOP/s of the five products that it takes, 920 of the eight that run
 // (scores twice for wide heads' dk and dv, and again for dq).  Bound by LDS reads, products and exponentials of two waves a SIMD that take turns but for
 // the meetings at each tile (matrix units 41 % busy, vector units 35 %), no bank conflicts.  fp16, ragged 300 tokens: 37 us, the chain of three launches.  fp32, 2744
-// tokens: 151 us, matrix units of one or two workgroups a unit, 40 of 64 columns useful.  Registers run out in fp32 for heads of 97 to 128 (196 bytes of scratch a lane) and where
-// weights are two values for heads of 33 to 64 (8 and 48 bytes) and of 97 to 128 (40 and 56).
+// tokens: 151 us, matrix units of one or two workgroups a unit, 40 of 64 columns useful.  Registers run out in fp32 for heads of 97 to 128 (196 bytes of
+// scratch a lane) and where weights are two values for heads of 33 to 64 (bf16 8 bytes, fp16 48) and of 97 to 128 (40 and 56).
 #include <initializer_list>
 #include <type_traits>
 
@@ -93,7 +93,8 @@ struct RowNumber {
 
 // Sixteen lanes a row, 16 bytes a lane at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, Heads<const T> dout, Heads<const T> out, const float2* __restrict__ stats, typename RowNumber<T>::type* __restrict__ rows)
+__global__ __launch_bounds__(256) void k_back_rows(BackArgs a, Heads<const T> dout, Heads<const T> out, const float2* __restrict__ stats,
+                                                   typename RowNumber<T>::type* __restrict__ rows)
 {
     constexpr bool F16 = std::is_same<T, f16>::value;
     constexpr int EC = 16 / sizeof(T);
